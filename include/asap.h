@@ -227,6 +227,144 @@ asap_status asap_compact_kv(asap_ctx *ctx, const int32_t *src_row, const int32_t
                             int32_t rows_capacity, int32_t src_rows, size_t row_bytes, int32_t n_tensors,
                             const void *const *src, void *const *dst, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * After the prefill: new tokens over the shortened cache.  asap_compact_kv leaves the rows of the
+ * shortened sequences; the calls below rotate and append new rows, attend over the cache, weigh its
+ * rows by the attention they receive, and keep it within a budget by those weights.  Element type of
+ * queries, keys and values: bf16 or fp16.  Strides are in elements.  Bad entries of the per-sequence
+ * device arrays are recorded for asap_check like those of the other calls, and the sequence (or group,
+ * with its sequences) is skipped: its outputs stay as they are. */
+enum { ASAP_BF16 = 0, ASAP_FP16 = 1 };
+
+/* Rotary positions.  The first 2 * n_pairs elements of every head are rotated in pairs,
+ *     (a, b) -> magnitude * (a cos f - b sin f, b cos f + a sin f),   f = 2 pi * pos * turns[i] / 2^64,
+ * elements i and i + n_pairs (half layout) or 2i and 2i + 1 (interleaved); the rest passes through.
+ * The product pos * turns[i] keeps its low 64 bits, which are the fraction of a turn: positions may be
+ * negative or as far as an int32 goes, and the angle is as exact at the last as at the first. */
+enum { ASAP_ROPE_PLAIN = 0, ASAP_ROPE_LINEAR = 1, ASAP_ROPE_NTK = 2, ASAP_ROPE_YARN = 3, ASAP_ROPE_BANDS = 4 };
+typedef struct {
+  int32_t n_pairs;      /* 1 .. 128 */
+  int32_t interleaved;
+  float magnitude;
+  int32_t reserved;
+  uint64_t turns[128];  /* turns per position of pair i, in units of 2^-64 */
+} asap_rope_plan;
+
+/* Fills a plan (host memory; no GPU needed).  Pair i of rot_dim / 2 turns by theta^(-2i / rot_dim) radians per
+ * position.  For contexts `factor` times as long as `original_positions`:
+ *   PLAIN   unchanged (factor is not used)
+ *   LINEAR  every frequency divided by factor
+ *   NTK     theta * factor^(rot_dim / (rot_dim - 2)) in place of theta (rot_dim > 2)
+ *   YARN    pairs that turn more than `fast` times over the original positions keep their frequency, those that
+ *           turn less than `slow` times are divided by factor, a linear ramp over the pair index between (its ends
+ *           rounded outwards to whole pairs); magnitude = 0.1 ln(factor) + 1
+ *   BANDS   the same division, the ramp linear in the number of turns; magnitude 1
+ * Typical bounds: YARN fast = 32, slow = 1; BANDS fast = 4, slow = 1.  Errors are described by asap_last_error(NULL). */
+asap_status asap_rope_make(asap_rope_plan *plan, int32_t rot_dim, int32_t interleaved, int32_t scaling, double theta,
+                           double factor, double original_positions, double fast, double slow);
+
+typedef struct {
+  const void *src;      /* [n_rows, heads, head_dim] */
+  void *dst;            /* [n_rows or dst_rows, heads, head_dim] */
+  int32_t heads;
+  int32_t rotate;       /* 0: copied (the values that go into the cache beside the rotated keys) */
+  int32_t mapped;       /* 1: row r goes to row dst_map[r] of dst */
+  int32_t reserved;
+  int64_t src_row, src_head, dst_row, dst_head;   /* strides, multiples of 8 */
+} asap_rope_tensor;
+
+typedef struct {
+  int32_t n_rows, head_dim, dtype; /* head_dim: a multiple of 8, at most 256, at least 2 * n_pairs */
+  int32_t inverse;                 /* 1: rotates by -f (the transpose: undoes a rotation of magnitude 1) */
+  int32_t n_tensors;               /* 1 .. 4 */
+  int32_t dst_rows;                /* rows of the mapped destinations */
+  const int32_t *pos;              /* [n_rows] */
+  const int32_t *dst_map;          /* [n_rows]; may be NULL if no tensor is mapped.  An entry outside [0, dst_rows) writes nothing
+                                      (a padded row); entries must not repeat */
+  const asap_rope_tensor *tensors; /* HOST array */
+} asap_rope_args;
+
+/* Rotates (and copies) up to four tensors with the same positions in one launch: the queries, the keys into their cache rows,
+ * the values into theirs.  src == dst with the same strides, unmapped, rotates in place; other overlaps of a tensor's source and
+ * destination are refused.  n_rows == 0 does nothing. */
+asap_status asap_rope(asap_ctx *ctx, const asap_rope_plan *plan, const asap_rope_args *args, void *stream);
+
+/* Attention of new rows over a cache.  Sequence b owns rows start[b] .. start[b] + len[b] - 1 of the cache, its nq = q_cu[b + 1] -
+ * q_cu[b] query rows are the last nq of them: query row t admits the own rows 0 .. len[b] - nq + t.  Sequences group_cu[g] ..
+ * group_cu[g + 1] - 1 share the prefix_len[g] rows from prefix_start[g], which all of their query rows admit and which are read
+ * once for all of them.  For query head h, with key/value head h / (H / kv_heads),
+ *     out[t, h, :] = sum_j p_j v_j,   p = Softmax_j(scale * q . k_j) over all admitted rows,   lse[t, h] = ln sum_j exp(scale * q . k_j)
+ * and, if `weights` is given, weights[j] += (1 / H) sum over the query rows and heads of p_j, for every cache row j (in a fixed
+ * order: a call gives the same bits every time).  A query row that admits nothing gets out = 0 and lse = -infinity.  Rows that
+ * no query row admits are not looked at, whatever they hold; a row that only later query rows admit does not touch earlier ones.
+ * Probabilities enter the second product rounded to the element type; logits, sums and outputs before the last rounding are fp32. */
+typedef struct {
+  int32_t B, H, kv_heads, head_dim, dtype;  /* head_dim must be 128; kv_heads divides H */
+  int32_t n_q;                              /* query rows in total, q_cu[B] */
+  int32_t max_q, max_len, max_prefix;       /* host-known bounds of the query rows, own rows and prefix rows */
+  int32_t n_groups;                         /* 0: no prefixes.  B + n_groups <= 1024 */
+  int32_t cache_rows;                       /* rows of k and v */
+  float scale;                              /* 0: 1 / sqrt(head_dim) */
+  int64_t q_row, q_head, out_row, out_head, kv_row, kv_head;  /* strides, multiples of 8; k and v have the same */
+  const int32_t *q_cu;                      /* [B + 1]; NULL: one query row per sequence */
+  const int32_t *start, *len;               /* [B] */
+  const int32_t *group_cu, *prefix_start, *prefix_len; /* [n_groups + 1], [n_groups], [n_groups]; sequences outside every group
+                                               have no prefix */
+  const void *q;                            /* [n_q, H, head_dim] */
+  const void *k, *v;                        /* [cache_rows, kv_heads, head_dim] */
+  void *out;                                /* [n_q, H, head_dim] */
+  float *lse;                               /* [n_q, H], may be NULL */
+  float *weights;                           /* [cache_rows], may be NULL; rows of different sequences and prefixes must not overlap then */
+} asap_cache_attention_args;
+
+/* `scratch`: caller-owned device memory of at least asap_cache_attention_scratch_bytes bytes (a function of the sizes and of whether
+ * weights are given; 0 for arguments that the call refuses), 256-byte aligned; nothing is kept in it between calls.  Calls that may
+ * run at the same time need scratch of their own.  May be recorded by a stream capture; a replay uses the lengths that the arrays
+ * hold then, within the bounds given. */
+size_t asap_cache_attention_scratch_bytes(const asap_ctx *ctx, const asap_cache_attention_args *args);
+asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args *args, void *scratch, size_t scratch_bytes,
+                                 void *stream);
+
+/* Cuts every sequence of a cache back to its `keep` best rows, in their order.  A sequence of at most `keep` rows stays whole.
+ * Rows rank: held rows first (the first `sink` rows of the sequence, and those with pos > newest - recent, newest = the largest
+ * position of the sequence), then by weight, largest first (-0 equals +0, NaN is below everything); lower row first among
+ * equals.  For row i of the kept ones, each of the n_tensors (0 .. 64) tensors moves row start[b] + keep_idx[b][i] to row
+ * dst_start[b] + i, and weights and pos likewise.  dst[t] == src[t] moves in place (dst_start NULL then); partly overlapping tensors are
+ * refused. */
+typedef struct {
+  int32_t B, max_len, keep, sink, recent;  /* 0 <= sink, 0 <= recent, sink + recent <= keep, 0 < keep */
+  int32_t rows, dst_rows;                  /* rows of the sources / of the destinations */
+  int32_t n_tensors;
+  size_t row_bytes;                        /* a multiple of 16 */
+  const int32_t *start, *len;              /* [B] */
+  const int32_t *dst_start;                /* [B]; NULL: start */
+  const float *weights;                    /* [rows] */
+  const int32_t *pos;                      /* [rows]; NULL: a row's number in its sequence */
+  int32_t *keep_idx;                       /* [B, keep] kept rows, sequence-relative, ascending; -1 behind the last */
+  int32_t *new_len;                        /* [B]; may be `len` */
+  float *dst_weights;                      /* [dst_rows], may be NULL or `weights` */
+  int32_t *dst_pos;                        /* [dst_rows], may be NULL or `pos` */
+  const void *const *src;                  /* HOST arrays of device pointers, [rows, row_bytes] and [dst_rows, row_bytes] */
+  void *const *dst;
+} asap_cache_evict_args;
+asap_status asap_cache_evict(asap_ctx *ctx, const asap_cache_evict_args *args, void *stream);
+
+/* The row for every sequence's next token: row[b] = start[b] + len[b] and len[b] grows by one, or, where len[b] == capacity, the
+ * row that asap_cache_evict with keep = capacity - 1 and newest = new_pos[b] - 1 would drop.  weights[row] becomes 0 and
+ * pos[row] new_pos[b].  row[] is what asap_rope takes as dst_map.  Once a row has been reused the rows of a sequence are no longer in
+ * the order of their positions: a call of asap_cache_attention with more than one query row per sequence needs them in order. */
+typedef struct {
+  int32_t B, capacity, sink, recent;       /* sink + recent < capacity */
+  int32_t rows;                            /* rows of weights and pos */
+  const int32_t *start;                    /* [B] */
+  int32_t *len;                            /* [B] */
+  float *weights;                          /* [rows] */
+  int32_t *pos;                            /* [rows] */
+  const int32_t *new_pos;                  /* [B] */
+  int32_t *row;                            /* [B]; -1 for a sequence that is skipped */
+} asap_cache_slot_args;
+asap_status asap_cache_slot(asap_ctx *ctx, const asap_cache_slot_args *args, void *stream);
+
 /* Reads the device status word (one 4-byte copy after synchronising `stream`).  ASAP_OK, or
  * ASAP_ERR_DEVICE with the reason in asap_last_error; the word is cleared.  After a time-out bit
  * (a bounded wait ran out in a tensor-core kernel) every result enqueued on the context since

@@ -15,6 +15,7 @@
 #include "kernels_stream.cuh"
 #include "kernels_tc.cuh"
 #include "kernels_attn.cuh"
+#include "kernels_cache.cuh"
 
 using namespace asap;
 
@@ -746,6 +747,8 @@ routing:
 
 }  // namespace
 
+#include "cache_api.cuh"
+
 // =================================================================================================
 // C ABI
 // =================================================================================================
@@ -847,6 +850,8 @@ asap_status asap_init(asap_ctx **ctx_out, int device, size_t max_total_tokens, i
   if (e == cudaSuccess) e = cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(route_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, AT_SMEM_BYTES);
+  for (auto kernel : {ca_stream_kernel<false>, ca_stream_kernel<true>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ca_smem_bytes(CA_MAX_SEGMENTS));
   if (e == cudaSuccess && ctx->sim_cluster) {
     // the cluster form of the sliced similarity launch needs eight co-resident blocks of up to 195 KB each in one
     // cluster; where the device (or the partition of it this process sees) cannot place one, the form is not used
@@ -1034,19 +1039,20 @@ asap_status asap_check(asap_ctx *ctx, void *stream) {
   if (e != cudaSuccess) return fail(ctx, ASAP_ERR_CUDA, "asap_check: %s", cudaGetErrorString(e));
   if (word == 0) { ctx->err[0] = 0; return ASAP_OK; }
   cudaMemsetAsync(ctx->status, 0, sizeof(uint32_t), st);
-  if (word & (STATUS_MASS_TIMEOUT | STATUS_SCORE_TIMEOUT | STATUS_SIM_TIMEOUT | STATUS_ATTN_TIMEOUT)) {
+  if (word & (STATUS_MASS_TIMEOUT | STATUS_SCORE_TIMEOUT | STATUS_SIM_TIMEOUT | STATUS_ATTN_TIMEOUT | STATUS_CACHE_TIMEOUT)) {
     // blocks that gave up did not finish the hand-shakes that leave the counters at zero
     cudaMemsetAsync(ctx->arena + ctx->counters_off, 0, ctx->counters_bytes, st);
     cudaMemsetAsync(ctx->arena + ctx->tiles_off, 0, ctx->tiles_bytes, st);
   }
   cudaStreamSynchronize(st);
-  return fail(ctx, ASAP_ERR_DEVICE, "device status 0x%x:%s%s%s%s%s%s", word,
+  return fail(ctx, ASAP_ERR_DEVICE, "device status 0x%x:%s%s%s%s%s%s%s", word,
               (word & STATUS_BAD_SAMPLE) ? " a per-sample span failed validation (sample skipped);" : "",
               (word & STATUS_OUT_CAPACITY) ? " shortened batch exceeds out_rows_capacity (nothing written);" : "",
               (word & STATUS_MASS_TIMEOUT) ? " a wait timed out in the mass kernel;" : "",
               (word & STATUS_SCORE_TIMEOUT) ? " a wait timed out in the score kernel;" : "",
               (word & STATUS_SIM_TIMEOUT) ? " a wait timed out in the similarity kernel;" : "",
-              (word & STATUS_ATTN_TIMEOUT) ? " a wait timed out in the attention kernel;" : "");
+              (word & STATUS_ATTN_TIMEOUT) ? " a wait timed out in the attention kernel;" : "",
+              (word & STATUS_CACHE_TIMEOUT) ? " a wait timed out in the cache attention kernel;" : "");
 }
 
 asap_status asap_debug_wait_limit(asap_ctx *ctx, long long cycles) {

@@ -1,0 +1,1073 @@
+// New tokens over a key / value cache: rotary positions with the rows appended, attention of the new rows over a shared prefix
+// and their own rows, accumulated attention weights, and eviction by those weights.
+//
+//   rope_kernel         (a, b) -> m (a cos f - b sin f, b cos f + a sin f) for up to four tensors of the same rows
+//   ca_stream_kernel    partial softmax sums of (query rows x a range of keys), keys and values streamed once
+//   ca_join_kernel      partial sums of a row -> output and ln of the sum
+//   ca_weight_kernel    probabilities summed over query rows and heads, per key
+//   evict_select_kernel rows kept by rank, their weights and positions
+//   evict_move_kernel   kept rows of the cache tensors
+//   slot_kernel         the row of every sequence's next token
+#pragma once
+
+#include <cuda_fp16.h>
+#include <limits.h>
+
+#include "common.cuh"
+
+namespace asap {
+
+enum : uint32_t { STATUS_CACHE_TIMEOUT = 64u };   // a bounded wait ran out in a cache attention kernel
+
+__device__ __forceinline__ void ld_prev8(const void *p, uint4 &v) {
+  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2_t(float a, float b) {
+  if constexpr (F16) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+  } else {
+    return pack2_rn(a, b);
+  }
+}
+template <bool F16>
+__device__ __forceinline__ float2 unpack2_t(uint32_t w) {
+  if constexpr (F16) return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+  else return make_float2(bf16_lo(w), bf16_hi(w));
+}
+
+// =======================================================================================
+// Rotary positions
+// =======================================================================================
+constexpr int ROPE_THREADS = 256;
+constexpr int ROPE_MAX_PAIRS = 128;
+constexpr int ROPE_MAX_ROWS = 4;       // rows of a block
+
+struct RopeTensor {
+  const uint16_t *src;
+  uint16_t *dst;
+  int heads, rotate, mapped;
+  long long src_row, src_head, dst_row, dst_head;
+};
+struct RopeArgs {
+  RopeTensor t[4];
+  int n_tensors, n_rows, rows_per_block, head_dim, n_pairs, interleaved, dst_rows;
+  float magnitude, sign;
+  const int *pos, *map;
+  unsigned long long turns[ROPE_MAX_PAIRS];
+};
+
+// One element pair, or eight elements at a time (VEC) where the pairs allow it: half layout n_pairs % 8 == 0, interleaved
+// n_pairs % 4 == 0.  The angles of a row are taken once for all its heads: pos * turns modulo 2^64 is the fraction of a turn, whose
+// upper 32 bits, as a signed number, are the angle in (-1/2, 1/2] turns (2^-32 turns off at most); sincospi takes it in fp32.
+template <bool F16, bool VEC>
+__global__ void __launch_bounds__(ROPE_THREADS)
+rope_kernel(const __grid_constant__ RopeArgs a) {
+  __shared__ __align__(16) float cs[ROPE_MAX_ROWS][2][ROPE_MAX_PAIRS];
+  __shared__ int dst_of[ROPE_MAX_ROWS];
+  pdl_enter();
+  const int row0 = blockIdx.x * a.rows_per_block;
+  const int rows = min(a.rows_per_block, a.n_rows - row0);
+  for (int i = threadIdx.x; i < rows * a.n_pairs; i += ROPE_THREADS) {
+    const int r = i / a.n_pairs, p = i - r * a.n_pairs;
+    const long long pos = ld_prev(a.pos + row0 + r);
+    const unsigned long long turn = (unsigned long long)pos * a.turns[p];
+    const float half_turns = (float)(int)(turn >> 32) * 0x1p-31f;      // in units of pi
+    float s, c;
+    sincospif(half_turns, &s, &c);
+    cs[r][0][p] = c * a.magnitude;
+    cs[r][1][p] = s * a.magnitude * a.sign;
+  }
+  if (threadIdx.x < rows) {
+    int d = row0 + threadIdx.x;
+    if (a.map) {
+      d = ld_prev(a.map + d);
+      if (d >= a.dst_rows) d = -1;
+    }
+    dst_of[threadIdx.x] = d;
+  }
+  __syncthreads();
+  const int P = a.n_pairs, rot = 2 * P;
+  const RopeTensor &t = a.t[blockIdx.y];
+  // tasks of a head: rotated pieces first, then pieces that pass through
+  const int n_rot = t.rotate ? (VEC ? (a.interleaved ? P / 4 : P / 8) : P) : 0;
+  const int n_pass = VEC ? (a.head_dim - (t.rotate ? rot : 0)) / 8 : a.head_dim - (t.rotate ? rot : 0);
+  const int per_head = n_rot + n_pass;
+  const int lanes = ROPE_THREADS / per_head * per_head;      // threads at work: whole heads
+  const int v = threadIdx.x % per_head;
+  if (threadIdx.x >= lanes) return;
+  for (int j = threadIdx.x / per_head; j < rows * t.heads; j += ROPE_THREADS / per_head) {
+    const int r = j / t.heads, h = j - r * t.heads;
+    const int d = t.mapped ? dst_of[r] : row0 + r;
+    if (d < 0) continue;
+    const uint16_t *src = t.src + (long long)(row0 + r) * t.src_row + (long long)h * t.src_head;
+    uint16_t *dst = t.dst + (long long)d * t.dst_row + (long long)h * t.dst_head;
+    if (v >= n_rot) {
+      const int e = (t.rotate ? rot : 0) + (v - n_rot) * (VEC ? 8 : 1);
+      if constexpr (VEC) {
+        uint4 x;
+        ld_prev8(src + e, x);
+        *reinterpret_cast<uint4 *>(dst + e) = x;
+      } else {
+        dst[e] = *reinterpret_cast<const volatile uint16_t *>(src + e);
+      }
+      continue;
+    }
+    if constexpr (VEC) {
+      if (a.interleaved) {
+        uint4 x;
+        ld_prev8(src + v * 8, x);
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        const float4 c = *reinterpret_cast<const float4 *>(&cs[r][0][v * 4]), s = *reinterpret_cast<const float4 *>(&cs[r][1][v * 4]);
+        const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 p = unpack2_t<F16>(w[e]);
+          w[e] = pack2_t<F16>(p.x * cc[e] - p.y * ss[e], p.y * cc[e] + p.x * ss[e]);
+        }
+        *reinterpret_cast<uint4 *>(dst + v * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+        uint4 x, y;
+        ld_prev8(src + v * 8, x);
+        ld_prev8(src + P + v * 8, y);
+        uint32_t wx[4] = {x.x, x.y, x.z, x.w}, wy[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 p = unpack2_t<F16>(wx[e]), q = unpack2_t<F16>(wy[e]);
+          const float2 c = *reinterpret_cast<const float2 *>(&cs[r][0][v * 8 + 2 * e]), s = *reinterpret_cast<const float2 *>(&cs[r][1][v * 8 + 2 * e]);
+          wx[e] = pack2_t<F16>(p.x * c.x - q.x * s.x, p.y * c.y - q.y * s.y);
+          wy[e] = pack2_t<F16>(q.x * c.x + p.x * s.x, q.y * c.y + p.y * s.y);
+        }
+        *reinterpret_cast<uint4 *>(dst + v * 8) = make_uint4(wx[0], wx[1], wx[2], wx[3]);
+        *reinterpret_cast<uint4 *>(dst + P + v * 8) = make_uint4(wy[0], wy[1], wy[2], wy[3]);
+      }
+    } else {
+      const int ea = a.interleaved ? 2 * v : v, eb = a.interleaved ? 2 * v + 1 : v + P;
+      const uint32_t w = *reinterpret_cast<const volatile uint16_t *>(src + ea) | (uint32_t)*reinterpret_cast<const volatile uint16_t *>(src + eb) << 16;
+      const float2 p = unpack2_t<F16>(w);
+      const float c = cs[r][0][v], s = cs[r][1][v];
+      const uint32_t o = pack2_t<F16>(p.x * c - p.y * s, p.y * c + p.x * s);
+      dst[ea] = (uint16_t)o;
+      dst[eb] = (uint16_t)(o >> 16);
+    }
+  }
+}
+
+// =======================================================================================
+// Attention over the cache
+// =======================================================================================
+// A segment is a run of cache rows with the query rows that look at it: segment g < G is the prefix of group g with all query
+// rows of its sequences, segment G + b the own rows of sequence b.  Per key / value head the R = (query rows) * (H / kv_heads)
+// stacked rows of a segment are cut into row tiles of CA_ROWS, the keys that a row tile admits into tiles of CA_KEYS.  All key
+// tiles of all row tiles, heads and segments are numbered through, and every block takes an equal range of numbers: lengths may be
+// as ragged as they like, and the host needs to know none of them.  A row tile whose key tiles lie in one block is complete there;
+// otherwise each block leaves a partial result (maximum, sum, weighted values) and the join adds them up in order.
+constexpr int CA_ROWS = 16, CA_KEYS = 64;
+constexpr int CA_CONSUMERS = 4;                           // warps; each takes 16 keys of a tile
+constexpr int CA_THREADS = 32 * (CA_CONSUMERS + 1);       // and the copying warp
+constexpr int CA_STAGES = 3;
+constexpr int CA_BLOCK_BYTES = CA_KEYS * 128;             // 64 keys x 64 columns
+constexpr int CA_STAGE_BYTES = 4 * CA_BLOCK_BYTES;        // K and V
+constexpr int CA_JOIN_BYTES = 4 * 4 * 128 * 4;            // the warps' sums of an item, a piece at a time
+constexpr int CA_MAX_SEGMENTS = 1024;
+constexpr long long CA_WAIT_LIMIT = 2000000000LL;
+
+struct CacheArgs {
+  int B, G, H, kv, rep;                    // rep = H / kv
+  int n_q, max_q, max_len, max_prefix, cache_rows;
+  long long q_row, q_head, out_row, out_head;
+  const int *q_cu, *start, *len, *group_cu, *prefix_start, *prefix_len;
+  const uint16_t *q;
+  uint16_t *out;
+  float *lse, *weights;
+  float scale_log2;                        // scale * log2(e)
+  // scratch
+  long long *plan;                         // [0]: all tiles, [1]: tiles per block, [2 + s]: first tile of segment s
+  int2 *row_owner;                         // [n_q] (sequence, group or -1) of a query row
+  float2 *rec_ml, *full_ml;                // partial results: two per block and row of a tile; [2][n_q * H] (prefix, own) complete ones
+  float *rec_o, *full_o;                   // 128 values each
+  float *lse2;                             // [n_q * H] log2 of a row's sum of 2^x; +inf: the row adds no weight
+  float *logits;                           // [n_q * H, pitch] x = scale * log2(e) * q.k; prefix keys first, own keys from own_off on
+  long long pitch;
+  int own_off;
+  uint32_t *status;
+  long long wait_limit;
+};
+
+struct CaSeg {
+  int q0, nq;          // query rows
+  int row0, keys;      // cache rows
+  int causal;          // own rows
+  bool valid;
+};
+
+__device__ __forceinline__ int ca_qcu(const CacheArgs &a, int b) { return a.q_cu ? ld_prev(a.q_cu + b) : b; }
+
+__device__ __forceinline__ CaSeg ca_segment(const CacheArgs &a, int s) {
+  CaSeg g;
+  if (s < a.G) {
+    const int b0 = ld_prev(a.group_cu + s), b1 = ld_prev(a.group_cu + s + 1);
+    g.row0 = ld_prev(a.prefix_start + s); g.keys = ld_prev(a.prefix_len + s);
+    g.causal = 0;
+    g.valid = b0 >= 0 && b0 <= b1 && b1 <= a.B && g.keys <= a.max_prefix;
+    g.q0 = g.valid ? ca_qcu(a, b0) : 0;
+    g.nq = g.valid ? ca_qcu(a, b1) - g.q0 : 0;
+    g.valid = g.valid && (long long)g.nq <= (long long)(b1 - b0) * a.max_q;
+  } else {
+    const int b = s - a.G;
+    g.row0 = ld_prev(a.start + b); g.keys = ld_prev(a.len + b);
+    g.q0 = ca_qcu(a, b); g.nq = ca_qcu(a, b + 1) - g.q0;
+    g.causal = 1;
+    g.valid = g.keys <= a.max_len && g.nq <= a.max_q;
+  }
+  g.valid = g.valid && g.keys >= 0 && g.row0 >= 0 && (long long)g.row0 + g.keys <= a.cache_rows && g.q0 >= 0 && g.nq >= 0 &&
+            g.q0 <= a.n_q && (long long)g.q0 + g.nq <= a.n_q;
+  if (!g.valid) g.nq = g.keys = 0;
+  return g;
+}
+// group of a sequence: -1 none, -2 one that failed validation
+__device__ __forceinline__ int ca_group(const CacheArgs &a, int b) {
+  int lo = 0, hi = a.G;                    // the last g with group_cu[g] <= b
+  if (a.G == 0 || ld_prev(a.group_cu) > b) return -1;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (ld_prev(a.group_cu + mid) <= b) lo = mid;
+    else hi = mid;
+  }
+  if (b >= ld_prev(a.group_cu + lo + 1)) return -1;
+  return ca_segment(a, lo).valid ? lo : -2;
+}
+// keys that stacked row i of the segment admits
+__device__ __forceinline__ int ca_admitted(const CacheArgs &a, const CaSeg &g, int i) {
+  if (!g.causal) return g.keys;
+  const int n = g.keys - g.nq + 1 + i / a.rep;
+  return max(0, min(g.keys, n));
+}
+__device__ __forceinline__ int ca_row_tiles(const CacheArgs &a, const CaSeg &g) { return (g.nq * a.rep + CA_ROWS - 1) / CA_ROWS; }
+// key tiles of row tile rt
+__device__ __forceinline__ int ca_key_tiles(const CacheArgs &a, const CaSeg &g, int rt) {
+  const int last = min((rt + 1) * CA_ROWS, g.nq * a.rep) - 1;
+  return (ca_admitted(a, g, last) + CA_KEYS - 1) / CA_KEYS;
+}
+// key tiles of the first `n` row tiles
+__device__ __forceinline__ long long ca_tiles_before(const CacheArgs &a, const CaSeg &g, int n) {
+  if (!g.causal) return (long long)n * ((g.keys + CA_KEYS - 1) / CA_KEYS);
+  long long t = 0;
+  for (int rt = 0; rt < n; ++rt) t += ca_key_tiles(a, g, rt);
+  return t;
+}
+
+// The work of a block, item by item (an item: a range of key tiles of one row tile).  Copying warp and consumers walk alike.
+struct CaItem {
+  CaSeg g;
+  int seg, head, rt;
+  int kt0, kt1, kt_all;    // key tiles of this block, and of the row tile
+};
+struct CaWalk {
+  long long t, end;        // tile numbers left
+  int seg, head, rt, kt;
+  CaSeg g;
+  __device__ __forceinline__ void begin(const CacheArgs &a, const long long *off, int n_seg, long long t0, long long t1) {
+    t = t0; end = t1;
+    if (t >= end) return;
+    int lo = 0, hi = n_seg;                // off[lo] <= t < off[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (off[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    seg = lo;
+    g = ca_segment(a, seg);
+    const long long per_head = (off[seg + 1] - off[seg]) / a.kv;
+    long long u = t - off[seg];
+    head = (int)(u / per_head);
+    u -= head * per_head;
+    rt = 0;
+    if (!g.causal) {
+      const int n = ca_key_tiles(a, g, 0);
+      rt = (int)(u / n);
+      kt = (int)(u - (long long)rt * n);
+    } else {
+      int n;
+      while (u >= (n = ca_key_tiles(a, g, rt))) { u -= n; ++rt; }
+      kt = (int)u;
+    }
+  }
+  __device__ __forceinline__ bool next(const CacheArgs &a, const long long *off, CaItem &it) {
+    if (t >= end) return false;
+    it.g = g; it.seg = seg; it.head = head; it.rt = rt;
+    it.kt_all = ca_key_tiles(a, g, rt);
+    it.kt0 = kt;
+    it.kt1 = (int)min((long long)it.kt_all, kt + (end - t));
+    t += it.kt1 - it.kt0;
+    if (t < end) {                         // the next row tile that has keys
+      kt = 0;
+      do {
+        if (++rt >= ca_row_tiles(a, g)) {
+          rt = 0;
+          if (++head >= a.kv) {
+            head = 0;
+            do ++seg; while (off[seg + 1] <= t);
+            g = ca_segment(a, seg);
+          }
+        }
+      } while (ca_key_tiles(a, g, rt) == 0);
+    }
+    return true;
+  }
+};
+
+// First tile number of every segment into off[0 .. n_seg] (shared memory); all threads of the block.
+template <int THREADS>
+__device__ __forceinline__ void ca_plan(const CacheArgs &a, long long *off, int n_seg, long long *warp_part) {
+  const int per = (n_seg + THREADS - 1) / THREADS, s0 = min(n_seg, (int)threadIdx.x * per), s1 = min(n_seg, s0 + per);
+  long long mine = 0;
+  for (int s = s0; s < s1; ++s) {
+    const CaSeg g = ca_segment(a, s);
+    const long long n = a.kv * ca_tiles_before(a, g, ca_row_tiles(a, g));
+    off[s + 1] = n;
+    mine += n;
+    if (!g.valid && blockIdx.x == 0) atomicOr(a.status, (uint32_t)STATUS_BAD_SAMPLE);
+  }
+  long long scan = mine;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, scan, o);
+    if (lane >= o) scan += v;
+  }
+  if (lane == 31) warp_part[warp] = scan;
+  __syncthreads();
+  long long base = scan - mine;
+  for (int w = 0; w < warp; ++w) base += warp_part[w];
+  for (int s = s0; s < s1; ++s) {
+    const long long n = off[s + 1];
+    base += n;
+    off[s + 1] = base;                     // (its own entries only)
+  }
+  if (threadIdx.x == 0) off[0] = 0;
+  __syncthreads();
+}
+
+// Where the partial result of row tile (seg, head, rt) that block c leaves lies: record 2c if the row tile holds the block's first
+// tile, else 2c + 1 (it then runs past the block's last one).
+struct CaPlace {
+  long long first, last;   // tile numbers of the row tile
+  int c0, c1;              // blocks
+};
+__device__ __forceinline__ CaPlace ca_place(long long first, int n, long long chunk) {
+  CaPlace p;
+  p.first = first; p.last = first + n - 1;
+  p.c0 = (int)(p.first / chunk);
+  p.c1 = (int)(p.last / chunk);
+  return p;
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <bool F16>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (F16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void tma_load_3d_w(uint32_t smem_dst, const void *tmap, uint32_t bar, int32_t x, int32_t y, int32_t z, uint32_t leader) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5}], [%2];\n\t}"
+      ::"r"(smem_dst), "l"(tmap), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ bool not_finite16(uint32_t w, bool f16) {        // either half is an infinity or NaN
+  const uint32_t e = f16 ? 0x7c00u : 0x7f80u;
+  return (w & e) == e || ((w >> 16) & e) == e;
+}
+
+struct CaBook {
+  uint64_t full[CA_STAGES], empty[CA_STAGES];
+  long long warp_part[8];
+  int abort_flag;
+  float2 ml[CA_CONSUMERS][CA_ROWS];
+};
+
+template <bool F16>
+__global__ void __launch_bounds__(CA_THREADS, 2)
+ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CacheArgs a) {
+  extern __shared__ __align__(1024) uint8_t ca_smem[];
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  float *join = reinterpret_cast<float *>(ca_smem + CA_STAGES * CA_STAGE_BYTES);
+  CaBook *bk = reinterpret_cast<CaBook *>(ca_smem + CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES);
+  long long *off = reinterpret_cast<long long *>(bk + 1);
+  const uint32_t base = smem_u32(ca_smem);
+  const int n_seg = a.G + a.B;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < CA_STAGES; ++s) {
+      mbar_init(smem_u32(&bk->full[s]), 1);
+      mbar_init(smem_u32(&bk->empty[s]), CA_CONSUMERS);
+    }
+    bk->abort_flag = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&tmap_k);
+    tma_prefetch_desc(&tmap_v);
+  }
+  __syncthreads();
+  WaitCtx wc{&bk->abort_flag, a.status, STATUS_CACHE_TIMEOUT, a.wait_limit};
+  pdl_enter();
+  const bool stop = __syncthreads_or((*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) != 0);
+  ca_plan<CA_THREADS>(a, off, n_seg, bk->warp_part);
+  const long long all = off[n_seg], chunk = max(1LL, (all + gridDim.x - 1) / gridDim.x);
+  if (blockIdx.x == 0) {
+    for (int s = threadIdx.x; s <= n_seg; s += CA_THREADS) a.plan[2 + s] = off[s];
+    if (threadIdx.x == 0) { a.plan[0] = all; }
+  }
+  // the query rows' owners, for the join
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    const CaSeg g = ca_segment(a, a.G + b);
+    const int grp = ca_group(a, b);
+    if (!g.valid) continue;
+    for (int r = threadIdx.x; r < g.nq; r += CA_THREADS) a.row_owner[g.q0 + r] = make_int2(b, grp);
+  }
+  CaWalk walk;
+  CaItem it;
+  walk.begin(a, off, n_seg, min(all, blockIdx.x * chunk), min(all, (blockIdx.x + 1) * chunk));
+  if (stop) walk.end = walk.t;
+
+  if (warp == CA_CONSUMERS) {
+    // ------------------------------------------------------------------ copies
+    const uint32_t leader = warp_leader();
+    RingPos pos;
+    int issued = 0, used = 0;
+    while (walk.next(a, off, it)) {
+      for (int kt = it.kt0; kt < it.kt1; ++kt, ++used) {
+        if (used >= CA_STAGES) mbar_wait_warp(smem_u32(&bk->empty[pos.slot]), pos.phase ^ 1u, wc);
+        if (!__shfl_sync(0xffffffffu, bk->abort_flag, 0)) {
+          const uint32_t bar = smem_u32(&bk->full[pos.slot]), dst = base + pos.slot * CA_STAGE_BYTES;
+          const int row = it.g.row0 + kt * CA_KEYS;
+          mbar_expect_tx_w(bar, CA_STAGE_BYTES, leader);
+          tma_load_3d_w(dst, &tmap_k, bar, 0, it.head, row, leader);
+          tma_load_3d_w(dst + CA_BLOCK_BYTES, &tmap_k, bar, 64, it.head, row, leader);
+          tma_load_3d_w(dst + 2 * CA_BLOCK_BYTES, &tmap_v, bar, 0, it.head, row, leader);
+          tma_load_3d_w(dst + 3 * CA_BLOCK_BYTES, &tmap_v, bar, 64, it.head, row, leader);
+          issued = used + 1;
+        }
+        pos.step(CA_STAGES);
+      }
+    }
+    // every copy issued has landed before the block leaves
+    for (int s = 0; s < CA_STAGES; ++s) {
+      const int fills = issued > s ? (issued - s + CA_STAGES - 1) / CA_STAGES : 0;
+      if (fills > 0) mbar_wait_drain(smem_u32(&bk->full[s]), (fills - 1) & 1, CA_WAIT_LIMIT);
+    }
+    __syncwarp();
+    return;
+  }
+  // -------------------------------------------------------------------- consumers
+  const int gq = lane >> 2, tq = lane & 3;       // fragment row / column pair
+  RingPos pos;
+  while (walk.next(a, off, it)) {
+    const int R = it.g.nq * a.rep;
+    int adm[2];                                  // admitted keys of fragment rows gq, gq + 8
+    long long entry[2];                          // (query row, head)
+    uint32_t qa[8][4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = it.rt * CA_ROWS + gq + 8 * e;
+      const bool in = i < R;
+      const int qr = it.g.q0 + i / a.rep, h = it.head * a.rep + i % a.rep;
+      adm[e] = in ? ca_admitted(a, it.g, i) : 0;
+      entry[e] = in ? (long long)qr * a.H + h : -1;
+      const uint16_t *qp = a.q + (long long)qr * a.q_row + (long long)h * a.q_head + 2 * tq;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          uint32_t w = 0u;
+          if (in) asm volatile("ld.global.u32 %0, [%1];" : "=r"(w) : "l"(qp + kk * 16 + s * 8));
+          qa[kk][e + 2 * s] = w;
+        }
+    }
+    float o[16][4];
+#pragma unroll
+    for (int n = 0; n < 16; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    for (int kt = it.kt0; kt < it.kt1; ++kt) {
+      mbar_wait_warp(smem_u32(&bk->full[pos.slot]), pos.phase, wc);
+      const uint32_t ks = base + pos.slot * CA_STAGE_BYTES, vs = ks + 2 * CA_BLOCK_BYTES;
+      const int j0 = kt * CA_KEYS + warp * 16;   // this warp's first key
+      const int mi = lane >> 3, mr = lane & 7;
+      // ---- logits of 16 rows x 16 keys
+      float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      {
+        const int key = warp * 16 + (mi >> 1) * 8 + mr;
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+          const int c = kk * 2 + (mi & 1);
+          uint32_t b[4];
+          ldsm4(ks + (c >> 3) * CA_BLOCK_BYTES + key * 128 + (((c & 7) ^ (key & 7)) << 4), b);
+          mma16816<F16>(x[0], qa[kk], b[0], b[1]);
+          mma16816<F16>(x[1], qa[kk], b[2], b[3]);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = j0 + n * 8 + 2 * tq + (e & 1);
+          x[n][e] = j < adm[e >> 1] ? x[n][e] * a.scale_log2 : -INFINITY;
+        }
+      if (a.logits) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (entry[e] < 0) continue;
+          float *row = a.logits + entry[e] * a.pitch + (it.g.causal ? a.own_off : 0);
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+            *reinterpret_cast<float2 *>(row + j0 + n * 8 + 2 * tq) = make_float2(x[n][2 * e], x[n][2 * e + 1]);
+        }
+      }
+      // ---- probabilities relative to the running maximum
+      uint32_t pa[4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float mx = fmaxf(fmaxf(x[0][2 * e], x[0][2 * e + 1]), fmaxf(x[1][2 * e], x[1][2 * e + 1]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        const float m_new = fmaxf(m[e], mx), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float f = fast_exp2(m[e] - ref);
+        m[e] = m_new;
+        l[e] *= f;
+        if (__any_sync(0xffffffffu, f != 1.f)) {
+#pragma unroll
+          for (int n = 0; n < 16; ++n) { o[n][2 * e] *= f; o[n][2 * e + 1] *= f; }
+        }
+        float p[2][2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) p[n][c] = fast_exp2(x[n][2 * e + c] - ref);
+        l[e] += (p[0][0] + p[0][1]) + (p[1][0] + p[1][1]);
+        pa[e] = pack2_t<F16>(p[0][0], p[0][1]);
+        pa[e + 2] = pack2_t<F16>(p[1][0], p[1][1]);
+      }
+      // ---- values.  Rows that no query row of the tile admits are cleared (0 * NaN is NaN).  A row that only some of them
+      // admit may hold infinities or NaN too: then its part is added without the matrix instruction, to the rows that admit it.
+      const int vcol = (mi & 1) * 8 + mr;
+      uint32_t bad = 0u;                         // keys of this warp's 16 to be added apart
+      if (j0 + 16 > (it.g.causal ? it.g.keys - it.g.nq + 1 : it.g.keys)) {
+        const int r = lane >> 1, half = lane & 1;           // two lanes per key
+        const bool dead = j0 + r >= it.g.keys;
+        uint8_t *vrow = ca_smem + pos.slot * CA_STAGE_BYTES + (2 + half) * CA_BLOCK_BYTES + (warp * 16 + r) * 128;
+        bool nf = false;
+        if (!dead)
+          for (int c = 0; c < 8; ++c) {
+            const uint4 v = reinterpret_cast<const uint4 *>(vrow)[c];
+            nf = nf || not_finite16(v.x, F16) || not_finite16(v.y, F16) || not_finite16(v.z, F16) || not_finite16(v.w, F16);
+          }
+        const uint32_t who = __ballot_sync(0xffffffffu, nf);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) bad |= ((who >> (2 * e)) & 3u) ? 1u << e : 0u;
+        if (dead)
+          for (int c = 0; c < 8; ++c) reinterpret_cast<uint4 *>(vrow)[c] = make_uint4(0u, 0u, 0u, 0u);
+        __syncwarp();
+        for (uint32_t left = bad; left; left &= left - 1) {
+          const int r2 = __ffs(left) - 1;        // key
+          const int src = (lane & ~3) | ((r2 & 7) >> 1);
+          const uint32_t w0 = __shfl_sync(0xffffffffu, (r2 & 8) ? pa[2] : pa[0], src), w1 = __shfl_sync(0xffffffffu, (r2 & 8) ? pa[3] : pa[1], src);
+          const float2 u0 = unpack2_t<F16>(w0), u1 = unpack2_t<F16>(w1);
+          const float p0 = (r2 & 1) ? u0.y : u0.x, p1 = (r2 & 1) ? u1.y : u1.x;
+          const bool in0 = j0 + r2 < adm[0], in1 = j0 + r2 < adm[1];
+#pragma unroll
+          for (int n = 0; n < 16; ++n) {
+            const int key = warp * 16 + r2;
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(ca_smem + pos.slot * CA_STAGE_BYTES + (2 + (n >> 3)) * CA_BLOCK_BYTES +
+                                                                   key * 128 + (((n & 7) ^ (key & 7)) << 4) + tq * 4);
+            const float2 v = unpack2_t<F16>(w);
+            if (in0) { o[n][0] += p0 * v.x; o[n][1] += p0 * v.y; }
+            if (in1) { o[n][2] += p1 * v.x; o[n][3] += p1 * v.y; }
+          }
+        }
+        __syncwarp();
+        if (bad) {
+          if ((bad >> r) & 1u)
+            for (int c = 0; c < 8; ++c) reinterpret_cast<uint4 *>(vrow)[c] = make_uint4(0u, 0u, 0u, 0u);
+          __syncwarp();
+        }
+        fence_proxy_async();                     // these writes come before the next copy into the slot
+      }
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) {
+        const int c = dt * 2 + (mi >> 1), key = warp * 16 + vcol;
+        uint32_t b[4];
+        ldsm4t(vs + (c >> 3) * CA_BLOCK_BYTES + key * 128 + (((c & 7) ^ (key & 7)) << 4), b);
+        mma16816<F16>(o[2 * dt], pa, b[0], b[1]);
+        mma16816<F16>(o[2 * dt + 1], pa, b[2], b[3]);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&bk->empty[pos.slot]));
+      pos.step(CA_STAGES);
+    }
+    // ---- the four warps' sums of the item
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
+      l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
+      if (l[e] != l[e] && m[e] == -INFINITY) m[e] = 0.f;      // every logit was NaN: not an empty row
+      if (tq == 0) bk->ml[warp][gq + 8 * e] = make_float2(m[e], l[e]);
+    }
+    const int rows = min(CA_ROWS, R - it.rt * CA_ROWS);
+    const int pad_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : 16, width = 512 / pad_rows;    // columns a piece
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
+    float f[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float top = -INFINITY;
+      for (int w = 0; w < CA_CONSUMERS; ++w) top = fmaxf(top, bk->ml[w][gq + 8 * e].x);
+      f[e] = m[e] == -INFINITY ? 0.f : fast_exp2(m[e] - top);
+    }
+    const long long before = off[it.seg] + it.head * ((off[it.seg + 1] - off[it.seg]) / a.kv) + ca_tiles_before(a, it.g, it.rt);
+    const CaPlace pl = ca_place(before, it.kt_all, chunk);
+    for (int c0 = 0; c0 < 128; c0 += width) {
+#pragma unroll
+      for (int n = 0; n < 16; ++n) {
+        const int c = n * 8 + 2 * tq - c0;
+        if (c < 0 || c >= width) continue;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (gq + 8 * e < pad_rows)
+            *reinterpret_cast<float2 *>(join + (warp * pad_rows + gq + 8 * e) * width + c) = make_float2(o[n][2 * e] * f[e], o[n][2 * e + 1] * f[e]);
+      }
+      asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
+      const int r = threadIdx.x / (width / 4), c = threadIdx.x % (width / 4) * 4;
+      if (r < rows && !bk->abort_flag) {
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        float top = -INFINITY, sum = 0.f;
+        for (int w = 0; w < CA_CONSUMERS; ++w) {
+          const float4 v = *reinterpret_cast<const float4 *>(join + (w * pad_rows + r) * width + c);
+          s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+          top = fmaxf(top, bk->ml[w][r].x);
+        }
+        for (int w = 0; w < CA_CONSUMERS; ++w)
+          if (bk->ml[w][r].x != -INFINITY) sum += bk->ml[w][r].y * fast_exp2(bk->ml[w][r].x - top);
+        const int i = it.rt * CA_ROWS + r;
+        const int qr = it.g.q0 + i / a.rep, h = it.head * a.rep + i % a.rep;
+        const long long ent = (long long)qr * a.H + h;
+        float2 *ml;
+        float *dst;
+        if (pl.c0 == pl.c1) {
+          const long long e = (it.g.causal ? (long long)a.n_q * a.H : 0) + ent;
+          ml = a.full_ml + e;
+          dst = a.full_o + e * 128;
+        } else {
+          const long long e = (long long)(2 * blockIdx.x + (pl.first <= blockIdx.x * chunk ? 0 : 1)) * CA_ROWS + r;
+          ml = a.rec_ml + e;
+          dst = a.rec_o + e * 128;
+        }
+        *reinterpret_cast<float4 *>(dst + c0 + c) = s;
+        if (c0 + c == 0) *ml = make_float2(top, sum);
+      }
+      asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Partial results of a (query row, head) -> output.  A warp each; a lane holds four of the 128 values.
+// ---------------------------------------------------------------------------------------
+constexpr int CA_JOIN_THREADS = 128;
+
+__device__ __forceinline__ float2 ld_prev2f(const float2 *p) {
+  float2 v;
+  asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ float4 ld_prev4f(const float *p) {
+  float4 v;
+  asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ long long ld_prev64(const long long *p) {
+  long long v;
+  asm volatile("ld.global.s64 %0, [%1];" : "=l"(v) : "l"(p));
+  return v;
+}
+
+template <bool F16>
+__global__ void __launch_bounds__(CA_JOIN_THREADS)
+ca_join_kernel(const __grid_constant__ CacheArgs a, int stream_blocks) {
+  pdl_enter();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long entry = (long long)blockIdx.x * (CA_JOIN_THREADS / 32) + warp;
+  if (entry >= (long long)a.n_q * a.H) return;
+  if (*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) return;
+  const int qr = (int)(entry / a.H), h = (int)(entry - (long long)qr * a.H);
+  const int2 own = ld_prev(a.row_owner + qr);
+  CaSeg seg[2];                                  // prefix, own
+  bool ok = own.x >= 0 && own.x < a.B && own.y < a.G && own.y >= -1;
+  if (ok) {
+    seg[1] = ca_segment(a, a.G + own.x);
+    ok = seg[1].valid && qr >= seg[1].q0 && qr < seg[1].q0 + seg[1].nq;
+  }
+  if (!ok) {                                     // a row of a sequence that is skipped
+    if (lane == 0) a.lse2[entry] = INFINITY;
+    return;
+  }
+  const long long all = ld_prev64(a.plan), chunk = max(1LL, (all + stream_blocks - 1) / stream_blocks);
+  float top = -INFINITY, sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float2 ml, float4 o) {
+    if (ml.x == -INFINITY) return;
+    const float t = fmaxf(top, ml.x), f = top == -INFINITY ? 0.f : fast_exp2(top - t), g = fast_exp2(ml.x - t);
+    sum = sum * f + ml.y * g;
+    acc.x = acc.x * f + o.x * g; acc.y = acc.y * f + o.y * g; acc.z = acc.z * f + o.z * g; acc.w = acc.w * f + o.w * g;
+    top = t;
+  };
+  for (int part = own.y >= 0 ? 0 : 1; part < 2; ++part) {
+    const int s = part == 0 ? own.y : a.G + own.x;
+    if (part == 0) seg[0] = ca_segment(a, s);
+    const CaSeg &g = seg[part];
+    const int i = (qr - g.q0) * a.rep + h % a.rep, rt = i / CA_ROWS, r = i % CA_ROWS;
+    const int n = ca_key_tiles(a, g, rt);
+    if (n == 0) continue;
+    const long long off0 = ld_prev64(a.plan + 2 + s), off1 = ld_prev64(a.plan + 3 + s);
+    const CaPlace pl = ca_place(off0 + (h / a.rep) * ((off1 - off0) / a.kv) + ca_tiles_before(a, g, rt), n, chunk);
+    if (pl.c0 == pl.c1) {
+      const long long e = (long long)part * a.n_q * a.H + entry;
+      add(ld_prev2f(a.full_ml + e), ld_prev4f(a.full_o + e * 128 + lane * 4));
+      continue;
+    }
+#pragma unroll 4
+    for (int c = pl.c0; c <= pl.c1; ++c) {
+      const long long e = (long long)(2 * c + (pl.first <= c * chunk ? 0 : 1)) * CA_ROWS + r;
+      add(ld_prev2f(a.rec_ml + e), ld_prev4f(a.rec_o + e * 128 + lane * 4));
+    }
+  }
+  const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);    // (NaN stays NaN)
+  uint16_t *dst = a.out + (long long)qr * a.out_row + (long long)h * a.out_head + lane * 4;
+  *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2_t<F16>(acc.x * inv, acc.y * inv), pack2_t<F16>(acc.z * inv, acc.w * inv));
+  if (lane == 0) {
+    const float l2 = top + __log2f(sum);
+    if (a.lse) a.lse[entry] = sum == 0.f ? -INFINITY : l2 * 0.6931471805599453f;
+    a.lse2[entry] = sum == 0.f ? INFINITY : l2;
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// weights[j] += 1 / H * sum over the segment's query rows and heads of 2^(x - lse2).  A block per 32 keys of a segment: lane = key, the
+// warps share the (row, head) pairs and their sums are added in the order of the warps.
+// ---------------------------------------------------------------------------------------
+constexpr int CA_WEIGHT_THREADS = 512;
+
+__global__ void __launch_bounds__(CA_WEIGHT_THREADS)
+ca_weight_kernel(const __grid_constant__ CacheArgs a, int prefix_blocks, int own_blocks) {
+  __shared__ float part[CA_WEIGHT_THREADS / 32][32];
+  pdl_enter();
+  const int n_pre = a.G * prefix_blocks;
+  const int s = (int)blockIdx.x < n_pre ? blockIdx.x / prefix_blocks : a.G + (blockIdx.x - n_pre) / own_blocks;
+  const int kb = (int)blockIdx.x < n_pre ? blockIdx.x % prefix_blocks : (blockIdx.x - n_pre) % own_blocks;
+  const CaSeg g = ca_segment(a, s);
+  if (!g.valid || kb * 32 >= g.keys) return;
+  if (*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = kb * 32 + lane;
+  const long long n = (long long)g.nq * a.H;
+  const float *x = a.logits + (long long)g.q0 * a.H * a.pitch + (g.causal ? a.own_off : 0) + j;
+  float sum = 0.f;
+#pragma unroll 4
+  for (long long e = warp; e < n; e += CA_WEIGHT_THREADS / 32) {
+    const float l2 = ld_prev(a.lse2 + (long long)g.q0 * a.H + e);
+    const bool in = j < g.keys && (!g.causal || j < g.keys - g.nq + 1 + (int)(e / a.H));
+    const float v = in ? ld_prev(x + e * a.pitch) : -INFINITY;
+    sum += in && l2 != INFINITY ? fast_exp2(v - l2) : 0.f;
+  }
+  part[warp][lane] = sum;
+  __syncthreads();
+  if (warp == 0 && j < g.keys) {
+    float t = 0.f;
+    for (int w = 0; w < CA_WEIGHT_THREADS / 32; ++w) t += part[w][lane];
+    float *p = a.weights + g.row0 + j;
+    *p = ld_prev(p) + t / (float)a.H;
+  }
+}
+
+// =======================================================================================
+// Eviction
+// =======================================================================================
+constexpr int EV_THREADS = 1024;
+
+struct EvictArgs {
+  int B, max_len, keep, sink, recent, rows, dst_rows;
+  const int *start, *len, *dst_start;
+  const float *weights;
+  const int *pos;
+  int *keep_idx, *new_len;
+  float *dst_weights;
+  int *dst_pos;
+  uint32_t *status;
+};
+
+// A float's order as an unsigned number: -inf .. +inf ascending from 1 up, -0 as +0, NaN 0.
+__device__ __forceinline__ uint32_t rank_key(float w) {
+  if (!(w == w)) return 0u;
+  const uint32_t u = __float_as_uint(w + 0.f);           // -0 + 0 = +0
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+// ... with the held rows above everything (no float's order is 2^32 - 1)
+__device__ __forceinline__ uint32_t row_key(float w, int row, int pos, int sink, int recent, long long newest) {
+  return row < sink || (long long)pos > newest - recent ? 0xffffffffu : rank_key(w);
+}
+
+// A block per sequence: the keep-th largest key by radix selection, eight bits a pass; then every warp compacts a range of rows.
+__global__ void __launch_bounds__(EV_THREADS)
+evict_select_kernel(const __grid_constant__ EvictArgs a) {
+  __shared__ int hist[256];
+  __shared__ int warp_gt[32], warp_eq[32];
+  __shared__ uint32_t sh_prefix;
+  __shared__ int sh_need;
+  __shared__ long long sh_newest;
+  pdl_enter();
+  const int b = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int n = ld_prev(a.len + b), row0 = ld_prev(a.start + b), dst0 = a.dst_start ? ld_prev(a.dst_start + b) : row0;
+  int *idx = a.keep_idx + (size_t)b * a.keep;
+  const int m = min(n, a.keep);
+  if (n < 0 || n > a.max_len || row0 < 0 || (long long)row0 + n > a.rows || dst0 < 0 || (long long)dst0 + m > a.dst_rows) {
+    for (int i = tid; i < a.keep; i += EV_THREADS) idx[i] = -1;
+    if (tid == 0) atomicOr(a.status, (uint32_t)STATUS_BAD_SAMPLE);
+    return;
+  }
+  const float *w = a.weights + row0;
+  const int *pos = a.pos ? a.pos + row0 : nullptr;
+  for (int i = m + tid; i < a.keep; i += EV_THREADS) idx[i] = -1;
+  if (n <= a.keep) {
+    for (int i = tid; i < n; i += EV_THREADS) idx[i] = i;
+  } else {
+    long long newest = n - 1;
+    if (pos) {
+      int top = INT_MIN;
+      for (int i = tid; i < n; i += EV_THREADS) top = max(top, ld_prev(pos + i));
+      top = __reduce_max_sync(0xffffffffu, top);
+      if (lane == 0) warp_gt[warp] = top;
+      __syncthreads();
+      if (warp == 0) {
+        top = __reduce_max_sync(0xffffffffu, warp_gt[lane]);
+        if (lane == 0) sh_newest = top;
+      }
+      __syncthreads();
+      newest = sh_newest;
+    }
+    auto key = [&](int i) { return row_key(ld_prev(w + i), i, pos ? ld_prev(pos + i) : i, a.sink, a.recent, newest); };
+    uint32_t prefix = 0u;
+    int need = a.keep;                           // rows still to be taken among those that share the prefix
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      if (tid < 256) hist[tid] = 0;
+      __syncthreads();
+      for (int i = tid; i < n; i += EV_THREADS) {
+        const uint32_t k = key(i);
+        if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1);
+      }
+      __syncthreads();
+      if (warp == 0) {                           // from the top: lane holds bins 255 - 8 lane .. 248 - 8 lane
+        int c[8], mine = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { c[e] = hist[255 - 8 * lane - e]; mine += c[e]; }
+        int above = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, above, o);
+          if (lane >= o) above += v;
+        }
+        above -= mine;
+        if (above < need && above + mine >= need) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            if (above < need && above + c[e] >= need) {
+              sh_prefix = (prefix << 8) | (uint32_t)(255 - 8 * lane - e);
+              sh_need = need - above;
+              above = INT_MAX / 2;
+            } else {
+              above += c[e];
+            }
+          }
+        }
+      }
+      __syncthreads();
+      prefix = sh_prefix;
+      need = sh_need;
+    }
+    // rows above the threshold, and the first `need` equal to it
+    const int per = ((n + 1023) / 1024) * 32, lo = min(n, warp * per), hi = min(n, lo + per);
+    int gt = 0, eq = 0;
+    for (int i = lo + lane; i < hi; i += 32) {
+      const uint32_t k = key(i);
+      gt += k > prefix;
+      eq += k == prefix;
+    }
+    gt = __reduce_add_sync(0xffffffffu, gt);
+    eq = __reduce_add_sync(0xffffffffu, eq);
+    if (lane == 0) { warp_gt[warp] = gt; warp_eq[warp] = eq; }
+    __syncthreads();
+    int gt0 = 0, eq0 = 0;
+    for (int v = 0; v < warp; ++v) { gt0 += warp_gt[v]; eq0 += warp_eq[v]; }
+    int at = gt0 + min(eq0, need);
+    for (int i0 = lo; i0 < hi; i0 += 32) {
+      const int i = i0 + lane;
+      const uint32_t k = i < hi ? key(i) : 0u;
+      const uint32_t beq = __ballot_sync(0xffffffffu, i < hi && k == prefix);
+      const bool take = i < hi && (k > prefix || (k == prefix && eq0 + __popc(beq & ((1u << lane) - 1u)) < need));
+      const uint32_t bt = __ballot_sync(0xffffffffu, take);
+      if (take) idx[at + __popc(bt & ((1u << lane) - 1u))] = i;
+      at += __popc(bt);
+      eq0 += __popc(beq);
+    }
+  }
+  if (tid == 0) a.new_len[b] = m;
+  __syncthreads();
+  // weights and positions; a piece is read before it is written, and no later piece has its source where an earlier one goes
+  for (int i0 = 0; i0 < m; i0 += EV_THREADS) {
+    const int i = i0 + tid;
+    float wv = 0.f;
+    int pv = 0;
+    if (i < m) {
+      const int s = *reinterpret_cast<const volatile int *>(idx + i);
+      if (a.dst_weights) wv = ld_prev(w + s);
+      if (a.dst_pos) pv = pos ? ld_prev(pos + s) : s;
+    }
+    __syncthreads();
+    if (i < m) {
+      if (a.dst_weights) a.dst_weights[dst0 + i] = wv;
+      if (a.dst_pos) a.dst_pos[dst0 + i] = pv;
+    }
+    __syncthreads();
+  }
+}
+
+constexpr int EV_MAX_TENSORS = 64;
+constexpr int EV_MOVE_THREADS = 256;
+struct EvictMoveArgs {
+  const uint4 *src[EV_MAX_TENSORS];
+  uint4 *dst[EV_MAX_TENSORS];
+  const int *keep_idx, *start, *dst_start;
+  int keep, rows, dst_rows, row_vecs;
+};
+
+// Into other tensors: a warp per kept row.
+__global__ void __launch_bounds__(EV_MOVE_THREADS)
+evict_move_kernel(const __grid_constant__ EvictMoveArgs a) {
+  pdl_enter();
+  const int b = blockIdx.y, t = blockIdx.z, i = blockIdx.x * (EV_MOVE_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (i >= a.keep) return;
+  const int k = ld_prev(a.keep_idx + (size_t)b * a.keep + i);
+  const int row0 = ld_prev(a.start + b), dst0 = a.dst_start ? ld_prev(a.dst_start + b) : row0;
+  if (k < 0) return;
+  const uint4 *s = a.src[t] + (size_t)(row0 + k) * a.row_vecs;
+  uint4 *d = a.dst[t] + (size_t)(dst0 + i) * a.row_vecs;
+  int v = lane;
+  for (; v + 7 * 32 < a.row_vecs; v += 8 * 32) {
+    uint4 x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ld_prev8(s + v + 32 * e, x[e]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[v + 32 * e] = x[e];
+  }
+  for (; v < a.row_vecs; v += 32) {
+    uint4 x;
+    ld_prev8(s + v, x);
+    d[v] = x;
+  }
+}
+
+// In place: a block per (sequence, tensor, 256 bytes of every row) takes the kept rows in ascending order, 128 at a time, and reads a piece
+// before it writes it.  Row i of the kept ones goes to row i <= its own number, so no later piece reads what an earlier one wrote.
+__global__ void __launch_bounds__(EV_MOVE_THREADS)
+evict_in_place_kernel(const __grid_constant__ EvictMoveArgs a) {
+  pdl_enter();
+  const int b = blockIdx.y, t = blockIdx.z, v = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
+  const int *idx = a.keep_idx + (size_t)b * a.keep;
+  const int row0 = ld_prev(a.start + b);
+  uint4 *base = a.dst[t] + v;
+  const bool in = v < a.row_vecs;
+  for (int i0 = 0; i0 < a.keep; i0 += 128) {
+    uint4 x[8];
+    int k[8];
+    bool end = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int i = i0 + r0 + 16 * e;
+      k[e] = i < a.keep ? ld_prev(idx + i) : -1;
+      end = end || k[e] < 0;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (in && k[e] > i0 + r0 + 16 * e) ld_prev8(base + (size_t)(row0 + k[e]) * a.row_vecs, x[e]);
+    const bool last = __syncthreads_or(end);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int i = i0 + r0 + 16 * e;
+      if (in && k[e] > i) base[(size_t)(row0 + i) * a.row_vecs] = x[e];
+    }
+    if (last) break;
+    __syncthreads();
+  }
+}
+
+// The lowest ranked row of a full cache: smallest key, the last row among equals.
+constexpr int SLOT_THREADS = 512;
+struct SlotArgs {
+  int B, capacity, sink, recent, rows;
+  const int *start;
+  int *len;
+  float *weights;
+  int *pos;
+  const int *new_pos;
+  int *row;
+  uint32_t *status;
+};
+__global__ void __launch_bounds__(SLOT_THREADS)
+slot_kernel(const __grid_constant__ SlotArgs a) {
+  __shared__ unsigned long long part[SLOT_THREADS / 32];
+  pdl_enter();
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const int n = ld_prev(a.len + b), row0 = ld_prev(a.start + b), np = ld_prev(a.new_pos + b);
+  if (n < 0 || n > a.capacity || row0 < 0 || (long long)row0 + min(n + 1, a.capacity) > a.rows) {
+    if (tid == 0) {
+      a.row[b] = -1;
+      atomicOr(a.status, (uint32_t)STATUS_BAD_SAMPLE);
+    }
+    return;
+  }
+  int slot = n;
+  if (n == a.capacity) {
+    unsigned long long best = ~0ull;
+#pragma unroll 4
+    for (int i = tid; i < n; i += SLOT_THREADS) {
+      const uint32_t k = row_key(ld_prev(a.weights + row0 + i), i, ld_prev(a.pos + row0 + i), a.sink, a.recent, (long long)np - 1);
+      best = min(best, ((unsigned long long)k << 32) | (0xffffffffu - (uint32_t)i));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, o));
+    if ((tid & 31) == 0) part[tid >> 5] = best;
+    __syncthreads();
+    best = part[0];
+    for (int w = 1; w < SLOT_THREADS / 32; ++w) best = min(best, part[w]);
+    slot = (int)(0xffffffffu - (uint32_t)best);
+  }
+  if (tid == 0) {
+    a.row[b] = row0 + slot;
+    if (n < a.capacity) a.len[b] = n + 1;
+    a.weights[row0 + slot] = 0.f;
+    a.pos[row0 + slot] = np;
+  }
+}
+
+}  // namespace asap
