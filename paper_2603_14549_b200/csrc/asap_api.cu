@@ -31,6 +31,8 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+size_t ca_smem_bytes(int n_seg);
+size_t ct_smem_bytes(int n_seg);
 
 }  // namespace
 
@@ -852,6 +854,8 @@ asap_status asap_init(asap_ctx **ctx_out, int device, size_t max_total_tokens, i
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, AT_SMEM_BYTES);
   for (auto kernel : {ca_stream_kernel<false>, ca_stream_kernel<true>})
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ca_smem_bytes(CA_MAX_SEGMENTS));
+  for (auto kernel : {ca_tile_kernel<false>, ca_tile_kernel<true>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ct_smem_bytes(CA_MAX_SEGMENTS));
   if (e == cudaSuccess && ctx->sim_cluster) {
     // the cluster form of the sliced similarity launch needs eight co-resident blocks of up to 195 KB each in one
     // cluster; where the device (or the partition of it this process sees) cannot place one, the form is not used

@@ -20,6 +20,8 @@ size_t ca_smem_bytes(int n_seg) {
   return CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES + sizeof(CaBook) + (size_t)(n_seg + 1) * sizeof(long long);
 }
 
+size_t ct_smem_bytes(int n_seg) { return CT_BOOK_OFF + sizeof(CtBook) + (size_t)(n_seg + 1) * sizeof(long long); }
+
 // Elements that [rows, heads, dim] with the given strides spans.
 long long span_of(long long rows, long long heads, long long dim, long long row, long long head) {
   return (rows - 1) * row + (heads - 1) * head + dim;
@@ -74,33 +76,39 @@ asap_status check_cache_attention(asap_ctx *ctx, const asap_cache_attention_args
 // Scratch of a call; `at` NULL: only its size.
 struct CaLayout {
   size_t bytes = 0;
-  int stream_blocks = 0;
+  int blocks[2] = {0, 0};        // of the streaming and of the tile kernel; 0: nothing to launch
 };
 CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint8_t *at, CacheArgs *a) {
   CaLayout l;
   const size_t entries = (size_t)p->n_q * p->H, n_seg = (size_t)p->B + p->n_groups;
-  // no more blocks than there can be tiles
-  const int rep = p->H / p->kv_heads;
-  auto most = [&](long long segs, long long rows, long long keys) { return segs * ((rows * rep + CA_ROWS - 1) / CA_ROWS) * ((keys + CA_KEYS - 1) / CA_KEYS) * p->kv_heads; };
-  const long long tiles = most(p->B, p->max_q, p->max_len) + (p->n_groups ? most(p->n_groups, p->n_q, p->max_prefix) : 0);
-  l.stream_blocks = (int)(tiles < 2LL * ctx->num_sms ? (tiles > 1 ? tiles : 1) : 2LL * ctx->num_sms);
+  // no more blocks than there can be key tiles; no tile kernel where no segment can have more than 16 stacked rows
+  const long long rep = p->H / p->kv_heads, heads = p->kv_heads, group_rows = p->n_groups > 0 && p->max_prefix > 0 ? p->n_q * rep : 0;
+  auto tiles = [&](long long segs, long long rows, long long keys, int R, int K) { return segs * ((rows + R - 1) / R) * ((keys + K - 1) / K) * heads; };
+  auto at_most = [](long long n, long long most) { return (int)(n < 1 ? 1 : n < most ? n : most); };
+  const long long own_rows = p->max_q * rep, S = StreamWork::ROWS;
+  l.blocks[0] = at_most(tiles(p->B, 1, p->max_len, 1, StreamWork::KEYS) + (group_rows ? tiles(p->n_groups, 1, p->max_prefix, 1, StreamWork::KEYS) : 0), 2LL * ctx->num_sms);
+  if (own_rows > S || group_rows > S)
+    l.blocks[1] = at_most((own_rows > S ? tiles(p->B, own_rows, p->max_len, TileWork::ROWS, TileWork::KEYS) : 0) +
+                              (group_rows > S ? tiles(p->n_groups, group_rows, p->max_prefix, TileWork::ROWS, TileWork::KEYS) : 0), ctx->num_sms);
   auto carve = [&](size_t bytes) {
-    uint8_t *q = at + l.bytes;
+    const size_t o = l.bytes;
     l.bytes = align_up(l.bytes + bytes, 256);
-    return q;
+    return at + o;
   };
-  const size_t records = (size_t)2 * l.stream_blocks * CA_ROWS;
-  const long long own_off = p->n_groups ? ((long long)p->max_prefix + 63) / 64 * 64 : 0;
-  const long long pitch = own_off + ((long long)p->max_len + 63) / 64 * 64;
-  uint8_t *plan = carve((n_seg + 3) * 8), *owner = carve((size_t)p->n_q * 8), *rec_ml = carve(records * 8), *full_ml = carve(2 * entries * 8),
-          *rec_o = carve(records * 512), *full_o = carve(2 * entries * 512), *lse2 = carve(entries * 4),
-          *logits = p->weights ? carve(entries * (size_t)pitch * 4) : nullptr;
+  const size_t rec[2] = {(size_t)2 * l.blocks[0] * StreamWork::ROWS, (size_t)2 * l.blocks[1] * TileWork::ROWS};
+  const long long own_off = p->n_groups ? ((long long)p->max_prefix + 127) / 128 * 128 : 0;
+  const long long pitch = own_off + ((long long)p->max_len + 127) / 128 * 128;       // (a key tile is written whole)
+  uint8_t *plan = carve(2 * (n_seg + 1) * 8), *owner = carve((size_t)p->n_q * 8), *rec_ml0 = carve(rec[0] * 8), *rec_ml1 = carve(rec[1] * 8),
+          *full_ml = carve(2 * entries * 8), *rec_o0 = carve(rec[0] * 512), *rec_o1 = carve(rec[1] * 512), *full_o = carve(2 * entries * 512),
+          *lse2 = carve(entries * 4), *logits = p->weights ? carve(entries * (size_t)pitch * 4) : nullptr;
   if (a) {
     a->plan = reinterpret_cast<long long *>(plan); a->row_owner = reinterpret_cast<int2 *>(owner);
-    a->rec_ml = reinterpret_cast<float2 *>(rec_ml); a->full_ml = reinterpret_cast<float2 *>(full_ml);
-    a->rec_o = reinterpret_cast<float *>(rec_o); a->full_o = reinterpret_cast<float *>(full_o);
-    a->lse2 = reinterpret_cast<float *>(lse2); a->logits = reinterpret_cast<float *>(logits);
-    a->pitch = pitch; a->own_off = (int)own_off;
+    a->rec_ml[0] = reinterpret_cast<float2 *>(rec_ml0); a->rec_ml[1] = reinterpret_cast<float2 *>(rec_ml1);
+    a->full_ml = reinterpret_cast<float2 *>(full_ml);
+    a->rec_o[0] = reinterpret_cast<float *>(rec_o0); a->rec_o[1] = reinterpret_cast<float *>(rec_o1);
+    a->full_o = reinterpret_cast<float *>(full_o); a->lse2 = reinterpret_cast<float *>(lse2);
+    a->logits = reinterpret_cast<float *>(logits); a->pitch = pitch; a->own_off = (int)own_off;
+    a->blocks[0] = l.blocks[0]; a->blocks[1] = l.blocks[1];
   }
   return l;
 }
@@ -228,27 +236,37 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   const CaLayout layout = ca_layout(ctx, p, static_cast<uint8_t *>(scratch), &a);
   if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0 || scratch_bytes < layout.bytes)
     return fail(ctx, ASAP_ERR_WORKSPACE, "asap_cache_attention: scratch is null, not 256-byte aligned or smaller than asap_cache_attention_scratch_bytes");
-  CUtensorMap map_k, map_v;
-  if (!make_cache_map(ctx, &map_k, p->k, p, CA_KEYS) || !make_cache_map(ctx, &map_v, p->v, p, CA_KEYS))
-    return fail(ctx, ASAP_ERR_CUDA, "cuTensorMapEncodeTiled failed for k / v");
+  CUtensorMap map_k[2], map_v[2];
+  for (int w = 0; w < 2; ++w) {
+    const uint32_t box = w == 0 ? StreamWork::KEYS : TileWork::KEYS;
+    if (layout.blocks[w] && (!make_cache_map(ctx, &map_k[w], p->k, p, box) || !make_cache_map(ctx, &map_v[w], p->v, p, box)))
+      return fail(ctx, ASAP_ERR_CUDA, "cuTensorMapEncodeTiled failed for k / v");
+  }
   a.B = p->B; a.G = p->n_groups; a.H = p->H; a.kv = p->kv_heads; a.rep = p->H / p->kv_heads;
   a.n_q = p->n_q; a.max_q = p->max_q; a.max_len = p->max_len; a.max_prefix = p->max_prefix; a.cache_rows = p->cache_rows;
   a.q_row = p->q_row; a.q_head = p->q_head; a.out_row = p->out_row; a.out_head = p->out_head;
   a.q_cu = p->q_cu; a.start = p->start; a.len = p->len; a.group_cu = p->group_cu; a.prefix_start = p->prefix_start; a.prefix_len = p->prefix_len;
-  a.q = static_cast<const uint16_t *>(p->q); a.out = static_cast<uint16_t *>(p->out); a.lse = p->lse; a.weights = p->weights;
+  a.q = static_cast<const uint16_t *>(p->q); a.v = static_cast<const uint16_t *>(p->v); a.kv_row = p->kv_row; a.kv_head = p->kv_head;
+  a.out = static_cast<uint16_t *>(p->out); a.lse = p->lse; a.weights = p->weights;
   a.scale_log2 = 1.4426950408889634f * (p->scale > 0.f ? p->scale : 1.0f / sqrtf(128.f));
   a.status = ctx->status; a.wait_limit = ctx->wait_limit;
   const bool f16 = p->dtype == ASAP_FP16;
   DeviceGuard guard(ctx->device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (layout.blocks[1]) {
+    mark(ctx, "cache_tile", st);
+    launch_pdl(f16 ? ca_tile_kernel<true> : ca_tile_kernel<false>, dim3(layout.blocks[1]), dim3(CT_THREADS), ct_smem_bytes(p->B + p->n_groups), st,
+               map_k[1], map_v[1], a);
+    ASAP_TRY(after_launch(ctx, "cache_tile"));
+  }
   mark(ctx, "cache_stream", st);
-  launch_pdl(f16 ? ca_stream_kernel<true> : ca_stream_kernel<false>, dim3(layout.stream_blocks), dim3(CA_THREADS),
-             ca_smem_bytes(p->B + p->n_groups), st, map_k, map_v, a);
+  launch_pdl(f16 ? ca_stream_kernel<true> : ca_stream_kernel<false>, dim3(layout.blocks[0]), dim3(CA_THREADS), ca_smem_bytes(p->B + p->n_groups), st,
+             map_k[0], map_v[0], a);
   ASAP_TRY(after_launch(ctx, "cache_stream"));
   const long long entries = (long long)p->n_q * p->H;
   mark(ctx, "cache_join", st);
   launch_pdl(f16 ? ca_join_kernel<true> : ca_join_kernel<false>, dim3((unsigned)((entries + CA_JOIN_THREADS / 32 - 1) / (CA_JOIN_THREADS / 32))),
-             dim3(CA_JOIN_THREADS), 0, st, a, layout.stream_blocks);
+             dim3(CA_JOIN_THREADS), 0, st, a);
   ASAP_TRY(after_launch(ctx, "cache_join"));
   if (p->weights && (p->max_len > 0 || (p->n_groups && p->max_prefix > 0))) {
     const long long pre = (p->max_prefix + 31) / 32, own = (p->max_len + 31) / 32, blocks = pre * p->n_groups + own * p->B;

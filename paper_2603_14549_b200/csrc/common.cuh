@@ -458,6 +458,9 @@ __host__ __device__ constexpr uint32_t umma_idesc_bf16(int M, int N) {
          (static_cast<uint32_t>(M >> 4) << 24);
 }
 
+// The same with f16 A and B (format 0).
+__host__ __device__ constexpr uint32_t umma_idesc_f16(int M, int N) { return umma_idesc_bf16(M, N) & ~((1u << 7) | (1u << 10)); }
+
 // ---------------------------------------------------------------------------------------
 // Thread-block clusters: barrier over all threads of a cluster and access to the shared memory of
 // the other blocks of the cluster (distributed shared memory).

@@ -159,15 +159,21 @@ rope_kernel(const __grid_constant__ RopeArgs a) {
 // =======================================================================================
 // A segment is a run of cache rows with the query rows that look at it: segment g < G is the prefix of group g with all query
 // rows of its sequences, segment G + b the own rows of sequence b.  Per key / value head the R = (query rows) * (H / kv_heads)
-// stacked rows of a segment are cut into row tiles of CA_ROWS, the keys that a row tile admits into tiles of CA_KEYS.  All key
-// tiles of all row tiles, heads and segments are numbered through, and every block takes an equal range of numbers: lengths may be
-// as ragged as they like, and the host needs to know none of them.  A row tile whose key tiles lie in one block is complete there;
-// otherwise each block leaves a partial result (maximum, sum, weighted values) and the join adds them up in order.
-constexpr int CA_ROWS = 16, CA_KEYS = 64;
+// stacked rows of a segment are cut into row tiles, the keys that a row tile admits into key tiles.  Segments of up to 16 stacked rows
+// are streamed (ca_stream_kernel), the others go to the tensor cores as tiles of 128 rows, two side by side (ca_tile_kernel).  Each of
+// the two kernels numbers its key tiles through (all row tiles, heads and segments) and gives every block an equal range of numbers:
+// lengths may be as ragged as they like, and the host needs to know none of them.  A row tile whose key tiles lie in one block is
+// complete there; otherwise each block leaves a partial result (maximum, sum, weighted values) and the join adds them up in order.
+struct StreamWork {
+  static constexpr int ROWS = 16, KEYS = 64, INDEX = 0;
+};
+struct TileWork {
+  static constexpr int ROWS = 256, KEYS = 128, INDEX = 1;
+};
 constexpr int CA_CONSUMERS = 4;                           // warps; each takes 16 keys of a tile
 constexpr int CA_THREADS = 32 * (CA_CONSUMERS + 1);       // and the copying warp
 constexpr int CA_STAGES = 3;
-constexpr int CA_BLOCK_BYTES = CA_KEYS * 128;             // 64 keys x 64 columns
+constexpr int CA_BLOCK_BYTES = StreamWork::KEYS * 128;    // 64 keys x 64 columns
 constexpr int CA_STAGE_BYTES = 4 * CA_BLOCK_BYTES;        // K and V
 constexpr int CA_JOIN_BYTES = 4 * 4 * 128 * 4;            // the warps' sums of an item, a piece at a time
 constexpr int CA_MAX_SEGMENTS = 1024;
@@ -178,15 +184,17 @@ struct CacheArgs {
   int n_q, max_q, max_len, max_prefix, cache_rows;
   long long q_row, q_head, out_row, out_head;
   const int *q_cu, *start, *len, *group_cu, *prefix_start, *prefix_len;
-  const uint16_t *q;
+  const uint16_t *q, *v;
+  long long kv_row, kv_head;
   uint16_t *out;
   float *lse, *weights;
   float scale_log2;                        // scale * log2(e)
   // scratch
-  long long *plan;                         // [0]: all tiles, [1]: tiles per block, [2 + s]: first tile of segment s
+  long long *plan;                         // [2][n_seg + 1] first tile number of every segment, streamed and tiled; the last entry: all tiles
+  int blocks[2];                           // of the two kernels
   int2 *row_owner;                         // [n_q] (sequence, group or -1) of a query row
-  float2 *rec_ml, *full_ml;                // partial results: two per block and row of a tile; [2][n_q * H] (prefix, own) complete ones
-  float *rec_o, *full_o;                   // 128 values each
+  float2 *rec_ml[2], *full_ml;             // partial results: two per block and row of a row tile; [2][n_q * H] (prefix, own) complete ones
+  float *rec_o[2], *full_o;                // 128 values each
   float *lse2;                             // [n_q * H] log2 of a row's sum of 2^x; +inf: the row adds no weight
   float *logits;                           // [n_q * H, pitch] x = scale * log2(e) * q.k; prefix keys first, own keys from own_off on
   long long pitch;
@@ -244,26 +252,33 @@ __device__ __forceinline__ int ca_admitted(const CacheArgs &a, const CaSeg &g, i
   const int n = g.keys - g.nq + 1 + i / a.rep;
   return max(0, min(g.keys, n));
 }
-__device__ __forceinline__ int ca_row_tiles(const CacheArgs &a, const CaSeg &g) { return (g.nq * a.rep + CA_ROWS - 1) / CA_ROWS; }
+__device__ __forceinline__ bool ca_streamed(const CacheArgs &a, const CaSeg &g) { return g.nq * a.rep <= StreamWork::ROWS; }
+template <typename WORK>
+__device__ __forceinline__ int ca_row_tiles(const CacheArgs &a, const CaSeg &g) {
+  return ca_streamed(a, g) == (WORK::INDEX == 0) ? (g.nq * a.rep + WORK::ROWS - 1) / WORK::ROWS : 0;
+}
 // key tiles of row tile rt
+template <typename WORK>
 __device__ __forceinline__ int ca_key_tiles(const CacheArgs &a, const CaSeg &g, int rt) {
-  const int last = min((rt + 1) * CA_ROWS, g.nq * a.rep) - 1;
-  return (ca_admitted(a, g, last) + CA_KEYS - 1) / CA_KEYS;
+  const int last = min((rt + 1) * WORK::ROWS, g.nq * a.rep) - 1;
+  return (ca_admitted(a, g, last) + WORK::KEYS - 1) / WORK::KEYS;
 }
 // key tiles of the first `n` row tiles
+template <typename WORK>
 __device__ __forceinline__ long long ca_tiles_before(const CacheArgs &a, const CaSeg &g, int n) {
-  if (!g.causal) return (long long)n * ((g.keys + CA_KEYS - 1) / CA_KEYS);
+  if (!g.causal) return (long long)n * ((g.keys + WORK::KEYS - 1) / WORK::KEYS);
   long long t = 0;
-  for (int rt = 0; rt < n; ++rt) t += ca_key_tiles(a, g, rt);
+  for (int rt = 0; rt < n; ++rt) t += ca_key_tiles<WORK>(a, g, rt);
   return t;
 }
 
-// The work of a block, item by item (an item: a range of key tiles of one row tile).  Copying warp and consumers walk alike.
+// The work of a block, item by item (an item: a range of key tiles of one row tile).  All roles of a block walk alike.
 struct CaItem {
   CaSeg g;
   int seg, head, rt;
   int kt0, kt1, kt_all;    // key tiles of this block, and of the row tile
 };
+template <typename WORK>
 struct CaWalk {
   long long t, end;        // tile numbers left
   int seg, head, rt, kt;
@@ -285,26 +300,26 @@ struct CaWalk {
     u -= head * per_head;
     rt = 0;
     if (!g.causal) {
-      const int n = ca_key_tiles(a, g, 0);
+      const int n = ca_key_tiles<WORK>(a, g, 0);
       rt = (int)(u / n);
       kt = (int)(u - (long long)rt * n);
     } else {
       int n;
-      while (u >= (n = ca_key_tiles(a, g, rt))) { u -= n; ++rt; }
+      while (u >= (n = ca_key_tiles<WORK>(a, g, rt))) { u -= n; ++rt; }
       kt = (int)u;
     }
   }
   __device__ __forceinline__ bool next(const CacheArgs &a, const long long *off, CaItem &it) {
     if (t >= end) return false;
     it.g = g; it.seg = seg; it.head = head; it.rt = rt;
-    it.kt_all = ca_key_tiles(a, g, rt);
+    it.kt_all = ca_key_tiles<WORK>(a, g, rt);
     it.kt0 = kt;
     it.kt1 = (int)min((long long)it.kt_all, kt + (end - t));
     t += it.kt1 - it.kt0;
     if (t < end) {                         // the next row tile that has keys
       kt = 0;
       do {
-        if (++rt >= ca_row_tiles(a, g)) {
+        if (++rt >= ca_row_tiles<WORK>(a, g)) {
           rt = 0;
           if (++head >= a.kv) {
             head = 0;
@@ -312,23 +327,23 @@ struct CaWalk {
             g = ca_segment(a, seg);
           }
         }
-      } while (ca_key_tiles(a, g, rt) == 0);
+      } while (ca_key_tiles<WORK>(a, g, rt) == 0);
     }
     return true;
   }
 };
 
 // First tile number of every segment into off[0 .. n_seg] (shared memory); all threads of the block.
-template <int THREADS>
+template <typename WORK, int THREADS>
 __device__ __forceinline__ void ca_plan(const CacheArgs &a, long long *off, int n_seg, long long *warp_part) {
   const int per = (n_seg + THREADS - 1) / THREADS, s0 = min(n_seg, (int)threadIdx.x * per), s1 = min(n_seg, s0 + per);
   long long mine = 0;
   for (int s = s0; s < s1; ++s) {
     const CaSeg g = ca_segment(a, s);
-    const long long n = a.kv * ca_tiles_before(a, g, ca_row_tiles(a, g));
+    const long long n = a.kv * ca_tiles_before<WORK>(a, g, ca_row_tiles<WORK>(a, g));
     off[s + 1] = n;
     mine += n;
-    if (!g.valid && blockIdx.x == 0) atomicOr(a.status, (uint32_t)STATUS_BAD_SAMPLE);
+    if (WORK::INDEX == 0 && !g.valid && blockIdx.x == 0) atomicOr(a.status, (uint32_t)STATUS_BAD_SAMPLE);
   }
   long long scan = mine;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -348,7 +363,11 @@ __device__ __forceinline__ void ca_plan(const CacheArgs &a, long long *off, int 
   }
   if (threadIdx.x == 0) off[0] = 0;
   __syncthreads();
+  if (blockIdx.x == 0)
+    for (int s = threadIdx.x; s <= n_seg; s += THREADS) a.plan[WORK::INDEX * (n_seg + 1) + s] = off[s];
 }
+
+__device__ __forceinline__ long long ca_chunk(long long all, int blocks) { return max(1LL, (all + blocks - 1) / blocks); }
 
 // Where the partial result of row tile (seg, head, rt) that block c leaves lies: record 2c if the row tile holds the block's first
 // tile, else 2c + 1 (it then runs past the block's last one).
@@ -394,11 +413,18 @@ __device__ __forceinline__ bool not_finite16(uint32_t w, bool f16) {        // e
   return (w & e) == e || ((w >> 16) & e) == e;
 }
 
+// One arrival for the (converged) warp, which is converged afterwards too: lanes that went on to spin on another barrier while lane 0
+// had still to arrive here kept it from ever doing so.
+__device__ __forceinline__ void mbar_arrive_lane0(uint32_t bar, int lane) {
+  if (lane == 0) mbar_arrive(bar);
+  __syncwarp();
+}
+
 struct CaBook {
   uint64_t full[CA_STAGES], empty[CA_STAGES];
   long long warp_part[8];
   int abort_flag;
-  float2 ml[CA_CONSUMERS][CA_ROWS];
+  float2 ml[CA_CONSUMERS][StreamWork::ROWS];
 };
 
 template <bool F16>
@@ -425,12 +451,8 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   WaitCtx wc{&bk->abort_flag, a.status, STATUS_CACHE_TIMEOUT, a.wait_limit};
   pdl_enter();
   const bool stop = __syncthreads_or((*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) != 0);
-  ca_plan<CA_THREADS>(a, off, n_seg, bk->warp_part);
-  const long long all = off[n_seg], chunk = max(1LL, (all + gridDim.x - 1) / gridDim.x);
-  if (blockIdx.x == 0) {
-    for (int s = threadIdx.x; s <= n_seg; s += CA_THREADS) a.plan[2 + s] = off[s];
-    if (threadIdx.x == 0) { a.plan[0] = all; }
-  }
+  ca_plan<StreamWork, CA_THREADS>(a, off, n_seg, bk->warp_part);
+  const long long all = off[n_seg], chunk = ca_chunk(all, gridDim.x);
   // the query rows' owners, for the join
   for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
     const CaSeg g = ca_segment(a, a.G + b);
@@ -438,7 +460,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     if (!g.valid) continue;
     for (int r = threadIdx.x; r < g.nq; r += CA_THREADS) a.row_owner[g.q0 + r] = make_int2(b, grp);
   }
-  CaWalk walk;
+  CaWalk<StreamWork> walk;
   CaItem it;
   walk.begin(a, off, n_seg, min(all, blockIdx.x * chunk), min(all, (blockIdx.x + 1) * chunk));
   if (stop) walk.end = walk.t;
@@ -453,7 +475,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         if (used >= CA_STAGES) mbar_wait_warp(smem_u32(&bk->empty[pos.slot]), pos.phase ^ 1u, wc);
         if (!__shfl_sync(0xffffffffu, bk->abort_flag, 0)) {
           const uint32_t bar = smem_u32(&bk->full[pos.slot]), dst = base + pos.slot * CA_STAGE_BYTES;
-          const int row = it.g.row0 + kt * CA_KEYS;
+          const int row = it.g.row0 + kt * StreamWork::KEYS;
           mbar_expect_tx_w(bar, CA_STAGE_BYTES, leader);
           tma_load_3d_w(dst, &tmap_k, bar, 0, it.head, row, leader);
           tma_load_3d_w(dst + CA_BLOCK_BYTES, &tmap_k, bar, 64, it.head, row, leader);
@@ -482,7 +504,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     uint32_t qa[8][4];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int i = it.rt * CA_ROWS + gq + 8 * e;
+      const int i = it.rt * StreamWork::ROWS + gq + 8 * e;
       const bool in = i < R;
       const int qr = it.g.q0 + i / a.rep, h = it.head * a.rep + i % a.rep;
       adm[e] = in ? ca_admitted(a, it.g, i) : 0;
@@ -506,7 +528,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     for (int kt = it.kt0; kt < it.kt1; ++kt) {
       mbar_wait_warp(smem_u32(&bk->full[pos.slot]), pos.phase, wc);
       const uint32_t ks = base + pos.slot * CA_STAGE_BYTES, vs = ks + 2 * CA_BLOCK_BYTES;
-      const int j0 = kt * CA_KEYS + warp * 16;   // this warp's first key
+      const int j0 = kt * StreamWork::KEYS + warp * 16;   // this warp's first key
       const int mi = lane >> 3, mr = lane & 7;
       // ---- logits of 16 rows x 16 keys
       float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -616,7 +638,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         mma16816<F16>(o[2 * dt + 1], pa, b[2], b[3]);
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&bk->empty[pos.slot]));
+      mbar_arrive_lane0(smem_u32(&bk->empty[pos.slot]), lane);
       pos.step(CA_STAGES);
     }
     // ---- the four warps' sums of the item
@@ -627,7 +649,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       if (l[e] != l[e] && m[e] == -INFINITY) m[e] = 0.f;      // every logit was NaN: not an empty row
       if (tq == 0) bk->ml[warp][gq + 8 * e] = make_float2(m[e], l[e]);
     }
-    const int rows = min(CA_ROWS, R - it.rt * CA_ROWS);
+    const int rows = min(StreamWork::ROWS, R - it.rt * StreamWork::ROWS);
     const int pad_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : 16, width = 512 / pad_rows;    // columns a piece
     asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
     float f[2];
@@ -637,7 +659,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       for (int w = 0; w < CA_CONSUMERS; ++w) top = fmaxf(top, bk->ml[w][gq + 8 * e].x);
       f[e] = m[e] == -INFINITY ? 0.f : fast_exp2(m[e] - top);
     }
-    const long long before = off[it.seg] + it.head * ((off[it.seg + 1] - off[it.seg]) / a.kv) + ca_tiles_before(a, it.g, it.rt);
+    const long long before = off[it.seg] + it.head * ((off[it.seg + 1] - off[it.seg]) / a.kv) + ca_tiles_before<StreamWork>(a, it.g, it.rt);
     const CaPlace pl = ca_place(before, it.kt_all, chunk);
     for (int c0 = 0; c0 < 128; c0 += width) {
 #pragma unroll
@@ -661,7 +683,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         }
         for (int w = 0; w < CA_CONSUMERS; ++w)
           if (bk->ml[w][r].x != -INFINITY) sum += bk->ml[w][r].y * fast_exp2(bk->ml[w][r].x - top);
-        const int i = it.rt * CA_ROWS + r;
+        const int i = it.rt * StreamWork::ROWS + r;
         const int qr = it.g.q0 + i / a.rep, h = it.head * a.rep + i % a.rep;
         const long long ent = (long long)qr * a.H + h;
         float2 *ml;
@@ -671,15 +693,465 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
           ml = a.full_ml + e;
           dst = a.full_o + e * 128;
         } else {
-          const long long e = (long long)(2 * blockIdx.x + (pl.first <= blockIdx.x * chunk ? 0 : 1)) * CA_ROWS + r;
-          ml = a.rec_ml + e;
-          dst = a.rec_o + e * 128;
+          const long long e = (long long)(2 * blockIdx.x + (pl.first <= blockIdx.x * chunk ? 0 : 1)) * StreamWork::ROWS + r;
+          ml = a.rec_ml[0] + e;
+          dst = a.rec_o[0] + e * 128;
         }
         *reinterpret_cast<float4 *>(dst + c0 + c) = s;
         if (c0 + c == 0) *ml = make_float2(top, sum);
       }
       asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
     }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Segments of more than 16 stacked rows.  Persistent blocks; two row tiles of 128 rows share every key and value tile of 128 keys and take
+// turns on the tensor pipe: S = Q K^T into tensor memory, one thread per row turns it into probabilities relative to a reference
+// maximum, P goes back to tensor memory in the element type, O += P V accumulates there.
+// ---------------------------------------------------------------------------------------
+constexpr int CT_THREADS = 384;                 // warp 0: key / value copies, 1: MMA issue, 2: value rows to be cleared, 3: query rows, 4-11: softmax
+constexpr int CT_TILE_BYTES = 128 * 128 * 2;
+constexpr int CT_BLOCK_BYTES = CT_TILE_BYTES / 2;
+constexpr int CT_SLOTS = 4;                     // ring of key and value tiles in the order K0 V0 K1 V1 ...
+constexpr int CT_STAGE_BYTES = 32 * 64;         // per softmax warp: 32 rows x 16 floats
+constexpr int CT_STAGE_OFF = (2 + CT_SLOTS) * CT_TILE_BYTES;
+constexpr int CT_BOOK_OFF = CT_STAGE_OFF + 8 * CT_STAGE_BYTES;
+constexpr uint32_t CT_TMEM_COLS = 512, CT_S_COL = 256, CT_P_COL = 384;   // O of both row tiles, one S that they use in turn, P of both
+// A tile's sum relative to the reference at which the reference moves: no probability may leave the element type's range.
+constexpr float CT_SUM_LIMIT_BF16 = 1.0995116e12f, CT_SUM_LIMIT_F16 = 32768.f;
+
+struct CtBook {
+  uint64_t full[CT_SLOTS], empty[CT_SLOTS], raw[CT_SLOTS];
+  uint64_t q_full[2], q_empty[2], s_full[2], s_empty, p_ready[2], pv_done[2], mma_done;
+  long long warp_part[CT_THREADS / 32];
+  uint32_t tmem_base;
+  int abort_flag;
+  int bad[4];              // the item (modulo 4) has value rows with infinities or NaN that not all of its query rows admit
+};
+
+// The part of an item that row tile g of the pair takes: its first `n` key tiles.
+__device__ __forceinline__ int ct_active(const CacheArgs &a, const CaItem &it, int g) {
+  const int R = it.g.nq * a.rep, i0 = it.rt * TileWork::ROWS + g * 128;
+  if (i0 >= R) return 0;
+  const int n = (ca_admitted(a, it.g, min(i0 + 128, R) - 1) + 127) / 128;
+  return max(0, min(it.kt1, n) - it.kt0);
+}
+// Key tile kt holds rows that no query row of the pair admits, or not all of them do: its values pass through warp 2.
+__device__ __forceinline__ bool ct_passed(const CacheArgs &a, const CaItem &it, int kt) {
+  return (kt + 1) * 128 > ca_admitted(a, it.g, it.rt * TileWork::ROWS);
+}
+
+template <bool F16>
+__global__ void __launch_bounds__(CT_THREADS, 1)
+ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CacheArgs a) {
+  extern __shared__ __align__(1024) uint8_t ct_smem[];
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t base = smem_u32(ct_smem), q_smem = base, ring = base + 2 * CT_TILE_BYTES;
+  CtBook *bk = reinterpret_cast<CtBook *>(ct_smem + CT_BOOK_OFF);
+  long long *off = reinterpret_cast<long long *>(bk + 1);
+  const int n_seg = a.G + a.B;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < CT_SLOTS; ++s) {
+      mbar_init(smem_u32(&bk->full[s]), 1);
+      mbar_init(smem_u32(&bk->empty[s]), 1);
+      mbar_init(smem_u32(&bk->raw[s]), 1);
+    }
+    for (int g = 0; g < 2; ++g) {
+      mbar_init(smem_u32(&bk->q_full[g]), 1);
+      mbar_init(smem_u32(&bk->q_empty[g]), 1);
+      mbar_init(smem_u32(&bk->s_full[g]), 1);
+      mbar_init(smem_u32(&bk->p_ready[g]), 4);            // the row tile's four softmax warps
+      mbar_init(smem_u32(&bk->pv_done[g]), 1);
+    }
+    mbar_init(smem_u32(&bk->s_empty), 4);                 // the softmax warps that have taken an S into registers
+    mbar_init(smem_u32(&bk->mma_done), 1);
+    bk->abort_flag = 0;
+    for (int i = 0; i < 4; ++i) bk->bad[i] = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&tmap_k);
+    tma_prefetch_desc(&tmap_v);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&bk->tmem_base), CT_TMEM_COLS);
+    tmem_relinquish();
+    tc_fence_before();
+  }
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = bk->tmem_base;
+  WaitCtx wc{&bk->abort_flag, a.status, STATUS_CACHE_TIMEOUT, a.wait_limit};
+  pdl_enter();
+  const bool stop = __syncthreads_or((*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) != 0);
+  ca_plan<TileWork, CT_THREADS>(a, off, n_seg, bk->warp_part);
+  const long long all = off[n_seg], chunk = ca_chunk(all, gridDim.x);
+  CaWalk<TileWork> walk;
+  CaItem it;
+  walk.begin(a, off, n_seg, min(all, blockIdx.x * chunk), min(all, (blockIdx.x + 1) * chunk));
+  if (stop) walk.end = walk.t;
+
+  // The launch gives every thread 168 registers; a softmax thread holds its row's 128 logits and needs more, the first
+  // warpgroup needs few: 128 x 72 + 256 x 216 = 384 x 168.
+  if (warp < 4) {
+    reg_dec<72>();
+    if (warp == 0) {
+      // ---------------------------------------------------------------- key / value tiles
+      const uint32_t leader = warp_leader();
+      int tc = 0, issued = 0;
+      uint32_t raw_any = 0u, raw_odd = 0u, raw_last = 0u;     // per ring slot: copies through `raw`: any, an odd number, the latest one
+      while (walk.next(a, off, it)) {
+#pragma unroll 1
+        for (int kt = it.kt0; kt < it.kt1; ++kt) {
+          const bool passed = ct_passed(a, it, kt);
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv, ++tc) {
+            const int s = tc % CT_SLOTS;
+            if (tc >= CT_SLOTS) mbar_wait_warp(smem_u32(&bk->empty[s]), ((tc / CT_SLOTS) - 1) & 1, wc);
+            if (__shfl_sync(0xffffffffu, bk->abort_flag, 0)) continue;
+            const bool past = passed && kv == 1;
+            const uint32_t bar = smem_u32(past ? &bk->raw[s] : &bk->full[s]), dst = ring + s * CT_TILE_BYTES, bit = 1u << s;
+            raw_last = past ? raw_last | bit : raw_last & ~bit;
+            if (past) { raw_any |= bit; raw_odd ^= bit; }
+            const int row = it.g.row0 + kt * 128;
+            mbar_expect_tx_w(bar, CT_TILE_BYTES, leader);
+            tma_load_3d_w(dst, kv ? &tmap_v : &tmap_k, bar, 0, it.head, row, leader);
+            tma_load_3d_w(dst + CT_BLOCK_BYTES, kv ? &tmap_v : &tmap_k, bar, 64, it.head, row, leader);
+            issued = tc + 1;
+          }
+        }
+      }
+      // every copy issued has landed before the block leaves
+      for (int s = 0; s < CT_SLOTS; ++s) {
+        const int fills = issued > s ? (issued - s + CT_SLOTS - 1) / CT_SLOTS : 0;
+        if ((raw_any >> s) & 1u) mbar_wait_drain(smem_u32(&bk->raw[s]), ((raw_odd >> s) & 1u) ^ 1u, CA_WAIT_LIMIT);
+        if (fills > 0 && !((raw_last >> s) & 1u)) mbar_wait_drain(smem_u32(&bk->full[s]), (fills - 1) & 1, CA_WAIT_LIMIT);
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // ---------------------------------------------------------------- MMA issuer
+      // Per key tile and row tile: S of this key tile, then P V of the previous one (an S never waits in the pipe behind a P V that could
+      // as well run after it).  The whole warp walks the loop and stays converged (see warp_leader).
+      const uint32_t leader = warp_leader();
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem_base, 0);
+      const uint32_t idesc_s = F16 ? umma_idesc_f16(128, 128) : umma_idesc_bf16(128, 128), idesc_o = idesc_s | UMMA_IDESC_B_MN;
+      const uint64_t qdesc = umma_desc_sw128(q_smem), tile0 = umma_desc_sw128(ring), vtile0 = umma_desc_sw128_mn(ring, CT_BLOCK_BYTES);
+      int t0 = 0;                                 // first tile of the item in the ring
+      int qc[2] = {0, 0}, pc[2] = {0, 0}, sn = 0; // query tiles, P tiles and S so far
+      while (walk.next(a, off, it)) {
+        const int n[2] = {ct_active(a, it, 0), ct_active(a, it, 1)}, n_max = it.kt1 - it.kt0;
+        for (int kt = 0; kt <= n_max; ++kt) {
+          const int tk = t0 + 2 * kt, tv = tk - 1;            // ring tiles: K of this key tile, V of the previous one
+          const int sk = tk & (CT_SLOTS - 1), sv = tv & (CT_SLOTS - 1);
+          if (kt < n_max) mbar_wait_warp(smem_u32(&bk->full[sk]), (tk / CT_SLOTS) & 1, wc);
+          if (kt > 0) mbar_wait_warp(smem_u32(&bk->full[sv]), (tv / CT_SLOTS) & 1, wc);
+          const uint64_t kdesc = tile0 + sk * (CT_TILE_BYTES >> 4), vdesc = vtile0 + sv * (CT_TILE_BYTES >> 4);
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            if (kt < n[g]) {
+              if (kt == 0) {
+                mbar_wait_warp(smem_u32(&bk->q_full[g]), qc[g] & 1, wc);
+                ++qc[g];
+              }
+              if (sn > 0) mbar_wait_warp(smem_u32(&bk->s_empty), (sn - 1) & 1, wc);     // the previous S is in registers
+              ++sn;
+              tc_fence_after();
+              tc_mma_bf16_k128_w(tm + CT_S_COL, qdesc + g * (CT_TILE_BYTES >> 4), kdesc, CT_BLOCK_BYTES, CT_BLOCK_BYTES, idesc_s, leader);
+              tc_commit_w(smem_u32(&bk->s_full[g]), leader);
+              if (kt == n[g] - 1) tc_commit_w(smem_u32(&bk->q_empty[g]), leader);
+            }
+            if (kt > 0 && kt - 1 < n[g]) {
+              mbar_wait_warp(smem_u32(&bk->p_ready[g]), pc[g] & 1, wc);
+              ++pc[g];
+              tc_fence_after();
+#pragma unroll
+              for (int kk = 0; kk < 8; ++kk)
+                tc_mma_bf16_ta_w(tm + g * 128, tm + CT_P_COL + g * 64 + kk * 8, vdesc + kk * (2048 >> 4), idesc_o,
+                                 (kt > 1 || kk > 0) ? 1u : 0u, leader);
+              tc_commit_w(smem_u32(&bk->pv_done[g]), leader);
+            }
+          }
+          if (kt < n_max) tc_commit_w(smem_u32(&bk->empty[sk]), leader);
+          if (kt > 0) tc_commit_w(smem_u32(&bk->empty[sv]), leader);
+        }
+        t0 += 2 * n_max;
+      }
+      // every MMA this warp issued has completed before tensor memory is given back
+      tc_commit_w(smem_u32(&bk->mma_done), leader);
+      mbar_wait_drain(smem_u32(&bk->mma_done), 0, CA_WAIT_LIMIT);
+      __syncwarp();
+    } else if (warp == 2) {
+      // ---------------------------------------------------------------- value rows that must not reach every query row
+      // Their probabilities are exactly zero there, but 0 * NaN is NaN: rows past the segment are cleared, and elements that are not finite
+      // in rows that only some query rows admit are cleared too and added by the softmax warps at the item's end (bk->bad).
+      int t0 = 0, ic = 0;
+      uint32_t raw_phase = 0u;                    // per ring slot
+      while (walk.next(a, off, it)) {
+        if (lane == 0) *reinterpret_cast<volatile int *>(&bk->bad[ic & 3]) = 0;
+        __syncwarp();
+        for (int kt = it.kt0; kt < it.kt1; ++kt) {
+          if (!ct_passed(a, it, kt)) continue;
+          const int s = (t0 + 2 * (kt - it.kt0) + 1) & (CT_SLOTS - 1);
+          const bool landed = mbar_wait(smem_u32(&bk->raw[s]), (raw_phase >> s) & 1u, wc);
+          raw_phase ^= 1u << s;
+          if (!__all_sync(0xffffffffu, landed)) continue;     // (gave up: the copy may not have been issued)
+          uint8_t *tile = ct_smem + (2 + s) * CT_TILE_BYTES;
+          const int rows = max(0, min(128, it.g.keys - kt * 128));          // rows of the segment
+          const int free_rows = max(0, min(rows, ca_admitted(a, it.g, it.rt * TileWork::ROWS) - kt * 128));   // ... that all query rows admit
+          bool bad = false;
+          for (int i = free_rows * 8 + lane; i < 128 * 8; i += 32)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint4 *p = reinterpret_cast<uint4 *>(tile + h * CT_BLOCK_BYTES) + i;
+              if (i >= rows * 8) {
+                *p = make_uint4(0u, 0u, 0u, 0u);
+              } else {
+                uint4 x = *p;
+                if (not_finite16(x.x, F16) || not_finite16(x.y, F16) || not_finite16(x.z, F16) || not_finite16(x.w, F16)) {
+                  bad = true;
+                  uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    if (not_finite16(w[e] & 0xffffu, F16)) w[e] &= 0xffff0000u;
+                    if (not_finite16(w[e] & 0xffff0000u, F16)) w[e] &= 0xffffu;
+                  }
+                  *p = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+              }
+            }
+          if (__any_sync(0xffffffffu, bad) && lane == 0) *reinterpret_cast<volatile int *>(&bk->bad[ic & 3]) = 1;
+          __threadfence_block();
+          fence_proxy_async();
+          __syncwarp();
+          mbar_arrive_lane0(smem_u32(&bk->full[s]), lane);
+        }
+        t0 += 2 * (it.kt1 - it.kt0);
+        ++ic;
+      }
+    } else {
+      // ---------------------------------------------------------------- query rows
+      // (gathered: stacked row i is query row i / rep, head i % rep of the key / value head; rows past the last one are zero up to the next
+      // multiple of 32, so that their lanes of a softmax warp hold nothing that would move a reference)
+      int qc[2] = {0, 0};
+      while (walk.next(a, off, it)) {
+        const int R = it.g.nq * a.rep;
+#pragma unroll 1
+        for (int g = 0; g < 2; ++g) {
+          if (ct_active(a, it, g) == 0) continue;
+          if (qc[g] >= 1) mbar_wait_warp(smem_u32(&bk->q_empty[g]), (qc[g] - 1) & 1, wc);
+          ++qc[g];
+          const int i0 = it.rt * TileWork::ROWS + g * 128, n = min(128, R - i0);
+          const uint32_t dst = q_smem + g * CT_TILE_BYTES;
+          const int c = lane & 15;                // 16-byte piece of a row
+          for (int r = lane >> 4; r < ((n + 31) & ~31); r += 2) {
+            const int i = i0 + r;
+            if (r >= n) {
+              *reinterpret_cast<uint4 *>(ct_smem + g * CT_TILE_BYTES + (c >> 3) * CT_BLOCK_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+              continue;
+            }
+            const uint16_t *src = a.q + (long long)(it.g.q0 + i / a.rep) * a.q_row + (long long)(it.head * a.rep + i % a.rep) * a.q_head + c * 8;
+            cp_async16(dst + (c >> 3) * CT_BLOCK_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4), src);
+          }
+          cp_async_commit();
+          cp_async_wait<0>();
+          fence_proxy_async();
+          __syncwarp();
+          mbar_arrive_lane0(smem_u32(&bk->q_full[g]), lane);
+        }
+      }
+    }
+  } else {
+    reg_inc<216>();
+    // ------------------------------------------------------------------ softmax: one thread per stacked row
+    const int g = (warp - 4) >> 2;                // row tile of this warpgroup
+    const int quarter = warp & 3;                 // the TMEM lanes this warp may read
+    const int lrow = quarter * 32 + lane;
+    const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t s_addr = lane_addr + CT_S_COL, p_addr = lane_addr + CT_P_COL + g * 64, o_addr = lane_addr + g * 128;
+    const float scale = a.scale_log2;
+    const uint64_t scale2 = f2_pack(scale, scale);
+    uint8_t *stage = ct_smem + CT_STAGE_OFF + (warp - 4) * CT_STAGE_BYTES;
+    int sc = 0, ic = 0;                           // key tiles and items so far
+    for (; walk.next(a, off, it); ++ic) {
+      const int R = it.g.nq * a.rep, i = it.rt * TileWork::ROWS + g * 128 + lrow, i_lo = i - lane;
+      if (i_lo - quarter * 32 >= R) continue;     // no such row tile
+      const int n_act = ct_active(a, it, g);
+      const bool live = i_lo < R;                 // the warp has rows
+      const int adm = i < R ? ca_admitted(a, it.g, i) : 0, adm_lo = live ? ca_admitted(a, it.g, i_lo) : 0;
+      const long long entry = i < R ? (long long)(it.g.q0 + i / a.rep) * a.H + it.head * a.rep + i % a.rep : -1;
+      // p = 2^(x * scale - ref).  The reference is the maximum of the row's first key tile and then stays: one below the running
+      // maximum only scales the sums.  Should a tile's sum outgrow the limit in some row of the warp, that tile is done again with the
+      // row's true maximum as the new reference (O and the sum so far are rescaled).
+      float neg_ref = 0.f, l_run = 0.f;
+      bool unset = true;                          // no logit above -inf so far
+      for (int t = 0; t < n_act; ++t, ++sc) {
+        const int j0 = (it.kt0 + t) * 128;
+        mbar_wait_warp(smem_u32(&bk->s_full[g]), sc & 1, wc);    // (no lane may still wait for a phase when lane 0 has arrived for it)
+        tc_fence_after();
+        if (!live) {                              // (one arrival per phase: the previous P V comes first here too)
+          mbar_arrive_lane0(smem_u32(&bk->s_empty), lane);
+          if (t > 0) mbar_wait_warp(smem_u32(&bk->pv_done[g]), (sc - 1) & 1, wc);
+          mbar_arrive_lane0(smem_u32(&bk->p_ready[g]), lane);
+          continue;
+        }
+        uint32_t xr[128];
+#pragma unroll
+        for (int c = 0; c < 128; c += 32) tmem_ld32p(s_addr + c, xr + c);
+        tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        mbar_arrive_lane0(smem_u32(&bk->s_empty), lane);
+        if (j0 + 128 > adm_lo) {
+          const int lim = adm - j0;
+#pragma unroll
+          for (int c = 0; c < 128; ++c)
+            if (c >= lim) xr[c] = __float_as_uint(-INFINITY);
+        }
+        if (a.logits) {
+          // through shared memory, 16 columns at a time (16-byte chunk c of row r at c ^ ((r >> 1) & 3)): a store covers eight pieces of 64 bytes
+#pragma unroll
+          for (int c0 = 0; c0 < 128; c0 += 16) {
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              float4 v;
+              v.x = __uint_as_float(xr[c0 + 4 * c]) * scale; v.y = __uint_as_float(xr[c0 + 4 * c + 1]) * scale;
+              v.z = __uint_as_float(xr[c0 + 4 * c + 2]) * scale; v.w = __uint_as_float(xr[c0 + 4 * c + 3]) * scale;
+              *reinterpret_cast<float4 *>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = v;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int r8 = 0; r8 < 32; r8 += 8) {
+              const int rr = r8 + (lane >> 2), c = lane & 3;
+              const long long e = __shfl_sync(0xffffffffu, entry, rr);
+              const float4 v = *reinterpret_cast<const float4 *>(stage + rr * 64 + ((c ^ ((rr >> 1) & 3)) << 4));
+              if (e >= 0) *reinterpret_cast<float4 *>(a.logits + e * a.pitch + (it.g.causal ? a.own_off : 0) + j0 + c0 + 4 * c) = v;
+            }
+          }
+          __syncwarp();
+        }
+        if (t > 0) {
+          mbar_wait(smem_u32(&bk->pv_done[g]), (sc - 1) & 1, wc);      // O is complete up to here, and P may be overwritten
+          tc_fence_after();
+        }
+        bool move = unset, moved = false, again = __any_sync(0xffffffffu, unset && j0 < adm);
+        float tile_sum;
+#pragma unroll 1
+        while (true) {
+          if (again) {
+            float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};       // four independent chains
+#pragma unroll
+            for (int c = 0; c < 128; c += 8)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) mx4[e] = max3(mx4[e], __uint_as_float(xr[c + e]), __uint_as_float(xr[c + 4 + e]));
+            const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+            const float neg = mx == -INFINITY ? 0.f : -mx * scale;
+            if (t > 0) {
+              const float f = move && !unset ? fast_exp2(neg - neg_ref) : 1.0f;
+#pragma unroll 1
+              for (int c0 = 0; c0 < 128; c0 += 16) {
+                uint32_t r[16];
+                tmem_ld16(o_addr + c0, r);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
+                tmem_st16(o_addr + c0, r);
+              }
+              l_run *= f;
+            }
+            if (move) {
+              moved = true;
+              neg_ref = neg;
+              if (mx != -INFINITY) unset = false;
+            }
+          }
+          const uint64_t neg2 = f2_pack(neg_ref, neg_ref);
+          uint64_t sum2[2] = {0ull, 0ull};          // even and odd keys apart, two chains
+#pragma unroll
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float p0, p1;
+              f2_unpack(f2_fma(f2_pack(__uint_as_float(xr[c0 + 2 * e]), __uint_as_float(xr[c0 + 2 * e + 1])), scale2, neg2), p0, p1);
+              p0 = fast_exp2(p0);
+              p1 = fast_exp2(p1);
+              sum2[e & 1] = f2_add(sum2[e & 1], f2_pack(p0, p1));
+              w[e] = pack2_t<F16>(p0, p1);
+            }
+            tmem_st16(p_addr + (c0 >> 1), w);
+          }
+          float s0, s1;
+          f2_unpack(f2_add(sum2[0], sum2[1]), s0, s1);
+          tile_sum = s0 + s1;
+          move = !moved && !(tile_sum < (F16 ? CT_SUM_LIMIT_F16 : CT_SUM_LIMIT_BF16));     // (relative to the true maximum no sum exceeds 128)
+          if (!__any_sync(0xffffffffu, move)) break;
+          again = true;
+        }
+        l_run += tile_sum;
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        mbar_arrive_lane0(smem_u32(&bk->p_ready[g]), lane);
+      }
+      // ---- the item's part of the rows
+      if (n_act > 0) {
+        mbar_wait_warp(smem_u32(&bk->pv_done[g]), (sc - 1) & 1, wc);
+        tc_fence_after();
+      }
+      if (!live) continue;
+      const long long before = off[it.seg] + it.head * ((off[it.seg + 1] - off[it.seg]) / a.kv) + ca_tiles_before<TileWork>(a, it.g, it.rt);
+      const CaPlace pl = ca_place(before, it.kt_all, chunk);
+      const bool complete = pl.c0 == pl.c1;
+      // NaN in every logit leaves no maximum, but the row is not an empty one
+      const bool none = n_act == 0 || (unset && l_run == 0.f);
+      const long long at = i >= R ? -1 : complete ? (it.g.causal ? (long long)a.n_q * a.H : 0) + entry
+                                                  : (long long)(2 * blockIdx.x + (pl.first <= blockIdx.x * chunk ? 0 : 1)) * TileWork::ROWS + g * 128 + lrow;
+      const bool write = !bk->abort_flag;
+      if (at >= 0 && write) (complete ? a.full_ml : a.rec_ml[1])[at] = none ? make_float2(-INFINITY, 0.f) : make_float2(-neg_ref, l_run);
+      if (n_act == 0) continue;
+      float *dst = complete ? a.full_o : a.rec_o[1];
+      const bool bad = *reinterpret_cast<volatile int *>(&bk->bad[ic & 3]) != 0;
+#pragma unroll 1
+      for (int c0 = 0; c0 < 128; c0 += 16) {
+        uint32_t r[16];
+        tmem_ld16(o_addr + c0, r);
+        tmem_wait_ld();
+        if (bad) {                                  // what warp 2 left out
+          const int from = max(it.kt0 * 128, ca_admitted(a, it.g, it.rt * TileWork::ROWS)), to = min(it.kt1 * 128, adm);
+          for (int j = from; j < to; ++j) {
+            const uint16_t *v = a.v + (long long)(it.g.row0 + j) * a.kv_row + (long long)it.head * a.kv_head + c0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              uint32_t w;
+              asm volatile("ld.global.u32 %0, [%1];" : "=r"(w) : "l"(v + 2 * e));
+              const float2 x = unpack2_t<F16>(w);
+              if (!isfinite(x.x)) r[2 * e] = __float_as_uint(__uint_as_float(r[2 * e]) + x.x);
+              if (!isfinite(x.y)) r[2 * e + 1] = __float_as_uint(__uint_as_float(r[2 * e + 1]) + x.y);
+            }
+          }
+          __syncwarp();
+        }
+        __syncwarp();                               // the previous piece has been read
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          *reinterpret_cast<uint4 *>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int r8 = 0; r8 < 32; r8 += 8) {
+          const int rr = r8 + (lane >> 2), c = lane & 3;
+          const long long e = __shfl_sync(0xffffffffu, at, rr);
+          const uint4 x = *reinterpret_cast<const uint4 *>(stage + rr * 64 + ((c ^ ((rr >> 1) & 3)) << 4));
+          if (e >= 0 && write) *reinterpret_cast<uint4 *>(dst + e * 128 + c0 + 4 * c) = x;
+        }
+      }
+      tc_fence_before();                            // the next item's first P (and so its first P V) comes after these loads
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, CT_TMEM_COLS);
   }
 }
 
@@ -706,7 +1178,7 @@ __device__ __forceinline__ long long ld_prev64(const long long *p) {
 
 template <bool F16>
 __global__ void __launch_bounds__(CA_JOIN_THREADS)
-ca_join_kernel(const __grid_constant__ CacheArgs a, int stream_blocks) {
+ca_join_kernel(const __grid_constant__ CacheArgs a) {
   pdl_enter();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long entry = (long long)blockIdx.x * (CA_JOIN_THREADS / 32) + warp;
@@ -724,7 +1196,7 @@ ca_join_kernel(const __grid_constant__ CacheArgs a, int stream_blocks) {
     if (lane == 0) a.lse2[entry] = INFINITY;
     return;
   }
-  const long long all = ld_prev64(a.plan), chunk = max(1LL, (all + stream_blocks - 1) / stream_blocks);
+  const int n_seg = a.G + a.B;
   float top = -INFINITY, sum = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](float2 ml, float4 o) {
@@ -738,21 +1210,27 @@ ca_join_kernel(const __grid_constant__ CacheArgs a, int stream_blocks) {
     const int s = part == 0 ? own.y : a.G + own.x;
     if (part == 0) seg[0] = ca_segment(a, s);
     const CaSeg &g = seg[part];
-    const int i = (qr - g.q0) * a.rep + h % a.rep, rt = i / CA_ROWS, r = i % CA_ROWS;
-    const int n = ca_key_tiles(a, g, rt);
-    if (n == 0) continue;
-    const long long off0 = ld_prev64(a.plan + 2 + s), off1 = ld_prev64(a.plan + 3 + s);
-    const CaPlace pl = ca_place(off0 + (h / a.rep) * ((off1 - off0) / a.kv) + ca_tiles_before(a, g, rt), n, chunk);
-    if (pl.c0 == pl.c1) {
-      const long long e = (long long)part * a.n_q * a.H + entry;
-      add(ld_prev2f(a.full_ml + e), ld_prev4f(a.full_o + e * 128 + lane * 4));
-      continue;
-    }
+    const int i = (qr - g.q0) * a.rep + h % a.rep;
+    auto gather = [&](auto work) {
+      using WORK = decltype(work);
+      const int rt = i / WORK::ROWS, r = i % WORK::ROWS, n = ca_key_tiles<WORK>(a, g, rt);
+      if (n == 0) return;
+      const long long *plan = a.plan + WORK::INDEX * (n_seg + 1);
+      const long long off0 = ld_prev64(plan + s), off1 = ld_prev64(plan + s + 1), chunk = ca_chunk(ld_prev64(plan + n_seg), a.blocks[WORK::INDEX]);
+      const CaPlace pl = ca_place(off0 + (h / a.rep) * ((off1 - off0) / a.kv) + ca_tiles_before<WORK>(a, g, rt), n, chunk);
+      if (pl.c0 == pl.c1) {
+        const long long e = (long long)part * a.n_q * a.H + entry;
+        add(ld_prev2f(a.full_ml + e), ld_prev4f(a.full_o + e * 128 + lane * 4));
+        return;
+      }
 #pragma unroll 4
-    for (int c = pl.c0; c <= pl.c1; ++c) {
-      const long long e = (long long)(2 * c + (pl.first <= c * chunk ? 0 : 1)) * CA_ROWS + r;
-      add(ld_prev2f(a.rec_ml + e), ld_prev4f(a.rec_o + e * 128 + lane * 4));
-    }
+      for (int c = pl.c0; c <= pl.c1; ++c) {
+        const long long e = (long long)(2 * c + (pl.first <= c * chunk ? 0 : 1)) * WORK::ROWS + r;
+        add(ld_prev2f(a.rec_ml[WORK::INDEX] + e), ld_prev4f(a.rec_o[WORK::INDEX] + e * 128 + lane * 4));
+      }
+    };
+    if (ca_streamed(a, g)) gather(StreamWork{});
+    else gather(TileWork{});
   }
   const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);    // (NaN stays NaN)
   uint16_t *dst = a.out + (long long)qr * a.out_row + (long long)h * a.out_head + lane * 4;

@@ -194,6 +194,8 @@ CASES = {
     "group_rows": dict(lens=[70, 100, 33], nq=[70, 64, 33], H=4, kv=4, groups=[(0, 3, 500)]),
     "group_rows_gqa": dict(lens=[40, 90], nq=[33, 90], H=6, kv=2, groups=[(0, 2, 300)]),
     "prefix_only": dict(lens=[0, 0, 0], nq=[1, 3, 1], H=4, kv=1, groups=[(0, 3, 129)]),
+    "many_items": dict(lens=[150, 40, 70, 200, 33, 256], nq=[150, 33, 70, 181, 33, 130], H=24, kv=24, groups=[(0, 2, 300), (2, 6, 1000)]),
+    "many_items_gqa": dict(lens=[100] * 30, nq=[17] * 30, H=32, kv=8, groups=[(0, 30, 700)]),
     "late_rows": dict(lens=[2, 1], nq=[9, 5], H=2, kv=2, groups=[(0, 2, 70)]),
 }
 
