@@ -297,10 +297,11 @@ asap_status asap_rope(asap_ctx *ctx, const asap_rope_plan *plan, const asap_rope
  * and, if `weights` is given, weights[j] += (1 / H) sum over the query rows and heads of p_j, for every cache row j (in a fixed
  * order: a call gives the same bits every time).  A query row that admits nothing gets out = 0 and lse = -infinity.  Rows that
  * no query row admits are not looked at, whatever they hold; a row that only later query rows admit does not touch earlier ones.
+ * Offsets (q_cu, group_cu) that do not ascend within [0, n_q] and [0, B] skip the whole call.
  * Probabilities enter the second product rounded to the element type; logits, sums and outputs before the last rounding are fp32. */
 typedef struct {
   int32_t B, H, kv_heads, head_dim, dtype;  /* head_dim must be 128; kv_heads divides H */
-  int32_t n_q;                              /* query rows in total, q_cu[B] */
+  int32_t n_q;                              /* rows of q and out; q_cu[B] may be smaller, the rows behind it stay as they are */
   int32_t max_q, max_len, max_prefix;       /* host-known bounds of the query rows, own rows and prefix rows */
   int32_t n_groups;                         /* 0: no prefixes.  B + n_groups <= 1024 */
   int32_t cache_rows;                       /* rows of k and v */

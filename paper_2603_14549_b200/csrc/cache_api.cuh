@@ -17,10 +17,10 @@ struct DeviceGuard {
 };
 
 size_t ca_smem_bytes(int n_seg) {
-  return CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES + sizeof(CaBook) + (size_t)(n_seg + 1) * sizeof(long long);
+  return CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES + CA_JOBS * CA_Q_BYTES + sizeof(CaBook) + (size_t)(n_seg + 1) * sizeof(int);
 }
 
-size_t ct_smem_bytes(int n_seg) { return CT_BOOK_OFF + sizeof(CtBook) + (size_t)(n_seg + 1) * sizeof(long long); }
+size_t ct_smem_bytes(int n_seg) { return CT_BOOK_OFF + sizeof(CtBook) + (size_t)(n_seg + 1) * sizeof(int); }
 
 // Elements that [rows, heads, dim] with the given strides spans.
 long long span_of(long long rows, long long heads, long long dim, long long row, long long head) {
@@ -77,19 +77,26 @@ asap_status check_cache_attention(asap_ctx *ctx, const asap_cache_attention_args
 struct CaLayout {
   size_t bytes = 0;
   int blocks[2] = {0, 0};        // of the streaming and of the tile kernel; 0: nothing to launch
+  bool too_large = false;
 };
+constexpr long long CA_MAX_NUMBERS = 1LL << 30;    // key tiles are numbered in 32 bits
 CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint8_t *at, CacheArgs *a) {
   CaLayout l;
   const size_t entries = (size_t)p->n_q * p->H, n_seg = (size_t)p->B + p->n_groups;
   // no more blocks than there can be key tiles; no tile kernel where no segment can have more than 16 stacked rows
   const long long rep = p->H / p->kv_heads, heads = p->kv_heads, group_rows = p->n_groups > 0 && p->max_prefix > 0 ? p->n_q * rep : 0;
-  auto tiles = [&](long long segs, long long rows, long long keys, int R, int K) { return segs * ((rows + R - 1) / R) * ((keys + K - 1) / K) * heads; };
+  auto numbers = [&](long long segs, long long rows, long long keys, auto work) {
+    using WORK = decltype(work);
+    return segs * ((rows + WORK::ROWS - 1) / WORK::ROWS) * ((keys + WORK::KEYS - 1) / WORK::KEYS + WORK::EXTRA) * heads;
+  };
   auto at_most = [](long long n, long long most) { return (int)(n < 1 ? 1 : n < most ? n : most); };
   const long long own_rows = p->max_q * rep, S = StreamWork::ROWS;
-  l.blocks[0] = at_most(tiles(p->B, 1, p->max_len, 1, StreamWork::KEYS) + (group_rows ? tiles(p->n_groups, 1, p->max_prefix, 1, StreamWork::KEYS) : 0), 2LL * ctx->num_sms);
-  if (own_rows > S || group_rows > S)
-    l.blocks[1] = at_most((own_rows > S ? tiles(p->B, own_rows, p->max_len, TileWork::ROWS, TileWork::KEYS) : 0) +
-                              (group_rows > S ? tiles(p->n_groups, group_rows, p->max_prefix, TileWork::ROWS, TileWork::KEYS) : 0), ctx->num_sms);
+  const long long streamed = numbers(p->B, 1, p->max_len, StreamWork{}) + (group_rows ? numbers(p->n_groups, 1, p->max_prefix, StreamWork{}) : 0);
+  const long long tiled = (own_rows > S ? numbers(p->B, own_rows, p->max_len, TileWork{}) : 0) +
+                          (group_rows > S ? numbers(1, group_rows + (long long)TileWork::ROWS * p->n_groups, p->max_prefix, TileWork{}) : 0);
+  l.blocks[0] = at_most(streamed, 2LL * ctx->num_sms);
+  if (tiled > 0) l.blocks[1] = at_most(tiled, ctx->num_sms);
+  l.too_large = streamed > CA_MAX_NUMBERS || tiled > CA_MAX_NUMBERS;
   auto carve = [&](size_t bytes) {
     const size_t o = l.bytes;
     l.bytes = align_up(l.bytes + bytes, 256);
@@ -98,11 +105,11 @@ CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint
   const size_t rec[2] = {(size_t)2 * l.blocks[0] * StreamWork::ROWS, (size_t)2 * l.blocks[1] * TileWork::ROWS};
   const long long own_off = p->n_groups ? ((long long)p->max_prefix + 127) / 128 * 128 : 0;
   const long long pitch = own_off + ((long long)p->max_len + 127) / 128 * 128;       // (a key tile is written whole)
-  uint8_t *plan = carve(2 * (n_seg + 1) * 8), *owner = carve((size_t)p->n_q * 8), *rec_ml0 = carve(rec[0] * 8), *rec_ml1 = carve(rec[1] * 8),
+  uint8_t *plan = carve((2 * (n_seg + 1) + 1) * 4), *rows = carve((size_t)p->n_q * sizeof(CaRow)), *rec_ml0 = carve(rec[0] * 8), *rec_ml1 = carve(rec[1] * 8),
           *full_ml = carve(2 * entries * 8), *rec_o0 = carve(rec[0] * 512), *rec_o1 = carve(rec[1] * 512), *full_o = carve(2 * entries * 512),
           *lse2 = carve(entries * 4), *logits = p->weights ? carve(entries * (size_t)pitch * 4) : nullptr;
   if (a) {
-    a->plan = reinterpret_cast<long long *>(plan); a->row_owner = reinterpret_cast<int2 *>(owner);
+    a->plan = reinterpret_cast<int *>(plan); a->rows = reinterpret_cast<CaRow *>(rows);
     a->rec_ml[0] = reinterpret_cast<float2 *>(rec_ml0); a->rec_ml[1] = reinterpret_cast<float2 *>(rec_ml1);
     a->full_ml = reinterpret_cast<float2 *>(full_ml);
     a->rec_o[0] = reinterpret_cast<float *>(rec_o0); a->rec_o[1] = reinterpret_cast<float *>(rec_o1);
@@ -234,6 +241,7 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   ASAP_TRY(check_cache_attention(ctx, p));
   CacheArgs a;
   const CaLayout layout = ca_layout(ctx, p, static_cast<uint8_t *>(scratch), &a);
+  if (layout.too_large) return fail(ctx, ASAP_ERR_UNSUPPORTED, "asap_cache_attention: max_q, max_len, max_prefix and the batch are too large together");
   if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0 || scratch_bytes < layout.bytes)
     return fail(ctx, ASAP_ERR_WORKSPACE, "asap_cache_attention: scratch is null, not 256-byte aligned or smaller than asap_cache_attention_scratch_bytes");
   CUtensorMap map_k[2], map_v[2];
@@ -263,16 +271,15 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   launch_pdl(f16 ? ca_stream_kernel<true> : ca_stream_kernel<false>, dim3(layout.blocks[0]), dim3(CA_THREADS), ca_smem_bytes(p->B + p->n_groups), st,
              map_k[0], map_v[0], a);
   ASAP_TRY(after_launch(ctx, "cache_stream"));
-  const long long entries = (long long)p->n_q * p->H;
   mark(ctx, "cache_join", st);
-  launch_pdl(f16 ? ca_join_kernel<true> : ca_join_kernel<false>, dim3((unsigned)((entries + CA_JOIN_THREADS / 32 - 1) / (CA_JOIN_THREADS / 32))),
-             dim3(CA_JOIN_THREADS), 0, st, a);
+  launch_pdl(f16 ? ca_join_kernel<true> : ca_join_kernel<false>, dim3(p->n_q, (p->H + CA_JOIN_HEADS - 1) / CA_JOIN_HEADS), dim3(CA_JOIN_THREADS), 0, st, a);
   ASAP_TRY(after_launch(ctx, "cache_join"));
-  if (p->weights && (p->max_len > 0 || (p->n_groups && p->max_prefix > 0))) {
-    const long long pre = (p->max_prefix + 31) / 32, own = (p->max_len + 31) / 32, blocks = pre * p->n_groups + own * p->B;
+  if (p->weights) {
+    const long long pre = (p->max_prefix + CA_WEIGHT_KEYS - 1) / CA_WEIGHT_KEYS, own = (p->max_len + CA_WEIGHT_KEYS - 1) / CA_WEIGHT_KEYS;
+    const long long blocks = pre * p->n_groups + own * p->B;
     if (blocks > 0) {
       mark(ctx, "cache_weight", st);
-      launch_pdl(ca_weight_kernel, dim3((unsigned)blocks), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)pre, (int)(own > 0 ? own : 1));
+      launch_pdl(ca_weight_kernel, dim3((unsigned)blocks), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)(pre > 0 ? pre : 1), (int)(own > 0 ? own : 1));
       ASAP_TRY(after_launch(ctx, "cache_weight"));
     }
   }

@@ -164,20 +164,37 @@ rope_kernel(const __grid_constant__ RopeArgs a) {
 // the two kernels numbers its key tiles through (all row tiles, heads and segments) and gives every block an equal range of numbers:
 // lengths may be as ragged as they like, and the host needs to know none of them.  A row tile whose key tiles lie in one block is
 // complete there; otherwise each block leaves a partial result (maximum, sum, weighted values) and the join adds them up in order.
+// Every row tile counts EXTRA numbers more than it has key tiles, for its queries and its result: blocks of many short row tiles
+// and blocks of few long ones are then done at the same time.
 struct StreamWork {
-  static constexpr int ROWS = 16, KEYS = 64, INDEX = 0;
+  static constexpr int ROWS = 16, KEYS = 64, EXTRA = 2, INDEX = 0;
 };
 struct TileWork {
-  static constexpr int ROWS = 256, KEYS = 128, INDEX = 1;
+  static constexpr int ROWS = 256, KEYS = 128, EXTRA = 3, INDEX = 1;
 };
 constexpr int CA_CONSUMERS = 4;                           // warps; each takes 16 keys of a tile
 constexpr int CA_THREADS = 32 * (CA_CONSUMERS + 1);       // and the copying warp
 constexpr int CA_STAGES = 3;
 constexpr int CA_BLOCK_BYTES = StreamWork::KEYS * 128;    // 64 keys x 64 columns
 constexpr int CA_STAGE_BYTES = 4 * CA_BLOCK_BYTES;        // K and V
-constexpr int CA_JOIN_BYTES = 4 * 4 * 128 * 4;            // the warps' sums of an item, a piece at a time
+constexpr int CA_JOIN_BYTES = 4 * 4 * 64 * 4;             // the warps' sums of an item, a piece at a time
+constexpr int CA_JOBS = 2;                                // items announced ahead
+constexpr int CA_Q_PITCH = 272;                           // a query row of 256 bytes; eight rows side by side meet all banks
+constexpr int CA_Q_BYTES = StreamWork::ROWS * CA_Q_PITCH;
 constexpr int CA_MAX_SEGMENTS = 1024;
 constexpr long long CA_WAIT_LIMIT = 2000000000LL;
+
+// What the join has to know of a query row: its place in the prefix's and in its own segment.
+struct CaRowPart {
+  int i0, R;               // stacked row of its first head, stacked rows of the segment (0: no keys there)
+  int adm0, causal, keys;
+  int off, per_head;       // numbers of the segment and of one of its heads
+};
+struct CaRow {
+  CaRowPart part[2];
+  int valid, pad;
+};
+static_assert(sizeof(CaRow) == 64, "a row's entry is four 16-byte loads");
 
 struct CacheArgs {
   int B, G, H, kv, rep;                    // rep = H / kv
@@ -190,9 +207,10 @@ struct CacheArgs {
   float *lse, *weights;
   float scale_log2;                        // scale * log2(e)
   // scratch
-  long long *plan;                         // [2][n_seg + 1] first tile number of every segment, streamed and tiled; the last entry: all tiles
+  int *plan;                               // [2][n_seg + 1] first number of every segment, streamed and tiled; the last entry: all of them.  Behind
+                                           // them 0 if the call is skipped
   int blocks[2];                           // of the two kernels
-  int2 *row_owner;                         // [n_q] (sequence, group or -1) of a query row
+  CaRow *rows;                             // [n_q]
   float2 *rec_ml[2], *full_ml;             // partial results: two per block and row of a row tile; [2][n_q * H] (prefix, own) complete ones
   float *rec_o[2], *full_o;                // 128 values each
   float *lse2;                             // [n_q * H] log2 of a row's sum of 2^x; +inf: the row adds no weight
@@ -234,6 +252,12 @@ __device__ __forceinline__ CaSeg ca_segment(const CacheArgs &a, int s) {
   if (!g.valid) g.nq = g.keys = 0;
   return g;
 }
+// The offsets of a sequence's query rows, or of a group's sequences, do not ascend within their bounds.  Segments of other sequences may
+// then overlap this one's: the whole call is skipped.
+__device__ __forceinline__ bool ca_broken(const CacheArgs &a, int s) {
+  const int x0 = s < a.G ? ld_prev(a.group_cu + s) : ca_qcu(a, s - a.G), x1 = s < a.G ? ld_prev(a.group_cu + s + 1) : ca_qcu(a, s - a.G + 1);
+  return x0 < 0 || x1 < x0 || x1 > (s < a.G ? a.B : a.n_q);
+}
 // group of a sequence: -1 none, -2 one that failed validation
 __device__ __forceinline__ int ca_group(const CacheArgs &a, int b) {
   int lo = 0, hi = a.G;                    // the last g with group_cu[g] <= b
@@ -246,45 +270,52 @@ __device__ __forceinline__ int ca_group(const CacheArgs &a, int b) {
   if (b >= ld_prev(a.group_cu + lo + 1)) return -1;
   return ca_segment(a, lo).valid ? lo : -2;
 }
-// keys that stacked row i of the segment admits
-__device__ __forceinline__ int ca_admitted(const CacheArgs &a, const CaSeg &g, int i) {
-  if (!g.causal) return g.keys;
-  const int n = g.keys - g.nq + 1 + i / a.rep;
-  return max(0, min(g.keys, n));
-}
-__device__ __forceinline__ bool ca_streamed(const CacheArgs &a, const CaSeg &g) { return g.nq * a.rep <= StreamWork::ROWS; }
-template <typename WORK>
-__device__ __forceinline__ int ca_row_tiles(const CacheArgs &a, const CaSeg &g) {
-  return ca_streamed(a, g) == (WORK::INDEX == 0) ? (g.nq * a.rep + WORK::ROWS - 1) / WORK::ROWS : 0;
-}
+// Stacked row i admits the first adm0 + i / rep own keys (causal), or all of them.
+__device__ __forceinline__ int ca_admitted(int keys, int adm0, int causal, int t) { return causal ? max(0, min(keys, adm0 + t)) : keys; }
+__device__ __forceinline__ bool ca_streamed(int R) { return R <= StreamWork::ROWS; }
 // key tiles of row tile rt
 template <typename WORK>
-__device__ __forceinline__ int ca_key_tiles(const CacheArgs &a, const CaSeg &g, int rt) {
-  const int last = min((rt + 1) * WORK::ROWS, g.nq * a.rep) - 1;
-  return (ca_admitted(a, g, last) + WORK::KEYS - 1) / WORK::KEYS;
+__device__ __forceinline__ int ca_key_tiles(int R, int keys, int adm0, int causal, int rep, int rt) {
+  const int last = min((rt + 1) * WORK::ROWS, R) - 1;
+  return (ca_admitted(keys, adm0, causal, causal ? last / rep : 0) + WORK::KEYS - 1) / WORK::KEYS;
 }
-// key tiles of the first `n` row tiles
+// numbers of the first `n` row tiles of a head
 template <typename WORK>
-__device__ __forceinline__ long long ca_tiles_before(const CacheArgs &a, const CaSeg &g, int n) {
-  if (!g.causal) return (long long)n * ((g.keys + WORK::KEYS - 1) / WORK::KEYS);
-  long long t = 0;
-  for (int rt = 0; rt < n; ++rt) t += ca_key_tiles<WORK>(a, g, rt);
+__device__ __forceinline__ int ca_numbers(int R, int keys, int adm0, int causal, int rep, int n) {
+  if (!causal) return keys > 0 ? n * ((keys + WORK::KEYS - 1) / WORK::KEYS + WORK::EXTRA) : 0;
+  int t = 0;
+  for (int rt = 0; rt < n; ++rt) {
+    const int kt = ca_key_tiles<WORK>(R, keys, adm0, causal, rep, rt);
+    t += kt > 0 ? kt + WORK::EXTRA : 0;
+  }
   return t;
 }
+template <typename WORK>
+__device__ __forceinline__ int ca_row_tiles(int R) {
+  return ca_streamed(R) == (WORK::INDEX == 0) ? (R + WORK::ROWS - 1) / WORK::ROWS : 0;
+}
 
-// The work of a block, item by item (an item: a range of key tiles of one row tile).  All roles of a block walk alike.
-struct CaItem {
-  CaSeg g;
-  int seg, head, rt;
-  int kt0, kt1, kt_all;    // key tiles of this block, and of the row tile
+// An item of a block's work: a range of key tiles of one row tile.
+struct __align__(16) CaJob {
+  int q0, R, row0, keys;
+  int adm0, causal, head, rt;
+  int kt0, n;              // key tiles; n < 0: the block's work is done
+  int complete, record;    // the row tile has no other items; where the result goes otherwise
+  int n_act[2];            // (tile kernel) key tiles that the two row tiles of the pair look at
+  int pad[2];
 };
+__device__ __forceinline__ int ca_admitted(const CaJob &j, int t) { return ca_admitted(j.keys, j.adm0, j.causal, t); }
+
+// Walks the numbers [t, end) of a block.
 template <typename WORK>
 struct CaWalk {
-  long long t, end;        // tile numbers left
-  int seg, head, rt, kt;
+  int t, end, begin_t;
+  int seg, head, rt, pos;  // pos: numbers of the row tile that lie before t
+  int R;
   CaSeg g;
-  __device__ __forceinline__ void begin(const CacheArgs &a, const long long *off, int n_seg, long long t0, long long t1) {
-    t = t0; end = t1;
+  __device__ __forceinline__ int key_tiles(const CacheArgs &a) const { return ca_key_tiles<WORK>(R, g.keys, g.keys - g.nq + 1, g.causal, a.rep, rt); }
+  __device__ __forceinline__ void begin(const CacheArgs &a, const int *off, int n_seg, int t0, int t1) {
+    t = begin_t = t0; end = t1;
     if (t >= end) return;
     int lo = 0, hi = n_seg;                // off[lo] <= t < off[hi]
     while (hi - lo > 1) {
@@ -294,94 +325,84 @@ struct CaWalk {
     }
     seg = lo;
     g = ca_segment(a, seg);
-    const long long per_head = (off[seg + 1] - off[seg]) / a.kv;
-    long long u = t - off[seg];
-    head = (int)(u / per_head);
+    R = g.nq * a.rep;
+    const int per_head = (off[seg + 1] - off[seg]) / a.kv;
+    int u = t - off[seg];
+    head = u / per_head;
     u -= head * per_head;
-    rt = 0;
-    if (!g.causal) {
-      const int n = ca_key_tiles<WORK>(a, g, 0);
-      rt = (int)(u / n);
-      kt = (int)(u - (long long)rt * n);
-    } else {
-      int n;
-      while (u >= (n = ca_key_tiles<WORK>(a, g, rt))) { u -= n; ++rt; }
-      kt = (int)u;
+    for (rt = 0;; ++rt) {
+      const int kt = key_tiles(a), n = kt > 0 ? kt + WORK::EXTRA : 0;
+      if (u < n) break;
+      u -= n;
     }
+    pos = u;
   }
-  __device__ __forceinline__ bool next(const CacheArgs &a, const long long *off, CaItem &it) {
-    if (t >= end) return false;
-    it.g = g; it.seg = seg; it.head = head; it.rt = rt;
-    it.kt_all = ca_key_tiles<WORK>(a, g, rt);
-    it.kt0 = kt;
-    it.kt1 = (int)min((long long)it.kt_all, kt + (end - t));
-    t += it.kt1 - it.kt0;
-    if (t < end) {                         // the next row tile that has keys
-      kt = 0;
-      do {
-        if (++rt >= ca_row_tiles<WORK>(a, g)) {
-          rt = 0;
-          if (++head >= a.kv) {
-            head = 0;
-            do ++seg; while (off[seg + 1] <= t);
-            g = ca_segment(a, seg);
+  // the next item that has key tiles; false: none is left
+  __device__ __forceinline__ bool next(const CacheArgs &a, const int *off, CaJob &j) {
+    while (t < end) {
+      const int kt = key_tiles(a), p1 = min(kt + WORK::EXTRA, pos + (end - t));
+      const int k0 = max(0, pos - WORK::EXTRA), k1 = p1 - WORK::EXTRA, first = t - pos + WORK::EXTRA;
+      j.q0 = g.q0; j.R = R; j.row0 = g.row0; j.keys = g.keys; j.adm0 = g.keys - g.nq + 1; j.causal = g.causal; j.head = head; j.rt = rt;
+      j.kt0 = k0; j.n = k1 - k0; j.complete = k0 == 0 && k1 == kt; j.record = 2 * blockIdx.x + (first <= begin_t ? 0 : 1);
+      t += p1 - pos;
+      if (t < end) {                       // the next row tile that has keys
+        pos = 0;
+        do {
+          if (++rt >= ca_row_tiles<WORK>(R)) {
+            rt = 0;
+            if (++head >= a.kv) {
+              head = 0;
+              do ++seg; while (off[seg + 1] <= t);
+              g = ca_segment(a, seg);
+              R = g.nq * a.rep;
+            }
           }
-        }
-      } while (ca_key_tiles<WORK>(a, g, rt) == 0);
+        } while (key_tiles(a) == 0);
+      }
+      if (k1 > k0) return true;
     }
-    return true;
+    return false;
   }
 };
 
-// First tile number of every segment into off[0 .. n_seg] (shared memory); all threads of the block.
+// First number of every segment into off[0 .. n_seg] (shared memory); all threads of the block.  True if the call is to be skipped.
 template <typename WORK, int THREADS>
-__device__ __forceinline__ void ca_plan(const CacheArgs &a, long long *off, int n_seg, long long *warp_part) {
+__device__ __forceinline__ bool ca_plan(const CacheArgs &a, int *off, int n_seg, int *warp_part) {
   const int per = (n_seg + THREADS - 1) / THREADS, s0 = min(n_seg, (int)threadIdx.x * per), s1 = min(n_seg, s0 + per);
-  long long mine = 0;
+  int mine = 0;
+  bool broken = (*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) != 0;
   for (int s = s0; s < s1; ++s) {
+    broken = broken || ca_broken(a, s);
     const CaSeg g = ca_segment(a, s);
-    const long long n = a.kv * ca_tiles_before<WORK>(a, g, ca_row_tiles<WORK>(a, g));
+    const int R = g.nq * a.rep, n = a.kv * ca_numbers<WORK>(R, g.keys, g.keys - g.nq + 1, g.causal, a.rep, ca_row_tiles<WORK>(R));
     off[s + 1] = n;
     mine += n;
     if (WORK::INDEX == 0 && !g.valid && blockIdx.x == 0) atomicOr(a.status, (uint32_t)STATUS_BAD_SAMPLE);
   }
-  long long scan = mine;
+  int scan = mine;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, scan, o);
+    const int v = __shfl_up_sync(0xffffffffu, scan, o);
     if (lane >= o) scan += v;
   }
   if (lane == 31) warp_part[warp] = scan;
-  __syncthreads();
-  long long base = scan - mine;
+  broken = __syncthreads_or(broken);
+  int base = scan - mine;
   for (int w = 0; w < warp; ++w) base += warp_part[w];
   for (int s = s0; s < s1; ++s) {
-    const long long n = off[s + 1];
-    base += n;
+    base += off[s + 1];
     off[s + 1] = base;                     // (its own entries only)
   }
   if (threadIdx.x == 0) off[0] = 0;
   __syncthreads();
-  if (blockIdx.x == 0)
+  if (blockIdx.x == 0) {
     for (int s = threadIdx.x; s <= n_seg; s += THREADS) a.plan[WORK::INDEX * (n_seg + 1) + s] = off[s];
+    if (WORK::INDEX == 0 && threadIdx.x == 0) a.plan[2 * (n_seg + 1)] = broken ? 0 : 1;
+  }
+  return broken;
 }
-
-__device__ __forceinline__ long long ca_chunk(long long all, int blocks) { return max(1LL, (all + blocks - 1) / blocks); }
-
-// Where the partial result of row tile (seg, head, rt) that block c leaves lies: record 2c if the row tile holds the block's first
-// tile, else 2c + 1 (it then runs past the block's last one).
-struct CaPlace {
-  long long first, last;   // tile numbers of the row tile
-  int c0, c1;              // blocks
-};
-__device__ __forceinline__ CaPlace ca_place(long long first, int n, long long chunk) {
-  CaPlace p;
-  p.first = first; p.last = first + n - 1;
-  p.c0 = (int)(p.first / chunk);
-  p.c1 = (int)(p.last / chunk);
-  return p;
-}
+__device__ __forceinline__ int ca_chunk(int all, int blocks) { return max(1, (all + blocks - 1) / blocks); }
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -408,9 +429,11 @@ __device__ __forceinline__ void tma_load_3d_w(uint32_t smem_dst, const void *tma
       ::"r"(smem_dst), "l"(tmap), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(leader)
       : "memory");
 }
-__device__ __forceinline__ bool not_finite16(uint32_t w, bool f16) {        // either half is an infinity or NaN
-  const uint32_t e = f16 ? 0x7c00u : 0x7f80u;
-  return (w & e) == e || ((w >> 16) & e) == e;
+// Non-zero if either half is an infinity or NaN: an exponent of all ones, plus one, carries into the sign's place.
+template <bool F16>
+__device__ __forceinline__ uint32_t not_finite_bits(uint32_t w) {
+  constexpr uint32_t exponent = F16 ? 0x7c007c00u : 0x7f807f80u, one = F16 ? 0x04000400u : 0x00800080u;
+  return ((w & exponent) + one) & 0x80008000u;
 }
 
 // One arrival for the (converged) warp, which is converged afterwards too: lanes that went on to spin on another barrier while lane 0
@@ -421,11 +444,47 @@ __device__ __forceinline__ void mbar_arrive_lane0(uint32_t bar, int lane) {
 }
 
 struct CaBook {
-  uint64_t full[CA_STAGES], empty[CA_STAGES];
-  long long warp_part[8];
+  uint64_t full[CA_STAGES], empty[CA_STAGES], job_full[CA_JOBS], job_empty[CA_JOBS];
+  int warp_part[8];
   int abort_flag;
   float2 ml[CA_CONSUMERS][StreamWork::ROWS];
+  CaJob job[CA_JOBS];
 };
+
+// The entries of the query rows, for the join: a block takes every gridDim.x-th sequence.
+__device__ __forceinline__ void ca_describe_rows(const CacheArgs &a, const int *off, int n_seg, int thread, int threads) {
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    const CaSeg own = ca_segment(a, a.G + b);
+    const int grp = ca_group(a, b), q0 = ca_qcu(a, b), nq = ca_qcu(a, b + 1) - q0;
+    CaRow row;
+    row.valid = own.valid && grp >= -1;
+    row.pad = 0;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const int s = p == 0 ? grp : a.G + b;
+      CaRowPart &part = row.part[p];
+      part.R = 0;
+      part.i0 = part.adm0 = part.causal = part.keys = part.off = part.per_head = 0;
+      if (s < 0 || !row.valid) continue;
+      const CaSeg g = p == 0 ? ca_segment(a, s) : own;
+      const int R = g.nq * a.rep;
+      if (g.keys == 0) continue;
+      int o0 = off[s], o1 = off[s + 1];
+      if (!ca_streamed(R)) {
+        o0 = ld_prev(a.plan + n_seg + 1 + s);
+        o1 = ld_prev(a.plan + n_seg + 2 + s);
+      }
+      part.R = R; part.i0 = (own.q0 - g.q0) * a.rep; part.keys = g.keys; part.adm0 = g.keys - g.nq + 1; part.causal = g.causal;
+      part.off = o0; part.per_head = (o1 - o0) / a.kv;
+    }
+    for (int r = thread; r < nq; r += threads) {
+      CaRow mine = row;
+      mine.part[0].i0 += r * a.rep;
+      mine.part[1].i0 += r * a.rep;
+      a.rows[q0 + r] = mine;
+    }
+  }
+}
 
 template <bool F16>
 __global__ void __launch_bounds__(CA_THREADS, 2)
@@ -433,14 +492,18 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   extern __shared__ __align__(1024) uint8_t ca_smem[];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   float *join = reinterpret_cast<float *>(ca_smem + CA_STAGES * CA_STAGE_BYTES);
-  CaBook *bk = reinterpret_cast<CaBook *>(ca_smem + CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES);
-  long long *off = reinterpret_cast<long long *>(bk + 1);
-  const uint32_t base = smem_u32(ca_smem);
+  const uint32_t base = smem_u32(ca_smem), q_smem = base + CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES;
+  CaBook *bk = reinterpret_cast<CaBook *>(ca_smem + CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES + CA_JOBS * CA_Q_BYTES);
+  int *off = reinterpret_cast<int *>(bk + 1);
   const int n_seg = a.G + a.B;
   if (threadIdx.x == 0) {
     for (int s = 0; s < CA_STAGES; ++s) {
       mbar_init(smem_u32(&bk->full[s]), 1);
       mbar_init(smem_u32(&bk->empty[s]), CA_CONSUMERS);
+    }
+    for (int s = 0; s < CA_JOBS; ++s) {
+      mbar_init(smem_u32(&bk->job_full[s]), 1);
+      mbar_init(smem_u32(&bk->job_empty[s]), CA_CONSUMERS);
     }
     bk->abort_flag = 0;
     fence_barrier_init();
@@ -450,43 +513,57 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   __syncthreads();
   WaitCtx wc{&bk->abort_flag, a.status, STATUS_CACHE_TIMEOUT, a.wait_limit};
   pdl_enter();
-  const bool stop = __syncthreads_or((*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) != 0);
-  ca_plan<StreamWork, CA_THREADS>(a, off, n_seg, bk->warp_part);
-  const long long all = off[n_seg], chunk = ca_chunk(all, gridDim.x);
-  // the query rows' owners, for the join
-  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-    const CaSeg g = ca_segment(a, a.G + b);
-    const int grp = ca_group(a, b);
-    if (!g.valid) continue;
-    for (int r = threadIdx.x; r < g.nq; r += CA_THREADS) a.row_owner[g.q0 + r] = make_int2(b, grp);
-  }
-  CaWalk<StreamWork> walk;
-  CaItem it;
-  walk.begin(a, off, n_seg, min(all, blockIdx.x * chunk), min(all, (blockIdx.x + 1) * chunk));
-  if (stop) walk.end = walk.t;
+  const bool stop = ca_plan<StreamWork, CA_THREADS>(a, off, n_seg, bk->warp_part);
 
   if (warp == CA_CONSUMERS) {
-    // ------------------------------------------------------------------ copies
+    // ------------------------------------------------------------------ items, query rows, key and value tiles
+    // (the whole warp walks the loop and stays converged)
+    const int all = off[n_seg], chunk = ca_chunk(all, gridDim.x);
+    CaWalk<StreamWork> walk;
+    walk.begin(a, off, n_seg, stop ? 0 : min(all, (int)blockIdx.x * chunk), stop ? 0 : min(all, ((int)blockIdx.x + 1) * chunk));
     const uint32_t leader = warp_leader();
     RingPos pos;
     int issued = 0, used = 0;
-    while (walk.next(a, off, it)) {
-      for (int kt = it.kt0; kt < it.kt1; ++kt, ++used) {
+    CaJob j;
+    for (int jc = 0;; ++jc) {
+      const int slot = jc % CA_JOBS;
+      const bool more = walk.next(a, off, j);
+      if (!more) j.n = -1;
+      // The queue of items keeps working after an abort (its waits ignore the flag and are bounded on their own): all consumers must
+      // see the same sequence, ending with -1.
+      if (jc >= CA_JOBS) mbar_wait_drain(smem_u32(&bk->job_empty[slot]), ((jc / CA_JOBS) - 1) & 1, CA_WAIT_LIMIT);
+      __syncwarp();
+      const bool going = more && !__shfl_sync(0xffffffffu, bk->abort_flag, 0);
+      const uint32_t jbar = smem_u32(&bk->job_full[slot]);
+      if (lane == 0) {
+        bk->job[slot] = j;
+        if (going) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(jbar), "r"(j.R * 256) : "memory");
+        else mbar_arrive(jbar);
+      }
+      __syncwarp();
+      if (!more) break;
+      if (going && lane < j.R) {
+        const uint16_t *src = a.q + (long long)(j.q0 + lane / a.rep) * a.q_row + (long long)(j.head * a.rep + lane % a.rep) * a.q_head;
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];"
+                     ::"r"(q_smem + slot * CA_Q_BYTES + lane * CA_Q_PITCH), "l"(src), "r"(jbar) : "memory");
+      }
+      __syncwarp();
+      for (int kt = j.kt0; kt < j.kt0 + j.n; ++kt, ++used) {
         if (used >= CA_STAGES) mbar_wait_warp(smem_u32(&bk->empty[pos.slot]), pos.phase ^ 1u, wc);
         if (!__shfl_sync(0xffffffffu, bk->abort_flag, 0)) {
           const uint32_t bar = smem_u32(&bk->full[pos.slot]), dst = base + pos.slot * CA_STAGE_BYTES;
-          const int row = it.g.row0 + kt * StreamWork::KEYS;
+          const int row = j.row0 + kt * StreamWork::KEYS;
           mbar_expect_tx_w(bar, CA_STAGE_BYTES, leader);
-          tma_load_3d_w(dst, &tmap_k, bar, 0, it.head, row, leader);
-          tma_load_3d_w(dst + CA_BLOCK_BYTES, &tmap_k, bar, 64, it.head, row, leader);
-          tma_load_3d_w(dst + 2 * CA_BLOCK_BYTES, &tmap_v, bar, 0, it.head, row, leader);
-          tma_load_3d_w(dst + 3 * CA_BLOCK_BYTES, &tmap_v, bar, 64, it.head, row, leader);
+          tma_load_3d_w(dst, &tmap_k, bar, 0, j.head, row, leader);
+          tma_load_3d_w(dst + CA_BLOCK_BYTES, &tmap_k, bar, 64, j.head, row, leader);
+          tma_load_3d_w(dst + 2 * CA_BLOCK_BYTES, &tmap_v, bar, 0, j.head, row, leader);
+          tma_load_3d_w(dst + 3 * CA_BLOCK_BYTES, &tmap_v, bar, 64, j.head, row, leader);
           issued = used + 1;
         }
         pos.step(CA_STAGES);
       }
     }
-    // every copy issued has landed before the block leaves
+    // every copy issued has landed before the block leaves (the consumers wait for the query rows whatever happens)
     for (int s = 0; s < CA_STAGES; ++s) {
       const int fills = issued > s ? (issued - s + CA_STAGES - 1) / CA_STAGES : 0;
       if (fills > 0) mbar_wait_drain(smem_u32(&bk->full[s]), (fills - 1) & 1, CA_WAIT_LIMIT);
@@ -495,41 +572,40 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     return;
   }
   // -------------------------------------------------------------------- consumers
+  if (!stop) ca_describe_rows(a, off, n_seg, threadIdx.x, 32 * CA_CONSUMERS);
   const int gq = lane >> 2, tq = lane & 3;       // fragment row / column pair
+  const int mi = lane >> 3, mr = lane & 7;       // matrix of an ldmatrix, row in it
   RingPos pos;
-  while (walk.next(a, off, it)) {
-    const int R = it.g.nq * a.rep;
-    int adm[2];                                  // admitted keys of fragment rows gq, gq + 8
-    long long entry[2];                          // (query row, head)
+  for (int jc = 0;; ++jc) {
+    const int slot = jc % CA_JOBS;
+    const bool got = mbar_wait_drain(smem_u32(&bk->job_full[slot]), (jc / CA_JOBS) & 1, CA_WAIT_LIMIT);
+    __syncwarp();
+    const CaJob j = bk->job[slot];
     uint32_t qa[8][4];
 #pragma unroll
+    for (int kk = 0; kk < 8; ++kk) ldsm4(q_smem + slot * CA_Q_BYTES + ((mi & 1) * 8 + mr) * CA_Q_PITCH + (kk * 2 + (mi >> 1)) * 16, qa[kk]);
+    __syncwarp();
+    mbar_arrive_lane0(smem_u32(&bk->job_empty[slot]), lane);
+    if (!got || j.n < 0) break;
+    int adm[2];                                  // admitted keys of fragment rows gq, gq + 8 (rows past the last: none, whatever the buffer held)
+    long long entry[2];                          // (query row, head)
+#pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int i = it.rt * StreamWork::ROWS + gq + 8 * e;
-      const bool in = i < R;
-      const int qr = it.g.q0 + i / a.rep, h = it.head * a.rep + i % a.rep;
-      adm[e] = in ? ca_admitted(a, it.g, i) : 0;
-      entry[e] = in ? (long long)qr * a.H + h : -1;
-      const uint16_t *qp = a.q + (long long)qr * a.q_row + (long long)h * a.q_head + 2 * tq;
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          uint32_t w = 0u;
-          if (in) asm volatile("ld.global.u32 %0, [%1];" : "=r"(w) : "l"(qp + kk * 16 + s * 8));
-          qa[kk][e + 2 * s] = w;
-        }
+      const int i = gq + 8 * e, t = i / a.rep;
+      adm[e] = i < j.R ? ca_admitted(j, t) : 0;
+      entry[e] = i < j.R ? (long long)(j.q0 + t) * a.H + j.head * a.rep + (i - t * a.rep) : -1;
     }
+    const bool upper = j.R > 8;                  // rows 8 .. 15 are in use
     float o[16][4];
 #pragma unroll
     for (int n = 0; n < 16; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    for (int kt = it.kt0; kt < it.kt1; ++kt) {
+    for (int kt = j.kt0; kt < j.kt0 + j.n; ++kt) {
       mbar_wait_warp(smem_u32(&bk->full[pos.slot]), pos.phase, wc);
       const uint32_t ks = base + pos.slot * CA_STAGE_BYTES, vs = ks + 2 * CA_BLOCK_BYTES;
-      const int j0 = kt * StreamWork::KEYS + warp * 16;   // this warp's first key
-      const int mi = lane >> 3, mr = lane & 7;
+      const int j0 = kt * StreamWork::KEYS + warp * 16;      // this warp's first key
       // ---- logits of 16 rows x 16 keys
       float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
       {
@@ -547,33 +623,34 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int j = j0 + n * 8 + 2 * tq + (e & 1);
-          x[n][e] = j < adm[e >> 1] ? x[n][e] * a.scale_log2 : -INFINITY;
+          const int key = j0 + n * 8 + 2 * tq + (e & 1);
+          x[n][e] = key < adm[e >> 1] ? x[n][e] * a.scale_log2 : -INFINITY;
         }
       if (a.logits) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           if (entry[e] < 0) continue;
-          float *row = a.logits + entry[e] * a.pitch + (it.g.causal ? a.own_off : 0);
+          float *row = a.logits + entry[e] * a.pitch + (j.causal ? a.own_off : 0);
 #pragma unroll
           for (int n = 0; n < 2; ++n)
             *reinterpret_cast<float2 *>(row + j0 + n * 8 + 2 * tq) = make_float2(x[n][2 * e], x[n][2 * e + 1]);
         }
       }
       // ---- probabilities relative to the running maximum
-      uint32_t pa[4];
+      uint32_t pa[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
+        if (e == 1 && !upper) continue;
         float mx = fmaxf(fmaxf(x[0][2 * e], x[0][2 * e + 1]), fmaxf(x[1][2 * e], x[1][2 * e + 1]));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         const float m_new = fmaxf(m[e], mx), ref = m_new == -INFINITY ? 0.f : m_new;
-        const float f = fast_exp2(m[e] - ref);
-        m[e] = m_new;
-        l[e] *= f;
-        if (__any_sync(0xffffffffu, f != 1.f)) {
+        if (__any_sync(0xffffffffu, m_new != m[e])) {
+          const float f = m_new == m[e] ? 1.f : fast_exp2(m[e] - ref);
+          l[e] *= f;
 #pragma unroll
           for (int n = 0; n < 16; ++n) { o[n][2 * e] *= f; o[n][2 * e + 1] *= f; }
+          m[e] = m_new;
         }
         float p[2][2];
 #pragma unroll
@@ -586,43 +663,42 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       }
       // ---- values.  Rows that no query row of the tile admits are cleared (0 * NaN is NaN).  A row that only some of them
       // admit may hold infinities or NaN too: then its part is added without the matrix instruction, to the rows that admit it.
-      const int vcol = (mi & 1) * 8 + mr;
-      uint32_t bad = 0u;                         // keys of this warp's 16 to be added apart
-      if (j0 + 16 > (it.g.causal ? it.g.keys - it.g.nq + 1 : it.g.keys)) {
+      if (j0 + 16 > (j.causal ? j.adm0 : j.keys)) {
         const int r = lane >> 1, half = lane & 1;           // two lanes per key
-        const bool dead = j0 + r >= it.g.keys;
+        const bool dead = j0 + r >= j.keys;
         uint8_t *vrow = ca_smem + pos.slot * CA_STAGE_BYTES + (2 + half) * CA_BLOCK_BYTES + (warp * 16 + r) * 128;
-        bool nf = false;
+        uint32_t hit = 0u;
         if (!dead)
           for (int c = 0; c < 8; ++c) {
             const uint4 v = reinterpret_cast<const uint4 *>(vrow)[c];
-            nf = nf || not_finite16(v.x, F16) || not_finite16(v.y, F16) || not_finite16(v.z, F16) || not_finite16(v.w, F16);
+            hit |= not_finite_bits<F16>(v.x) | not_finite_bits<F16>(v.y) | not_finite_bits<F16>(v.z) | not_finite_bits<F16>(v.w);
           }
-        const uint32_t who = __ballot_sync(0xffffffffu, nf);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) bad |= ((who >> (2 * e)) & 3u) ? 1u << e : 0u;
+        const uint32_t who = __ballot_sync(0xffffffffu, hit != 0u);
         if (dead)
           for (int c = 0; c < 8; ++c) reinterpret_cast<uint4 *>(vrow)[c] = make_uint4(0u, 0u, 0u, 0u);
         __syncwarp();
-        for (uint32_t left = bad; left; left &= left - 1) {
-          const int r2 = __ffs(left) - 1;        // key
-          const int src = (lane & ~3) | ((r2 & 7) >> 1);
-          const uint32_t w0 = __shfl_sync(0xffffffffu, (r2 & 8) ? pa[2] : pa[0], src), w1 = __shfl_sync(0xffffffffu, (r2 & 8) ? pa[3] : pa[1], src);
-          const float2 u0 = unpack2_t<F16>(w0), u1 = unpack2_t<F16>(w1);
-          const float p0 = (r2 & 1) ? u0.y : u0.x, p1 = (r2 & 1) ? u1.y : u1.x;
-          const bool in0 = j0 + r2 < adm[0], in1 = j0 + r2 < adm[1];
+        if (who) {
+          uint32_t bad = 0u;                     // keys of this warp's 16 to be added apart
 #pragma unroll
-          for (int n = 0; n < 16; ++n) {
-            const int key = warp * 16 + r2;
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(ca_smem + pos.slot * CA_STAGE_BYTES + (2 + (n >> 3)) * CA_BLOCK_BYTES +
-                                                                   key * 128 + (((n & 7) ^ (key & 7)) << 4) + tq * 4);
-            const float2 v = unpack2_t<F16>(w);
-            if (in0) { o[n][0] += p0 * v.x; o[n][1] += p0 * v.y; }
-            if (in1) { o[n][2] += p1 * v.x; o[n][3] += p1 * v.y; }
+          for (int e = 0; e < 16; ++e) bad |= ((who >> (2 * e)) & 3u) ? 1u << e : 0u;
+          for (uint32_t left = bad; left; left &= left - 1) {
+            const int r2 = __ffs(left) - 1;      // key
+            const int src = (lane & ~3) | ((r2 & 7) >> 1);
+            const uint32_t w0 = __shfl_sync(0xffffffffu, (r2 & 8) ? pa[2] : pa[0], src), w1 = __shfl_sync(0xffffffffu, (r2 & 8) ? pa[3] : pa[1], src);
+            const float2 u0 = unpack2_t<F16>(w0), u1 = unpack2_t<F16>(w1);
+            const float p0 = (r2 & 1) ? u0.y : u0.x, p1 = (r2 & 1) ? u1.y : u1.x;
+            const bool in0 = j0 + r2 < adm[0], in1 = j0 + r2 < adm[1];
+#pragma unroll
+            for (int n = 0; n < 16; ++n) {
+              const int key = warp * 16 + r2;
+              const uint32_t w = *reinterpret_cast<const uint32_t *>(ca_smem + pos.slot * CA_STAGE_BYTES + (2 + (n >> 3)) * CA_BLOCK_BYTES +
+                                                                     key * 128 + (((n & 7) ^ (key & 7)) << 4) + tq * 4);
+              const float2 v = unpack2_t<F16>(w);
+              if (in0) { o[n][0] += p0 * v.x; o[n][1] += p0 * v.y; }
+              if (in1) { o[n][2] += p1 * v.x; o[n][3] += p1 * v.y; }
+            }
           }
-        }
-        __syncwarp();
-        if (bad) {
+          __syncwarp();
           if ((bad >> r) & 1u)
             for (int c = 0; c < 8; ++c) reinterpret_cast<uint4 *>(vrow)[c] = make_uint4(0u, 0u, 0u, 0u);
           __syncwarp();
@@ -631,7 +707,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       }
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) {
-        const int c = dt * 2 + (mi >> 1), key = warp * 16 + vcol;
+        const int c = dt * 2 + (mi >> 1), key = warp * 16 + (mi & 1) * 8 + mr;
         uint32_t b[4];
         ldsm4t(vs + (c >> 3) * CA_BLOCK_BYTES + key * 128 + (((c & 7) ^ (key & 7)) << 4), b);
         mma16816<F16>(o[2 * dt], pa, b[0], b[1]);
@@ -649,18 +725,36 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       if (l[e] != l[e] && m[e] == -INFINITY) m[e] = 0.f;      // every logit was NaN: not an empty row
       if (tq == 0) bk->ml[warp][gq + 8 * e] = make_float2(m[e], l[e]);
     }
-    const int rows = min(StreamWork::ROWS, R - it.rt * StreamWork::ROWS);
-    const int pad_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : 16, width = 512 / pad_rows;    // columns a piece
+    const int pad_rows = j.R <= 4 ? 4 : j.R <= 8 ? 8 : 16, width = 256 / pad_rows;    // columns a piece
     asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
     float f[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       float top = -INFINITY;
+#pragma unroll
       for (int w = 0; w < CA_CONSUMERS; ++w) top = fmaxf(top, bk->ml[w][gq + 8 * e].x);
       f[e] = m[e] == -INFINITY ? 0.f : fast_exp2(m[e] - top);
     }
-    const long long before = off[it.seg] + it.head * ((off[it.seg + 1] - off[it.seg]) / a.kv) + ca_tiles_before<StreamWork>(a, it.g, it.rt);
-    const CaPlace pl = ca_place(before, it.kt_all, chunk);
+    // threads of a piece: a float4 each for the first 64
+    const int r = (threadIdx.x & 63) / (width / 4), c4 = (threadIdx.x & 63) % (width / 4) * 4;
+    float2 *ml = nullptr;
+    float *dst = nullptr;
+    if (r < j.R && threadIdx.x < 64 && !bk->abort_flag) {
+      const int t = r / a.rep;
+      const long long e = j.complete ? (j.causal ? (long long)a.n_q * a.H : 0) + (long long)(j.q0 + t) * a.H + j.head * a.rep + (r - t * a.rep)
+                                     : (long long)j.record * StreamWork::ROWS + r;
+      ml = (j.complete ? a.full_ml : a.rec_ml[0]) + e;
+      dst = (j.complete ? a.full_o : a.rec_o[0]) + e * 128;
+      if (c4 == 0) {
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < CA_CONSUMERS; ++w) top = fmaxf(top, bk->ml[w][r].x);
+#pragma unroll
+        for (int w = 0; w < CA_CONSUMERS; ++w)
+          if (bk->ml[w][r].x != -INFINITY) sum += bk->ml[w][r].y * fast_exp2(bk->ml[w][r].x - top);
+        *ml = make_float2(top, sum);
+      }
+    }
     for (int c0 = 0; c0 < 128; c0 += width) {
 #pragma unroll
       for (int n = 0; n < 16; ++n) {
@@ -672,33 +766,14 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
             *reinterpret_cast<float2 *>(join + (warp * pad_rows + gq + 8 * e) * width + c) = make_float2(o[n][2 * e] * f[e], o[n][2 * e + 1] * f[e]);
       }
       asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
-      const int r = threadIdx.x / (width / 4), c = threadIdx.x % (width / 4) * 4;
-      if (r < rows && !bk->abort_flag) {
+      if (dst) {
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        float top = -INFINITY, sum = 0.f;
+#pragma unroll
         for (int w = 0; w < CA_CONSUMERS; ++w) {
-          const float4 v = *reinterpret_cast<const float4 *>(join + (w * pad_rows + r) * width + c);
+          const float4 v = *reinterpret_cast<const float4 *>(join + (w * pad_rows + r) * width + c4);
           s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-          top = fmaxf(top, bk->ml[w][r].x);
         }
-        for (int w = 0; w < CA_CONSUMERS; ++w)
-          if (bk->ml[w][r].x != -INFINITY) sum += bk->ml[w][r].y * fast_exp2(bk->ml[w][r].x - top);
-        const int i = it.rt * StreamWork::ROWS + r;
-        const int qr = it.g.q0 + i / a.rep, h = it.head * a.rep + i % a.rep;
-        const long long ent = (long long)qr * a.H + h;
-        float2 *ml;
-        float *dst;
-        if (pl.c0 == pl.c1) {
-          const long long e = (it.g.causal ? (long long)a.n_q * a.H : 0) + ent;
-          ml = a.full_ml + e;
-          dst = a.full_o + e * 128;
-        } else {
-          const long long e = (long long)(2 * blockIdx.x + (pl.first <= blockIdx.x * chunk ? 0 : 1)) * StreamWork::ROWS + r;
-          ml = a.rec_ml[0] + e;
-          dst = a.rec_o[0] + e * 128;
-        }
-        *reinterpret_cast<float4 *>(dst + c0 + c) = s;
-        if (c0 + c == 0) *ml = make_float2(top, sum);
+        *reinterpret_cast<float4 *>(dst + c0 + c4) = s;
       }
       asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
     }
@@ -717,29 +792,24 @@ constexpr int CT_SLOTS = 4;                     // ring of key and value tiles i
 constexpr int CT_STAGE_BYTES = 32 * 64;         // per softmax warp: 32 rows x 16 floats
 constexpr int CT_STAGE_OFF = (2 + CT_SLOTS) * CT_TILE_BYTES;
 constexpr int CT_BOOK_OFF = CT_STAGE_OFF + 8 * CT_STAGE_BYTES;
+constexpr int CT_JOBS = 4;                      // items announced ahead
 constexpr uint32_t CT_TMEM_COLS = 512, CT_S_COL = 256, CT_P_COL = 384;   // O of both row tiles, one S that they use in turn, P of both
 // A tile's sum relative to the reference at which the reference moves: no probability may leave the element type's range.
 constexpr float CT_SUM_LIMIT_BF16 = 1.0995116e12f, CT_SUM_LIMIT_F16 = 32768.f;
 
 struct CtBook {
   uint64_t full[CT_SLOTS], empty[CT_SLOTS], raw[CT_SLOTS];
-  uint64_t q_full[2], q_empty[2], s_full[2], s_empty, p_ready[2], pv_done[2], mma_done;
-  long long warp_part[CT_THREADS / 32];
+  uint64_t q_full[2], q_empty[2], s_full[2], s_empty, p_ready[2], pv_done[2], mma_done, job_full[CT_JOBS], job_empty[CT_JOBS];
+  CaJob job[CT_JOBS];
+  int warp_part[CT_THREADS / 32];
   uint32_t tmem_base;
   int abort_flag;
   int bad[4];              // the item (modulo 4) has value rows with infinities or NaN that not all of its query rows admit
 };
 
-// The part of an item that row tile g of the pair takes: its first `n` key tiles.
-__device__ __forceinline__ int ct_active(const CacheArgs &a, const CaItem &it, int g) {
-  const int R = it.g.nq * a.rep, i0 = it.rt * TileWork::ROWS + g * 128;
-  if (i0 >= R) return 0;
-  const int n = (ca_admitted(a, it.g, min(i0 + 128, R) - 1) + 127) / 128;
-  return max(0, min(it.kt1, n) - it.kt0);
-}
-// Key tile kt holds rows that no query row of the pair admits, or not all of them do: its values pass through warp 2.
-__device__ __forceinline__ bool ct_passed(const CacheArgs &a, const CaItem &it, int kt) {
-  return (kt + 1) * 128 > ca_admitted(a, it.g, it.rt * TileWork::ROWS);
+// Key tile kt holds rows that not all query rows of the pair admit: its values pass through warp 2.
+__device__ __forceinline__ bool ct_passed(const CaJob &j, int rep, int kt) {
+  return (kt + 1) * 128 > ca_admitted(j, j.causal ? j.rt * TileWork::ROWS / rep : 0);
 }
 
 template <bool F16>
@@ -749,9 +819,13 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t base = smem_u32(ct_smem), q_smem = base, ring = base + 2 * CT_TILE_BYTES;
   CtBook *bk = reinterpret_cast<CtBook *>(ct_smem + CT_BOOK_OFF);
-  long long *off = reinterpret_cast<long long *>(bk + 1);
+  int *off = reinterpret_cast<int *>(bk + 1);
   const int n_seg = a.G + a.B;
   if (threadIdx.x == 0) {
+    for (int s = 0; s < CT_JOBS; ++s) {
+      mbar_init(smem_u32(&bk->job_full[s]), 1);
+      mbar_init(smem_u32(&bk->job_empty[s]), 11);           // the MMA issuer, warps 2 and 3, every softmax warp
+    }
     for (int s = 0; s < CT_SLOTS; ++s) {
       mbar_init(smem_u32(&bk->full[s]), 1);
       mbar_init(smem_u32(&bk->empty[s]), 1);
@@ -782,27 +856,52 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
   const uint32_t tmem_base = bk->tmem_base;
   WaitCtx wc{&bk->abort_flag, a.status, STATUS_CACHE_TIMEOUT, a.wait_limit};
   pdl_enter();
-  const bool stop = __syncthreads_or((*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) != 0);
-  ca_plan<TileWork, CT_THREADS>(a, off, n_seg, bk->warp_part);
-  const long long all = off[n_seg], chunk = ca_chunk(all, gridDim.x);
-  CaWalk<TileWork> walk;
-  CaItem it;
-  walk.begin(a, off, n_seg, min(all, blockIdx.x * chunk), min(all, (blockIdx.x + 1) * chunk));
-  if (stop) walk.end = walk.t;
+  const bool stop = ca_plan<TileWork, CT_THREADS>(a, off, n_seg, bk->warp_part);
+  // the next item; false: there is none
+  auto take = [&](int jc, CaJob &j) {
+    const int slot = jc % CT_JOBS;
+    const bool got = mbar_wait_drain(smem_u32(&bk->job_full[slot]), (jc / CT_JOBS) & 1, CA_WAIT_LIMIT);
+    __syncwarp();
+    j = bk->job[slot];
+    __syncwarp();
+    mbar_arrive_lane0(smem_u32(&bk->job_empty[slot]), lane);
+    return got && j.n >= 0;
+  };
 
   // The launch gives every thread 168 registers; a softmax thread holds its row's 128 logits and needs more, the first
   // warpgroup needs few: 128 x 72 + 256 x 216 = 384 x 168.
   if (warp < 4) {
     reg_dec<72>();
     if (warp == 0) {
-      // ---------------------------------------------------------------- key / value tiles
+      // ---------------------------------------------------------------- items, key / value tiles
       const uint32_t leader = warp_leader();
+      const int all = off[n_seg], chunk = ca_chunk(all, gridDim.x);
+      CaWalk<TileWork> walk;
+      walk.begin(a, off, n_seg, stop ? 0 : min(all, (int)blockIdx.x * chunk), stop ? 0 : min(all, ((int)blockIdx.x + 1) * chunk));
+      CaJob j;
       int tc = 0, issued = 0;
       uint32_t raw_any = 0u, raw_odd = 0u, raw_last = 0u;     // per ring slot: copies through `raw`: any, an odd number, the latest one
-      while (walk.next(a, off, it)) {
+      for (int jc = 0;; ++jc) {
+        const int slot = jc % CT_JOBS;
+        const bool more = walk.next(a, off, j);
+        if (more) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const int i0 = j.rt * TileWork::ROWS + g * 128, last = min(i0 + 128, j.R) - 1;
+            j.n_act[g] = i0 < j.R ? max(0, min(j.kt0 + j.n, (ca_admitted(j, j.causal ? last / a.rep : 0) + 127) / 128) - j.kt0) : 0;
+          }
+        } else {
+          j.n = -1;
+        }
+        // (the queue of items keeps working after an abort: every consumer must see the same sequence, ending with -1)
+        if (jc >= CT_JOBS) mbar_wait_drain(smem_u32(&bk->job_empty[slot]), ((jc / CT_JOBS) - 1) & 1, CA_WAIT_LIMIT);
+        __syncwarp();
+        if (lane == 0) bk->job[slot] = j;
+        mbar_arrive_lane0(smem_u32(&bk->job_full[slot]), lane);
+        if (!more) break;
 #pragma unroll 1
-        for (int kt = it.kt0; kt < it.kt1; ++kt) {
-          const bool passed = ct_passed(a, it, kt);
+        for (int kt = j.kt0; kt < j.kt0 + j.n; ++kt) {
+          const bool passed = ct_passed(j, a.rep, kt);
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv, ++tc) {
             const int s = tc % CT_SLOTS;
@@ -812,10 +911,10 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
             const uint32_t bar = smem_u32(past ? &bk->raw[s] : &bk->full[s]), dst = ring + s * CT_TILE_BYTES, bit = 1u << s;
             raw_last = past ? raw_last | bit : raw_last & ~bit;
             if (past) { raw_any |= bit; raw_odd ^= bit; }
-            const int row = it.g.row0 + kt * 128;
+            const int row = j.row0 + kt * 128;
             mbar_expect_tx_w(bar, CT_TILE_BYTES, leader);
-            tma_load_3d_w(dst, kv ? &tmap_v : &tmap_k, bar, 0, it.head, row, leader);
-            tma_load_3d_w(dst + CT_BLOCK_BYTES, kv ? &tmap_v : &tmap_k, bar, 64, it.head, row, leader);
+            tma_load_3d_w(dst, kv ? &tmap_v : &tmap_k, bar, 0, j.head, row, leader);
+            tma_load_3d_w(dst + CT_BLOCK_BYTES, kv ? &tmap_v : &tmap_k, bar, 64, j.head, row, leader);
             issued = tc + 1;
           }
         }
@@ -837,8 +936,10 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       const uint64_t qdesc = umma_desc_sw128(q_smem), tile0 = umma_desc_sw128(ring), vtile0 = umma_desc_sw128_mn(ring, CT_BLOCK_BYTES);
       int t0 = 0;                                 // first tile of the item in the ring
       int qc[2] = {0, 0}, pc[2] = {0, 0}, sn = 0; // query tiles, P tiles and S so far
-      while (walk.next(a, off, it)) {
-        const int n[2] = {ct_active(a, it, 0), ct_active(a, it, 1)}, n_max = it.kt1 - it.kt0;
+      CaJob j;
+      for (int jc = 0; take(jc, j); ++jc) {
+        auto field = [&](int f) { return __shfl_sync(0xffffffffu, f, 0); };
+        const int n[2] = {field(j.n_act[0]), field(j.n_act[1])}, n_max = field(j.n);
         for (int kt = 0; kt <= n_max; ++kt) {
           const int tk = t0 + 2 * kt, tv = tk - 1;            // ring tiles: K of this key tile, V of the previous one
           const int sk = tk & (CT_SLOTS - 1), sv = tv & (CT_SLOTS - 1);
@@ -883,73 +984,87 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       // ---------------------------------------------------------------- value rows that must not reach every query row
       // Their probabilities are exactly zero there, but 0 * NaN is NaN: rows past the segment are cleared, and elements that are not finite
       // in rows that only some query rows admit are cleared too and added by the softmax warps at the item's end (bk->bad).
-      int t0 = 0, ic = 0;
+      int t0 = 0;
       uint32_t raw_phase = 0u;                    // per ring slot
-      while (walk.next(a, off, it)) {
-        if (lane == 0) *reinterpret_cast<volatile int *>(&bk->bad[ic & 3]) = 0;
+      CaJob j;
+      for (int jc = 0; take(jc, j); ++jc) {
+        if (lane == 0) *reinterpret_cast<volatile int *>(&bk->bad[jc & 3]) = 0;
         __syncwarp();
-        for (int kt = it.kt0; kt < it.kt1; ++kt) {
-          if (!ct_passed(a, it, kt)) continue;
-          const int s = (t0 + 2 * (kt - it.kt0) + 1) & (CT_SLOTS - 1);
+        for (int k = 0; k < j.n; ++k) {
+          const int kt = j.kt0 + k;
+          if (!ct_passed(j, a.rep, kt)) continue;
+          const int s = (t0 + 2 * k + 1) & (CT_SLOTS - 1);
           const bool landed = mbar_wait(smem_u32(&bk->raw[s]), (raw_phase >> s) & 1u, wc);
           raw_phase ^= 1u << s;
           if (!__all_sync(0xffffffffu, landed)) continue;     // (gave up: the copy may not have been issued)
           uint8_t *tile = ct_smem + (2 + s) * CT_TILE_BYTES;
-          const int rows = max(0, min(128, it.g.keys - kt * 128));          // rows of the segment
-          const int free_rows = max(0, min(rows, ca_admitted(a, it.g, it.rt * TileWork::ROWS) - kt * 128));   // ... that all query rows admit
-          bool bad = false;
-          for (int i = free_rows * 8 + lane; i < 128 * 8; i += 32)
+          const int rows = max(0, min(128, j.keys - kt * 128));             // rows of the segment
+          const int free_rows = max(0, min(rows, ca_admitted(j, j.causal ? j.rt * TileWork::ROWS / a.rep : 0) - kt * 128));   // ... that all query rows admit
+          uint32_t hit = 0u;
+#pragma unroll 8
+          for (int i = free_rows * 8 + lane; i < rows * 8; i += 32)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              uint4 *p = reinterpret_cast<uint4 *>(tile + h * CT_BLOCK_BYTES) + i;
-              if (i >= rows * 8) {
-                *p = make_uint4(0u, 0u, 0u, 0u);
-              } else {
-                uint4 x = *p;
-                if (not_finite16(x.x, F16) || not_finite16(x.y, F16) || not_finite16(x.z, F16) || not_finite16(x.w, F16)) {
-                  bad = true;
-                  uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) {
-                    if (not_finite16(w[e] & 0xffffu, F16)) w[e] &= 0xffff0000u;
-                    if (not_finite16(w[e] & 0xffff0000u, F16)) w[e] &= 0xffffu;
-                  }
-                  *p = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-              }
+              const uint4 x = reinterpret_cast<const uint4 *>(tile + h * CT_BLOCK_BYTES)[i];
+              hit |= not_finite_bits<F16>(x.x) | not_finite_bits<F16>(x.y) | not_finite_bits<F16>(x.z) | not_finite_bits<F16>(x.w);
             }
-          if (__any_sync(0xffffffffu, bad) && lane == 0) *reinterpret_cast<volatile int *>(&bk->bad[ic & 3]) = 1;
+          for (int i = rows * 8 + lane; i < 128 * 8; i += 32) {
+            reinterpret_cast<uint4 *>(tile)[i] = make_uint4(0u, 0u, 0u, 0u);
+            reinterpret_cast<uint4 *>(tile + CT_BLOCK_BYTES)[i] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          if (__any_sync(0xffffffffu, hit != 0u)) {
+            for (int i = free_rows * 16 + lane; i < rows * 16; i += 32) {
+              uint4 *p = reinterpret_cast<uint4 *>(tile + (i & 1) * CT_BLOCK_BYTES) + (i >> 1);
+              uint4 x = *p;
+              uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t b = not_finite_bits<F16>(w[e]);
+                if (b & 0x8000u) w[e] &= 0xffff0000u;
+                if (b & 0x80000000u) w[e] &= 0xffffu;
+              }
+              *p = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            if (lane == 0) *reinterpret_cast<volatile int *>(&bk->bad[jc & 3]) = 1;
+          }
           __threadfence_block();
           fence_proxy_async();
           __syncwarp();
           mbar_arrive_lane0(smem_u32(&bk->full[s]), lane);
         }
-        t0 += 2 * (it.kt1 - it.kt0);
-        ++ic;
+        t0 += 2 * j.n;
       }
     } else {
       // ---------------------------------------------------------------- query rows
-      // (gathered: stacked row i is query row i / rep, head i % rep of the key / value head; rows past the last one are zero up to the next
-      // multiple of 32, so that their lanes of a softmax warp hold nothing that would move a reference)
+      // (gathered: stacked row i is query row i / rep, head i % rep of the key / value head; rows past the last one keep whatever the
+      // buffer holds, nothing of theirs is used).  A lane works out the addresses of four rows; sixteen lanes copy a row.
       int qc[2] = {0, 0};
-      while (walk.next(a, off, it)) {
-        const int R = it.g.nq * a.rep;
+      CaJob j;
+      for (int jc = 0; take(jc, j); ++jc) {
 #pragma unroll 1
         for (int g = 0; g < 2; ++g) {
-          if (ct_active(a, it, g) == 0) continue;
-          if (qc[g] >= 1) mbar_wait_warp(smem_u32(&bk->q_empty[g]), (qc[g] - 1) & 1, wc);
-          ++qc[g];
-          const int i0 = it.rt * TileWork::ROWS + g * 128, n = min(128, R - i0);
-          const uint32_t dst = q_smem + g * CT_TILE_BYTES;
+          if ((g ? j.n_act[1] : j.n_act[0]) == 0) continue;
+          if ((g ? qc[1] : qc[0]) >= 1) mbar_wait_warp(smem_u32(&bk->q_empty[g]), ((g ? qc[1] : qc[0]) - 1) & 1, wc);
+          if (g) ++qc[1];
+          else ++qc[0];
+          const int i0 = j.rt * TileWork::ROWS + g * 128, n = min(128, j.R - i0);
           const int c = lane & 15;                // 16-byte piece of a row
-          for (int r = lane >> 4; r < ((n + 31) & ~31); r += 2) {
-            const int i = i0 + r;
-            if (r >= n) {
-              *reinterpret_cast<uint4 *>(ct_smem + g * CT_TILE_BYTES + (c >> 3) * CT_BLOCK_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
-              continue;
+          long long from[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int i = min(i0 + 32 * k + lane, j.R - 1), t = i / a.rep;
+            from[k] = (long long)(j.q0 + t) * a.q_row + (long long)(j.head * a.rep + (i - t * a.rep)) * a.q_head;
+          }
+          const uint32_t dst = q_smem + g * CT_TILE_BYTES + (c >> 3) * CT_BLOCK_BYTES;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (32 * k >= n) continue;
+#pragma unroll 4
+            for (int r2 = 0; r2 < 32; r2 += 2) {
+              const int r = 32 * k + r2 + (lane >> 4);
+              const long long at = __shfl_sync(0xffffffffu, from[k], r2 + (lane >> 4));
+              cp_async16(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4), a.q + at + c * 8);
             }
-            const uint16_t *src = a.q + (long long)(it.g.q0 + i / a.rep) * a.q_row + (long long)(it.head * a.rep + i % a.rep) * a.q_head + c * 8;
-            cp_async16(dst + (c >> 3) * CT_BLOCK_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4), src);
           }
           cp_async_commit();
           cp_async_wait<0>();
@@ -970,21 +1085,23 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
     const float scale = a.scale_log2;
     const uint64_t scale2 = f2_pack(scale, scale);
     uint8_t *stage = ct_smem + CT_STAGE_OFF + (warp - 4) * CT_STAGE_BYTES;
-    int sc = 0, ic = 0;                           // key tiles and items so far
-    for (; walk.next(a, off, it); ++ic) {
-      const int R = it.g.nq * a.rep, i = it.rt * TileWork::ROWS + g * 128 + lrow, i_lo = i - lane;
-      if (i_lo - quarter * 32 >= R) continue;     // no such row tile
-      const int n_act = ct_active(a, it, g);
-      const bool live = i_lo < R;                 // the warp has rows
-      const int adm = i < R ? ca_admitted(a, it.g, i) : 0, adm_lo = live ? ca_admitted(a, it.g, i_lo) : 0;
-      const long long entry = i < R ? (long long)(it.g.q0 + i / a.rep) * a.H + it.head * a.rep + i % a.rep : -1;
+    int sc = 0;                                   // key tiles so far
+    CaJob j;
+    for (int jc = 0; take(jc, j); ++jc) {
+      const int i = j.rt * TileWork::ROWS + g * 128 + lrow, i_lo = i - lane;
+      if (i_lo - quarter * 32 >= j.R) continue;   // no such row tile
+      const int n_act = g ? j.n_act[1] : j.n_act[0];
+      const bool live = i_lo < j.R;               // the warp has rows
+      const int qt = i / a.rep;
+      const int adm = i < j.R ? ca_admitted(j, qt) : 0, adm_lo = live ? ca_admitted(j, i_lo / a.rep) : 0;
+      const long long entry = i < j.R ? (long long)(j.q0 + qt) * a.H + j.head * a.rep + (i - qt * a.rep) : -1;
       // p = 2^(x * scale - ref).  The reference is the maximum of the row's first key tile and then stays: one below the running
       // maximum only scales the sums.  Should a tile's sum outgrow the limit in some row of the warp, that tile is done again with the
       // row's true maximum as the new reference (O and the sum so far are rescaled).
       float neg_ref = 0.f, l_run = 0.f;
       bool unset = true;                          // no logit above -inf so far
       for (int t = 0; t < n_act; ++t, ++sc) {
-        const int j0 = (it.kt0 + t) * 128;
+        const int j0 = (j.kt0 + t) * 128;
         mbar_wait_warp(smem_u32(&bk->s_full[g]), sc & 1, wc);    // (no lane may still wait for a phase when lane 0 has arrived for it)
         tc_fence_after();
         if (!live) {                              // (one arrival per phase: the previous P V comes first here too)
@@ -1024,7 +1141,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
               const int rr = r8 + (lane >> 2), c = lane & 3;
               const long long e = __shfl_sync(0xffffffffu, entry, rr);
               const float4 v = *reinterpret_cast<const float4 *>(stage + rr * 64 + ((c ^ ((rr >> 1) & 3)) << 4));
-              if (e >= 0) *reinterpret_cast<float4 *>(a.logits + e * a.pitch + (it.g.causal ? a.own_off : 0) + j0 + c0 + 4 * c) = v;
+              if (e >= 0) *reinterpret_cast<float4 *>(a.logits + e * a.pitch + (j.causal ? a.own_off : 0) + j0 + c0 + 4 * c) = v;
             }
           }
           __syncwarp();
@@ -1083,7 +1200,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
           float s0, s1;
           f2_unpack(f2_add(sum2[0], sum2[1]), s0, s1);
           tile_sum = s0 + s1;
-          move = !moved && !(tile_sum < (F16 ? CT_SUM_LIMIT_F16 : CT_SUM_LIMIT_BF16));     // (relative to the true maximum no sum exceeds 128)
+          move = i < j.R && !moved && !(tile_sum < (F16 ? CT_SUM_LIMIT_F16 : CT_SUM_LIMIT_BF16));     // (relative to the true maximum no sum exceeds 128)
           if (!__any_sync(0xffffffffu, move)) break;
           again = true;
         }
@@ -1099,27 +1216,23 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
         tc_fence_after();
       }
       if (!live) continue;
-      const long long before = off[it.seg] + it.head * ((off[it.seg + 1] - off[it.seg]) / a.kv) + ca_tiles_before<TileWork>(a, it.g, it.rt);
-      const CaPlace pl = ca_place(before, it.kt_all, chunk);
-      const bool complete = pl.c0 == pl.c1;
       // NaN in every logit leaves no maximum, but the row is not an empty one
-      const bool none = n_act == 0 || (unset && l_run == 0.f);
-      const long long at = i >= R ? -1 : complete ? (it.g.causal ? (long long)a.n_q * a.H : 0) + entry
-                                                  : (long long)(2 * blockIdx.x + (pl.first <= blockIdx.x * chunk ? 0 : 1)) * TileWork::ROWS + g * 128 + lrow;
+      const bool none = n_act == 0 || (unset && l_run == 0.f), complete = j.complete != 0;
+      const long long at = i >= j.R ? -1 : complete ? (j.causal ? (long long)a.n_q * a.H : 0) + entry : (long long)j.record * TileWork::ROWS + g * 128 + lrow;
       const bool write = !bk->abort_flag;
       if (at >= 0 && write) (complete ? a.full_ml : a.rec_ml[1])[at] = none ? make_float2(-INFINITY, 0.f) : make_float2(-neg_ref, l_run);
       if (n_act == 0) continue;
       float *dst = complete ? a.full_o : a.rec_o[1];
-      const bool bad = *reinterpret_cast<volatile int *>(&bk->bad[ic & 3]) != 0;
+      const bool bad = *reinterpret_cast<volatile int *>(&bk->bad[jc & 3]) != 0;
 #pragma unroll 1
       for (int c0 = 0; c0 < 128; c0 += 16) {
         uint32_t r[16];
         tmem_ld16(o_addr + c0, r);
         tmem_wait_ld();
         if (bad) {                                  // what warp 2 left out
-          const int from = max(it.kt0 * 128, ca_admitted(a, it.g, it.rt * TileWork::ROWS)), to = min(it.kt1 * 128, adm);
-          for (int j = from; j < to; ++j) {
-            const uint16_t *v = a.v + (long long)(it.g.row0 + j) * a.kv_row + (long long)it.head * a.kv_head + c0;
+          const int from = max(j.kt0 * 128, ca_admitted(j, j.causal ? j.rt * TileWork::ROWS / a.rep : 0)), to = min((j.kt0 + j.n) * 128, adm);
+          for (int key = from; key < to; ++key) {
+            const uint16_t *v = a.v + (long long)(j.row0 + key) * a.kv_row + (long long)j.head * a.kv_head + c0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               uint32_t w;
@@ -1159,6 +1272,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
 // Partial results of a (query row, head) -> output.  A warp each; a lane holds four of the 128 values.
 // ---------------------------------------------------------------------------------------
 constexpr int CA_JOIN_THREADS = 128;
+constexpr int CA_JOIN_HEADS = 8;                 // heads of a block; a warp takes every fourth
 
 __device__ __forceinline__ float2 ld_prev2f(const float2 *p) {
   float2 v;
@@ -1170,111 +1284,115 @@ __device__ __forceinline__ float4 ld_prev4f(const float *p) {
   asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
   return v;
 }
-__device__ __forceinline__ long long ld_prev64(const long long *p) {
-  long long v;
-  asm volatile("ld.global.s64 %0, [%1];" : "=l"(v) : "l"(p));
-  return v;
-}
 
-template <bool F16>
-__global__ void __launch_bounds__(CA_JOIN_THREADS)
-ca_join_kernel(const __grid_constant__ CacheArgs a) {
-  pdl_enter();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long entry = (long long)blockIdx.x * (CA_JOIN_THREADS / 32) + warp;
-  if (entry >= (long long)a.n_q * a.H) return;
-  if (*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) return;
-  const int qr = (int)(entry / a.H), h = (int)(entry - (long long)qr * a.H);
-  const int2 own = ld_prev(a.row_owner + qr);
-  CaSeg seg[2];                                  // prefix, own
-  bool ok = own.x >= 0 && own.x < a.B && own.y < a.G && own.y >= -1;
-  if (ok) {
-    seg[1] = ca_segment(a, a.G + own.x);
-    ok = seg[1].valid && qr >= seg[1].q0 && qr < seg[1].q0 + seg[1].nq;
-  }
-  if (!ok) {                                     // a row of a sequence that is skipped
-    if (lane == 0) a.lse2[entry] = INFINITY;
-    return;
-  }
-  const int n_seg = a.G + a.B;
-  float top = -INFINITY, sum = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto add = [&](float2 ml, float4 o) {
+struct CaSum {
+  float top, sum;
+  float4 acc;
+  __device__ __forceinline__ void add(float2 ml, float4 o) {
     if (ml.x == -INFINITY) return;
     const float t = fmaxf(top, ml.x), f = top == -INFINITY ? 0.f : fast_exp2(top - t), g = fast_exp2(ml.x - t);
     sum = sum * f + ml.y * g;
     acc.x = acc.x * f + o.x * g; acc.y = acc.y * f + o.y * g; acc.z = acc.z * f + o.z * g; acc.w = acc.w * f + o.w * g;
     top = t;
-  };
-  for (int part = own.y >= 0 ? 0 : 1; part < 2; ++part) {
-    const int s = part == 0 ? own.y : a.G + own.x;
-    if (part == 0) seg[0] = ca_segment(a, s);
-    const CaSeg &g = seg[part];
-    const int i = (qr - g.q0) * a.rep + h % a.rep;
-    auto gather = [&](auto work) {
-      using WORK = decltype(work);
-      const int rt = i / WORK::ROWS, r = i % WORK::ROWS, n = ca_key_tiles<WORK>(a, g, rt);
-      if (n == 0) return;
-      const long long *plan = a.plan + WORK::INDEX * (n_seg + 1);
-      const long long off0 = ld_prev64(plan + s), off1 = ld_prev64(plan + s + 1), chunk = ca_chunk(ld_prev64(plan + n_seg), a.blocks[WORK::INDEX]);
-      const CaPlace pl = ca_place(off0 + (h / a.rep) * ((off1 - off0) / a.kv) + ca_tiles_before<WORK>(a, g, rt), n, chunk);
-      if (pl.c0 == pl.c1) {
-        const long long e = (long long)part * a.n_q * a.H + entry;
-        add(ld_prev2f(a.full_ml + e), ld_prev4f(a.full_o + e * 128 + lane * 4));
-        return;
-      }
-#pragma unroll 4
-      for (int c = pl.c0; c <= pl.c1; ++c) {
-        const long long e = (long long)(2 * c + (pl.first <= c * chunk ? 0 : 1)) * WORK::ROWS + r;
-        add(ld_prev2f(a.rec_ml[WORK::INDEX] + e), ld_prev4f(a.rec_o[WORK::INDEX] + e * 128 + lane * 4));
-      }
-    };
-    if (ca_streamed(a, g)) gather(StreamWork{});
-    else gather(TileWork{});
   }
-  const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);    // (NaN stays NaN)
-  uint16_t *dst = a.out + (long long)qr * a.out_row + (long long)h * a.out_head + lane * 4;
-  *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2_t<F16>(acc.x * inv, acc.y * inv), pack2_t<F16>(acc.z * inv, acc.w * inv));
-  if (lane == 0) {
-    const float l2 = top + __log2f(sum);
-    if (a.lse) a.lse[entry] = sum == 0.f ? -INFINITY : l2 * 0.6931471805599453f;
-    a.lse2[entry] = sum == 0.f ? INFINITY : l2;
+};
+template <typename WORK>
+__device__ __forceinline__ void ca_gather(const CacheArgs &a, const CaRowPart &p, int which, int chunk, long long entry, int h, int lane, CaSum &out) {
+  const int i = p.i0 + h % a.rep, rt = i / WORK::ROWS, r = i - rt * WORK::ROWS;
+  const int kt = ca_key_tiles<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, rt);
+  if (kt == 0) return;
+  const int first = p.off + (h / a.rep) * p.per_head + ca_numbers<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, rt) + WORK::EXTRA;
+  const int c0 = first / chunk, c1 = (first + kt - 1) / chunk;
+  if (c0 == c1) {
+    const long long e = (long long)which * a.n_q * a.H + entry;
+    out.add(ld_prev2f(a.full_ml + e), ld_prev4f(a.full_o + e * 128 + lane * 4));
+    return;
+  }
+#pragma unroll 4
+  for (int c = c0; c <= c1; ++c) {
+    const long long e = (long long)(2 * c + (first <= c * chunk ? 0 : 1)) * WORK::ROWS + r;
+    out.add(ld_prev2f(a.rec_ml[WORK::INDEX] + e), ld_prev4f(a.rec_o[WORK::INDEX] + e * 128 + lane * 4));
+  }
+}
+
+template <bool F16>
+__global__ void __launch_bounds__(CA_JOIN_THREADS, 7)
+ca_join_kernel(const __grid_constant__ CacheArgs a) {
+  pdl_enter();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, qr = blockIdx.x, n_seg = a.G + a.B;
+  if (*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) return;
+  // every query row of [q_cu[0], q_cu[B]) has an entry of this call unless the call is skipped
+  const bool out_of_range = a.q_cu && (qr < ld_prev(a.q_cu) || qr >= ld_prev(a.q_cu + a.B));
+  if (out_of_range || ld_prev(a.plan + 2 * (n_seg + 1)) == 0) return;
+  CaRow row;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) ld_prev8(reinterpret_cast<const uint4 *>(a.rows + qr) + e, reinterpret_cast<uint4 *>(&row)[e]);
+  const int chunk0 = ca_chunk(ld_prev(a.plan + n_seg), a.blocks[0]), chunk1 = a.blocks[1] ? ca_chunk(ld_prev(a.plan + 2 * n_seg + 1), a.blocks[1]) : 1;
+  const int h1 = min(a.H, ((int)blockIdx.y + 1) * CA_JOIN_HEADS);
+#pragma unroll 2
+  for (int h = blockIdx.y * CA_JOIN_HEADS + warp; h < h1; h += CA_JOIN_THREADS / 32) {
+    const long long entry = (long long)qr * a.H + h;
+    if (row.valid != 1) {                        // a row of a sequence that is skipped
+      if (lane == 0) a.lse2[entry] = INFINITY;
+      continue;
+    }
+    CaSum s{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      if (row.part[p].R == 0) continue;
+      if (ca_streamed(row.part[p].R)) ca_gather<StreamWork>(a, row.part[p], p, chunk0, entry, h, lane, s);
+      else ca_gather<TileWork>(a, row.part[p], p, chunk1, entry, h, lane, s);
+    }
+    const float inv = s.sum > 0.f ? 1.f / s.sum : (s.sum == 0.f ? 0.f : s.sum);    // (NaN stays NaN)
+    uint16_t *dst = a.out + (long long)qr * a.out_row + (long long)h * a.out_head + lane * 4;
+    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2_t<F16>(s.acc.x * inv, s.acc.y * inv), pack2_t<F16>(s.acc.z * inv, s.acc.w * inv));
+    if (lane == 0) {
+      const float l2 = s.top + __log2f(s.sum);
+      if (a.lse) a.lse[entry] = s.sum == 0.f ? -INFINITY : l2 * 0.6931471805599453f;
+      a.lse2[entry] = s.sum == 0.f ? INFINITY : l2;
+    }
   }
 }
 
 // ---------------------------------------------------------------------------------------
-// weights[j] += 1 / H * sum over the segment's query rows and heads of 2^(x - lse2).  A block per 32 keys of a segment: lane = key, the
+// weights[j] += 1 / H * sum over the segment's query rows and heads of 2^(x - lse2).  A block per 128 keys of a segment, four of them a lane; the
 // warps share the (row, head) pairs and their sums are added in the order of the warps.
 // ---------------------------------------------------------------------------------------
-constexpr int CA_WEIGHT_THREADS = 512;
+constexpr int CA_WEIGHT_THREADS = 512, CA_WEIGHT_KEYS = 128;
 
 __global__ void __launch_bounds__(CA_WEIGHT_THREADS)
 ca_weight_kernel(const __grid_constant__ CacheArgs a, int prefix_blocks, int own_blocks) {
-  __shared__ float part[CA_WEIGHT_THREADS / 32][32];
+  __shared__ float4 part[CA_WEIGHT_THREADS / 32][32];
   pdl_enter();
   const int n_pre = a.G * prefix_blocks;
   const int s = (int)blockIdx.x < n_pre ? blockIdx.x / prefix_blocks : a.G + (blockIdx.x - n_pre) / own_blocks;
   const int kb = (int)blockIdx.x < n_pre ? blockIdx.x % prefix_blocks : (blockIdx.x - n_pre) % own_blocks;
   const CaSeg g = ca_segment(a, s);
-  if (!g.valid || kb * 32 >= g.keys) return;
+  if (!g.valid || kb * CA_WEIGHT_KEYS >= g.keys || ld_prev(a.plan + 2 * (a.G + a.B + 1)) == 0) return;
   if (*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = kb * 32 + lane;
-  const long long n = (long long)g.nq * a.H;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = kb * CA_WEIGHT_KEYS + lane * 4;
+  const int n = g.nq * a.H, adm0 = g.keys - g.nq + 1;
   const float *x = a.logits + (long long)g.q0 * a.H * a.pitch + (g.causal ? a.own_off : 0) + j;
-  float sum = 0.f;
+  const float *lse2 = a.lse2 + (long long)g.q0 * a.H;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (long long e = warp; e < n; e += CA_WEIGHT_THREADS / 32) {
-    const float l2 = ld_prev(a.lse2 + (long long)g.q0 * a.H + e);
-    const bool in = j < g.keys && (!g.causal || j < g.keys - g.nq + 1 + (int)(e / a.H));
-    const float v = in ? ld_prev(x + e * a.pitch) : -INFINITY;
-    sum += in && l2 != INFINITY ? fast_exp2(v - l2) : 0.f;
+  for (int e = warp; e < n; e += CA_WEIGHT_THREADS / 32) {
+    const float l2 = ld_prev(lse2 + e);
+    const int lim = ca_admitted(g.keys, adm0, g.causal, e / a.H) - j;          // keys of the lane's four that the row admits
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (lim > 0) v = ld_prev4f(x + e * a.pitch);
+    const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) sum[c] += c < lim && l2 != INFINITY ? fast_exp2(w[c] - l2) : 0.f;
   }
-  part[warp][lane] = sum;
+  part[warp][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
   __syncthreads();
-  if (warp == 0 && j < g.keys) {
+  const int key = kb * CA_WEIGHT_KEYS + (int)threadIdx.x;
+  if (threadIdx.x < CA_WEIGHT_KEYS && key < g.keys) {
     float t = 0.f;
-    for (int w = 0; w < CA_WEIGHT_THREADS / 32; ++w) t += part[w][lane];
-    float *p = a.weights + g.row0 + j;
+#pragma unroll
+    for (int w = 0; w < CA_WEIGHT_THREADS / 32; ++w) t += reinterpret_cast<const float *>(part[w])[threadIdx.x];
+    float *p = a.weights + g.row0 + key;
     *p = ld_prev(p) + t / (float)a.H;
   }
 }
