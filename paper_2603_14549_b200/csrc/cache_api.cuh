@@ -272,7 +272,11 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
              map_k[0], map_v[0], a);
   ASAP_TRY(after_launch(ctx, "cache_stream"));
   mark(ctx, "cache_join", st);
-  launch_pdl(f16 ? ca_join_kernel<true> : ca_join_kernel<false>, dim3(p->n_q, (p->H + CA_JOIN_HEADS - 1) / CA_JOIN_HEADS), dim3(CA_JOIN_THREADS), 0, st, a);
+  // (one wave of the split form: 1 x 32 heads 14 -> 8 us, 5 rows of up to 150 partial results 17 -> 8; 128 rows 21 -> 62)
+  const bool split = (long long)p->n_q * ((p->H + CA_JOIN_SPLIT_HEADS - 1) / CA_JOIN_SPLIT_HEADS) <= 2LL * ctx->num_sms;
+  const int heads = split ? CA_JOIN_SPLIT_HEADS : CA_JOIN_HEADS;
+  launch_pdl(f16 ? (split ? ca_join_kernel<true, true> : ca_join_kernel<true, false>) : (split ? ca_join_kernel<false, true> : ca_join_kernel<false, false>),
+             dim3(p->n_q, (p->H + heads - 1) / heads), dim3(CA_JOIN_THREADS), 0, st, a);
   ASAP_TRY(after_launch(ctx, "cache_join"));
   if (p->weights) {
     const long long pre = (p->max_prefix + CA_WEIGHT_KEYS - 1) / CA_WEIGHT_KEYS, own = (p->max_len + CA_WEIGHT_KEYS - 1) / CA_WEIGHT_KEYS;

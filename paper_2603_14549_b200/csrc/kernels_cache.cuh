@@ -1269,10 +1269,13 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
 }
 
 // ---------------------------------------------------------------------------------------
-// Partial results of a (query row, head) -> output.  A warp each; a lane holds four of the 128 values.
+// Partial results of a (query row, head) -> output, four of the 128 values a lane.  A thread works out where the partial results of one (head,
+// prefix or own rows) lie.  (With the addresses worked out by every warp for itself the kernel was bound by those instructions: 2254
+// rows x 32 heads 67 us.)  Two forms: with many rows a block takes 32 heads of a query row, a warp two of them; with few (SPLIT) a
+// block takes two heads and eight warps share the partial results of one, of which a long sequence has a hundred or more.
 // ---------------------------------------------------------------------------------------
-constexpr int CA_JOIN_THREADS = 128;
-constexpr int CA_JOIN_HEADS = 8;                 // heads of a block; a warp takes every fourth
+constexpr int CA_JOIN_THREADS = 512, CA_JOIN_WARPS = CA_JOIN_THREADS / 32;
+constexpr int CA_JOIN_HEADS = 32, CA_JOIN_SPLIT_HEADS = 2;
 
 __device__ __forceinline__ float2 ld_prev2f(const float2 *p) {
   float2 v;
@@ -1286,8 +1289,8 @@ __device__ __forceinline__ float4 ld_prev4f(const float *p) {
 }
 
 struct CaSum {
-  float top, sum;
-  float4 acc;
+  float top = -INFINITY, sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   __device__ __forceinline__ void add(float2 ml, float4 o) {
     if (ml.x == -INFINITY) return;
     const float t = fmaxf(top, ml.x), f = top == -INFINITY ? 0.f : fast_exp2(top - t), g = fast_exp2(ml.x - t);
@@ -1296,60 +1299,147 @@ struct CaSum {
     top = t;
   }
 };
+// The partial results of one part of a (query row, head): the first at entry `first` of `ml` and `o`, the others every `step` entries from
+// `next` on, `n` in all.
+struct CaParts {
+  const float2 *ml;
+  const float *o;
+  long long first, next;
+  int step, n;
+  int pad[2];
+  __device__ __forceinline__ long long at(int k) const { return k == 0 ? first : next + (long long)(k - 1) * step; }
+};
 template <typename WORK>
-__device__ __forceinline__ void ca_gather(const CacheArgs &a, const CaRowPart &p, int which, int chunk, long long entry, int h, int lane, CaSum &out) {
-  const int i = p.i0 + h % a.rep, rt = i / WORK::ROWS, r = i - rt * WORK::ROWS;
+__device__ __forceinline__ CaParts ca_parts_of(const CacheArgs &a, const CaRowPart &p, int which, int all, long long entry, int kvh, int sub) {
+  CaParts out;
+  const int i = p.i0 + sub, rt = i / WORK::ROWS, r = i - rt * WORK::ROWS;
   const int kt = ca_key_tiles<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, rt);
-  if (kt == 0) return;
-  const int first = p.off + (h / a.rep) * p.per_head + ca_numbers<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, rt) + WORK::EXTRA;
+  const int chunk = ca_chunk(all, a.blocks[WORK::INDEX]);
+  const int first = p.off + kvh * p.per_head + ca_numbers<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, rt) + WORK::EXTRA;
   const int c0 = first / chunk, c1 = (first + kt - 1) / chunk;
-  if (c0 == c1) {
-    const long long e = (long long)which * a.n_q * a.H + entry;
-    out.add(ld_prev2f(a.full_ml + e), ld_prev4f(a.full_o + e * 128 + lane * 4));
-    return;
-  }
-#pragma unroll 4
-  for (int c = c0; c <= c1; ++c) {
-    const long long e = (long long)(2 * c + (first <= c * chunk ? 0 : 1)) * WORK::ROWS + r;
-    out.add(ld_prev2f(a.rec_ml[WORK::INDEX] + e), ld_prev4f(a.rec_o[WORK::INDEX] + e * 128 + lane * 4));
-  }
+  const bool complete = c0 == c1;
+  out.n = kt == 0 ? 0 : c1 - c0 + 1;
+  out.step = 2 * WORK::ROWS;
+  out.ml = complete ? a.full_ml : a.rec_ml[WORK::INDEX];
+  out.o = complete ? a.full_o : a.rec_o[WORK::INDEX];
+  out.first = complete ? (long long)which * a.n_q * a.H + entry : (long long)(2 * c0 + (first <= c0 * chunk ? 0 : 1)) * WORK::ROWS + r;
+  out.next = (long long)(2 * c0 + 2) * WORK::ROWS + r;
+  return out;
 }
 
 template <bool F16>
-__global__ void __launch_bounds__(CA_JOIN_THREADS, 7)
+__device__ __forceinline__ void ca_finish_row(const CacheArgs &a, const CaSum &s, int qr, int h, int lane) {
+  const long long entry = (long long)qr * a.H + h;
+  const float inv = s.sum > 0.f ? 1.f / s.sum : (s.sum == 0.f ? 0.f : s.sum);    // (NaN stays NaN)
+  uint16_t *dst = a.out + (long long)qr * a.out_row + (long long)h * a.out_head + lane * 4;
+  *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2_t<F16>(s.acc.x * inv, s.acc.y * inv), pack2_t<F16>(s.acc.z * inv, s.acc.w * inv));
+  if (lane == 0) {
+    const float l2 = s.top + __log2f(s.sum);
+    if (a.lse) a.lse[entry] = s.sum == 0.f ? -INFINITY : l2 * 0.6931471805599453f;
+    a.lse2[entry] = s.sum == 0.f ? INFINITY : l2;
+  }
+}
+
+template <bool F16, bool SPLIT>
+__global__ void __launch_bounds__(CA_JOIN_THREADS)
 ca_join_kernel(const __grid_constant__ CacheArgs a) {
+  constexpr int HEADS = SPLIT ? CA_JOIN_SPLIT_HEADS : CA_JOIN_HEADS;
+  __shared__ CaParts sh_parts[HEADS][2];
+  __shared__ float4 sh_acc[SPLIT ? CA_JOIN_WARPS : 1][32];
+  __shared__ float2 sh_ml[SPLIT ? CA_JOIN_WARPS : 1];
   pdl_enter();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, qr = blockIdx.x, n_seg = a.G + a.B;
-  if (*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, qr = blockIdx.x, n_seg = a.G + a.B, h0 = blockIdx.y * HEADS;
   // every query row of [q_cu[0], q_cu[B]) has an entry of this call unless the call is skipped
-  const bool out_of_range = a.q_cu && (qr < ld_prev(a.q_cu) || qr >= ld_prev(a.q_cu + a.B));
-  if (out_of_range || ld_prev(a.plan + 2 * (n_seg + 1)) == 0) return;
-  CaRow row;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) ld_prev8(reinterpret_cast<const uint4 *>(a.rows + qr) + e, reinterpret_cast<uint4 *>(&row)[e]);
-  const int chunk0 = ca_chunk(ld_prev(a.plan + n_seg), a.blocks[0]), chunk1 = a.blocks[1] ? ca_chunk(ld_prev(a.plan + 2 * n_seg + 1), a.blocks[1]) : 1;
-  const int h1 = min(a.H, ((int)blockIdx.y + 1) * CA_JOIN_HEADS);
-#pragma unroll 2
-  for (int h = blockIdx.y * CA_JOIN_HEADS + warp; h < h1; h += CA_JOIN_THREADS / 32) {
-    const long long entry = (long long)qr * a.H + h;
-    if (row.valid != 1) {                        // a row of a sequence that is skipped
-      if (lane == 0) a.lse2[entry] = INFINITY;
-      continue;
+  const uint32_t status = *reinterpret_cast<volatile uint32_t *>(a.status);
+  const int q0 = a.q_cu ? ld_prev(a.q_cu) : 0, q1 = a.q_cu ? ld_prev(a.q_cu + a.B) : a.n_q, going = ld_prev(a.plan + 2 * (n_seg + 1));
+  const int valid = ld_prev(&a.rows[qr].valid);
+  if (threadIdx.x < 2 * HEADS) {
+    const int h = h0 + (threadIdx.x >> 1), p = threadIdx.x & 1;
+    const CaRowPart *src = &a.rows[qr].part[p];
+    CaRowPart part;
+    part.i0 = ld_prev(&src->i0); part.R = ld_prev(&src->R); part.adm0 = ld_prev(&src->adm0); part.causal = ld_prev(&src->causal);
+    part.keys = ld_prev(&src->keys); part.off = ld_prev(&src->off); part.per_head = ld_prev(&src->per_head);
+    const int all0 = ld_prev(a.plan + n_seg), all1 = a.blocks[1] ? ld_prev(a.plan + 2 * n_seg + 1) : 0;
+    CaParts mine;
+    mine.n = 0;
+    if (h < a.H && going && valid == 1 && qr >= q0 && qr < q1 && part.R > 0) {
+      const int kvh = h / a.rep, sub = h - kvh * a.rep;
+      const long long entry = (long long)qr * a.H + h;
+      mine = ca_streamed(part.R) ? ca_parts_of<StreamWork>(a, part, p, all0, entry, kvh, sub) : ca_parts_of<TileWork>(a, part, p, all1, entry, kvh, sub);
     }
-    CaSum s{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    sh_parts[threadIdx.x >> 1][p] = mine;
+  }
+  __syncthreads();
+  if ((status & STATUS_CACHE_TIMEOUT) || !going || qr < q0 || qr >= q1) return;
+  if (valid != 1) {                              // a row of a sequence that is skipped
+    if (threadIdx.x < HEADS && h0 + (int)threadIdx.x < a.H) a.lse2[(long long)qr * a.H + h0 + threadIdx.x] = INFINITY;
+    return;
+  }
+  if constexpr (SPLIT) {
+    constexpr int SHARE = CA_JOIN_WARPS / HEADS;
+    const int e = warp / SHARE, w = warp - e * SHARE;
+    CaSum s;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-      if (row.part[p].R == 0) continue;
-      if (ca_streamed(row.part[p].R)) ca_gather<StreamWork>(a, row.part[p], p, chunk0, entry, h, lane, s);
-      else ca_gather<TileWork>(a, row.part[p], p, chunk1, entry, h, lane, s);
+      const CaParts &c = sh_parts[e][p];
+      for (int k0 = w; k0 < c.n; k0 += 8 * SHARE) {
+        float2 m8[8];
+        float4 o8[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const long long at = c.at(min(k0 + k * SHARE, c.n - 1));
+          m8[k] = ld_prev2f(c.ml + at);
+          o8[k] = ld_prev4f(c.o + at * 128 + lane * 4);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k0 + k * SHARE < c.n) s.add(m8[k], o8[k]);
+      }
     }
-    const float inv = s.sum > 0.f ? 1.f / s.sum : (s.sum == 0.f ? 0.f : s.sum);    // (NaN stays NaN)
-    uint16_t *dst = a.out + (long long)qr * a.out_row + (long long)h * a.out_head + lane * 4;
-    *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2_t<F16>(s.acc.x * inv, s.acc.y * inv), pack2_t<F16>(s.acc.z * inv, s.acc.w * inv));
-    if (lane == 0) {
-      const float l2 = s.top + __log2f(s.sum);
-      if (a.lse) a.lse[entry] = s.sum == 0.f ? -INFINITY : l2 * 0.6931471805599453f;
-      a.lse2[entry] = s.sum == 0.f ? INFINITY : l2;
+    sh_acc[warp][lane] = s.acc;
+    if (lane == 0) sh_ml[warp] = make_float2(s.top, s.sum);
+    __syncthreads();
+    if (w != 0 || h0 + e >= a.H) return;
+    for (int k = 1; k < SHARE; ++k) s.add(sh_ml[warp + k], sh_acc[warp + k][lane]);
+    ca_finish_row<F16>(a, s, qr, h0 + e, lane);
+  } else {
+    constexpr int MINE = HEADS / CA_JOIN_WARPS;
+    float2 ml[MINE][2];
+    float4 o[MINE][2];
+#pragma unroll
+    for (int x = 0; x < MINE; ++x)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const CaParts &c = sh_parts[warp + x * CA_JOIN_WARPS][p];
+        if (c.n == 0) continue;
+        ml[x][p] = ld_prev2f(c.ml + c.first);
+        o[x][p] = ld_prev4f(c.o + c.first * 128 + lane * 4);
+      }
+#pragma unroll
+    for (int x = 0; x < MINE; ++x) {
+      const int e = warp + x * CA_JOIN_WARPS;
+      if (h0 + e >= a.H) break;
+      CaSum s;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const CaParts &c = sh_parts[e][p];
+        if (c.n == 0) continue;
+        s.add(ml[x][p], o[x][p]);
+        for (int k0 = 1; k0 < c.n; k0 += 4) {
+          float2 m4[4];
+          float4 o4[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const long long at = c.at(min(k0 + k, c.n - 1));
+            m4[k] = ld_prev2f(c.ml + at);
+            o4[k] = ld_prev4f(c.o + at * 128 + lane * 4);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k0 + k < c.n) s.add(m4[k], o4[k]);
+        }
+      }
+      ca_finish_row<F16>(a, s, qr, h0 + e, lane);
     }
   }
 }
