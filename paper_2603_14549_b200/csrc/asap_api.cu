@@ -799,7 +799,7 @@ asap_status asap_init(asap_ctx **ctx_out, int device, size_t max_total_tokens, i
   const size_t o_mpart = carve(Hc * T * sizeof(float));
   const size_t o_hnorm = carve(Bc * Hc * 2 * sizeof(float));
   const size_t o_kinv = carve(max_keep_rows * sizeof(float));
-  const size_t n_cnt = Bc + 4;
+  const size_t n_cnt = Bc + 6;
   const size_t o_cnt = carve(n_cnt * sizeof(unsigned int));
   const size_t o_role = carve(T * sizeof(int32_t));
   const size_t o_seg = carve((max_keep_rows + Bc) * sizeof(int32_t));

@@ -17,10 +17,10 @@ struct DeviceGuard {
 };
 
 size_t ca_smem_bytes(int n_seg) {
-  return CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES + CA_JOBS * CA_Q_BYTES + sizeof(CaBook) + (size_t)(n_seg + 1) * sizeof(int);
+  return CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES + CA_JOBS * CA_Q_BYTES + sizeof(CaBook) + (size_t)n_seg * sizeof(CaSeg) + (size_t)(n_seg + 1) * sizeof(int);
 }
 
-size_t ct_smem_bytes(int n_seg) { return CT_BOOK_OFF + sizeof(CtBook) + (size_t)(n_seg + 1) * sizeof(int); }
+size_t ct_smem_bytes(int n_seg) { return CT_BOOK_OFF + sizeof(CtBook) + (size_t)n_seg * sizeof(CaSeg) + (size_t)(n_seg + 1) * sizeof(int); }
 
 // Elements that [rows, heads, dim] with the given strides spans.
 long long span_of(long long rows, long long heads, long long dim, long long row, long long head) {
@@ -77,6 +77,8 @@ asap_status check_cache_attention(asap_ctx *ctx, const asap_cache_attention_args
 struct CaLayout {
   size_t bytes = 0;
   int blocks[2] = {0, 0};        // of the streaming and of the tile kernel; 0: nothing to launch
+  int pieces[2] = {0, 0};        // pieces of their work
+  int rec_rows = 0;
   bool too_large = false;
 };
 constexpr long long CA_MAX_NUMBERS = 1LL << 30;    // key tiles are numbered in 32 bits
@@ -96,13 +98,17 @@ CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint
                           (group_rows > S ? numbers(1, group_rows + (long long)TileWork::ROWS * p->n_groups, p->max_prefix, TileWork{}) : 0);
   l.blocks[0] = at_most(streamed, 2LL * ctx->num_sms);
   if (tiled > 0) l.blocks[1] = at_most(tiled, ctx->num_sms);
+  l.pieces[0] = at_most(streamed, 4LL * l.blocks[0]);
+  l.pieces[1] = l.blocks[1];
+  const long long group_max = group_rows > 0 ? (group_rows < S ? group_rows : S) : 0, own_max = own_rows < S ? own_rows : S;
+  l.rec_rows = (int)(group_max > own_max ? group_max : own_max);
   l.too_large = streamed > CA_MAX_NUMBERS || tiled > CA_MAX_NUMBERS;
   auto carve = [&](size_t bytes) {
     const size_t o = l.bytes;
     l.bytes = align_up(l.bytes + bytes, 256);
     return at + o;
   };
-  const size_t rec[2] = {(size_t)2 * l.blocks[0] * StreamWork::ROWS, (size_t)2 * l.blocks[1] * TileWork::ROWS};
+  const size_t rec[2] = {(size_t)2 * l.pieces[0] * l.rec_rows, (size_t)2 * l.pieces[1] * TileWork::ROWS};
   const long long own_off = p->n_groups ? ((long long)p->max_prefix + 127) / 128 * 128 : 0;
   const long long pitch = own_off + ((long long)p->max_len + 127) / 128 * 128;       // (a key tile is written whole)
   uint8_t *plan = carve((2 * (n_seg + 1) + 1) * 4), *rows = carve((size_t)p->n_q * sizeof(CaRow)), *rec_ml0 = carve(rec[0] * 8), *rec_ml1 = carve(rec[1] * 8),
@@ -115,7 +121,7 @@ CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint
     a->rec_o[0] = reinterpret_cast<float *>(rec_o0); a->rec_o[1] = reinterpret_cast<float *>(rec_o1);
     a->full_o = reinterpret_cast<float *>(full_o); a->lse2 = reinterpret_cast<float *>(lse2);
     a->logits = reinterpret_cast<float *>(logits); a->pitch = pitch; a->own_off = (int)own_off;
-    a->blocks[0] = l.blocks[0]; a->blocks[1] = l.blocks[1];
+    a->pieces[0] = l.pieces[0]; a->pieces[1] = l.pieces[1]; a->rec_rows = l.rec_rows;
   }
   return l;
 }
@@ -257,7 +263,7 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   a.q = static_cast<const uint16_t *>(p->q); a.v = static_cast<const uint16_t *>(p->v); a.kv_row = p->kv_row; a.kv_head = p->kv_head;
   a.out = static_cast<uint16_t *>(p->out); a.lse = p->lse; a.weights = p->weights;
   a.scale_log2 = 1.4426950408889634f * (p->scale > 0.f ? p->scale : 1.0f / sqrtf(128.f));
-  a.status = ctx->status; a.wait_limit = ctx->wait_limit;
+  a.status = ctx->status; a.wait_limit = ctx->wait_limit; a.work = ctx->cnt_work + 4;
   const bool f16 = p->dtype == ASAP_FP16;
   DeviceGuard guard(ctx->device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -279,11 +285,13 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
              dim3(p->n_q, (p->H + heads - 1) / heads), dim3(CA_JOIN_THREADS), 0, st, a);
   ASAP_TRY(after_launch(ctx, "cache_join"));
   if (p->weights) {
-    const long long pre = (p->max_prefix + CA_WEIGHT_KEYS - 1) / CA_WEIGHT_KEYS, own = (p->max_len + CA_WEIGHT_KEYS - 1) / CA_WEIGHT_KEYS;
+    const int own_lanes = (long long)p->max_q * p->H <= 64 ? 64 : 16, pre_lanes = 16;
+    const long long pre = (p->max_prefix + 4 * pre_lanes - 1) / (4 * pre_lanes), own = (p->max_len + 4 * own_lanes - 1) / (4 * own_lanes);
     const long long blocks = pre * p->n_groups + own * p->B;
     if (blocks > 0) {
       mark(ctx, "cache_weight", st);
-      launch_pdl(ca_weight_kernel, dim3((unsigned)blocks), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)(pre > 0 ? pre : 1), (int)(own > 0 ? own : 1));
+      launch_pdl(ca_weight_kernel, dim3((unsigned)blocks), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)(pre > 0 ? pre : 1), pre_lanes,
+                 (int)(own > 0 ? own : 1), own_lanes);
       ASAP_TRY(after_launch(ctx, "cache_weight"));
     }
   }

@@ -13,6 +13,8 @@
 #include <cuda_fp16.h>
 #include <limits.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace asap {
@@ -161,11 +163,11 @@ rope_kernel(const __grid_constant__ RopeArgs a) {
 // rows of its sequences, segment G + b the own rows of sequence b.  Per key / value head the R = (query rows) * (H / kv_heads)
 // stacked rows of a segment are cut into row tiles, the keys that a row tile admits into key tiles.  Segments of up to 16 stacked rows
 // are streamed (ca_stream_kernel), the others go to the tensor cores as tiles of 128 rows, two side by side (ca_tile_kernel).  Each of
-// the two kernels numbers its key tiles through (all row tiles, heads and segments) and gives every block an equal range of numbers:
-// lengths may be as ragged as they like, and the host needs to know none of them.  A row tile whose key tiles lie in one block is
-// complete there; otherwise each block leaves a partial result (maximum, sum, weighted values) and the join adds them up in order.
-// Every row tile counts EXTRA numbers more than it has key tiles, for its queries and its result: blocks of many short row tiles
-// and blocks of few long ones are then done at the same time.
+// the two kernels numbers its key tiles through (all row tiles, heads and segments) and cuts the numbers into equal pieces: lengths may be
+// as ragged as they like, and the host needs to know none of them.  A row tile whose key tiles lie in one piece is complete
+// there; otherwise each piece leaves a partial result (maximum, sum, weighted values) and the join adds them up in order.
+// Every row tile counts EXTRA numbers more than it has key tiles, for its queries and its result: pieces of many short row tiles
+// and pieces of few long ones then take the same time.  A block's first piece is its own number, further ones are drawn.
 struct StreamWork {
   static constexpr int ROWS = 16, KEYS = 64, EXTRA = 2, INDEX = 0;
 };
@@ -181,7 +183,7 @@ constexpr int CA_JOIN_BYTES = 4 * 4 * 64 * 4;             // the warps' sums of 
 constexpr int CA_JOBS = 2;                                // items announced ahead
 constexpr int CA_Q_PITCH = 272;                           // a query row of 256 bytes; eight rows side by side meet all banks
 constexpr int CA_Q_BYTES = StreamWork::ROWS * CA_Q_PITCH;
-constexpr int CA_MAX_SEGMENTS = 1024;
+constexpr int CA_MAX_SEGMENTS = 928;
 constexpr long long CA_WAIT_LIMIT = 2000000000LL;
 
 // What the join has to know of a query row: its place in the prefix's and in its own segment.
@@ -209,9 +211,11 @@ struct CacheArgs {
   // scratch
   int *plan;                               // [2][n_seg + 1] first number of every segment, streamed and tiled; the last entry: all of them.  Behind
                                            // them 0 if the call is skipped
-  int blocks[2];                           // of the two kernels
+  int pieces[2];                           // pieces of the two kernels' work; 0: the kernel is not launched
+  unsigned int *work;                      // [2] pieces drawn / blocks done; both zero between launches
+  int rec_rows;                            // rows of a streamed piece's partial result
   CaRow *rows;                             // [n_q]
-  float2 *rec_ml[2], *full_ml;             // partial results: two per block and row of a row tile; [2][n_q * H] (prefix, own) complete ones
+  float2 *rec_ml[2], *full_ml;             // partial results: two per piece and row of a row tile; [2][n_q * H] (prefix, own) complete ones
   float *rec_o[2], *full_o;                // 128 values each
   float *lse2;                             // [n_q * H] log2 of a row's sum of 2^x; +inf: the row adds no weight
   float *logits;                           // [n_q * H, pitch] x = scale * log2(e) * q.k; prefix keys first, own keys from own_off on
@@ -221,44 +225,39 @@ struct CacheArgs {
   long long wait_limit;
 };
 
-struct CaSeg {
+struct __align__(16) CaSeg {
   int q0, nq;          // query rows
-  int row0, keys;      // cache rows
-  int causal;          // own rows
-  bool valid;
+  int row0, keys;      // cache rows; keys < 0: the segment failed validation
 };
-
 __device__ __forceinline__ int ca_qcu(const CacheArgs &a, int b) { return a.q_cu ? ld_prev(a.q_cu + b) : b; }
 
-__device__ __forceinline__ CaSeg ca_segment(const CacheArgs &a, int s) {
+// Segment s as the caller's arrays have it.  `broken`: the offsets of its query rows, or of a group's sequences, do not ascend within
+// their bounds; segments of other sequences may then overlap this one's, and the whole call is skipped.
+__device__ __forceinline__ CaSeg ca_segment(const CacheArgs &a, int s, bool &broken) {
   CaSeg g;
+  bool valid;
   if (s < a.G) {
     const int b0 = ld_prev(a.group_cu + s), b1 = ld_prev(a.group_cu + s + 1);
     g.row0 = ld_prev(a.prefix_start + s); g.keys = ld_prev(a.prefix_len + s);
-    g.causal = 0;
-    g.valid = b0 >= 0 && b0 <= b1 && b1 <= a.B && g.keys <= a.max_prefix;
-    g.q0 = g.valid ? ca_qcu(a, b0) : 0;
-    g.nq = g.valid ? ca_qcu(a, b1) - g.q0 : 0;
-    g.valid = g.valid && (long long)g.nq <= (long long)(b1 - b0) * a.max_q;
+    broken = b0 < 0 || b0 > b1 || b1 > a.B;
+    valid = !broken && g.keys <= a.max_prefix;
+    g.q0 = broken ? 0 : ca_qcu(a, b0);
+    g.nq = broken ? 0 : ca_qcu(a, b1) - g.q0;
+    valid = valid && (long long)g.nq <= (long long)(b1 - b0) * a.max_q;
   } else {
     const int b = s - a.G;
     g.row0 = ld_prev(a.start + b); g.keys = ld_prev(a.len + b);
-    g.q0 = ca_qcu(a, b); g.nq = ca_qcu(a, b + 1) - g.q0;
-    g.causal = 1;
-    g.valid = g.keys <= a.max_len && g.nq <= a.max_q;
+    const int q0 = ca_qcu(a, b), q1 = ca_qcu(a, b + 1);
+    broken = q0 < 0 || q0 > q1 || q1 > a.n_q;
+    g.q0 = q0; g.nq = broken ? 0 : q1 - q0;
+    valid = g.keys <= a.max_len && g.nq <= a.max_q;
   }
-  g.valid = g.valid && g.keys >= 0 && g.row0 >= 0 && (long long)g.row0 + g.keys <= a.cache_rows && g.q0 >= 0 && g.nq >= 0 &&
-            g.q0 <= a.n_q && (long long)g.q0 + g.nq <= a.n_q;
-  if (!g.valid) g.nq = g.keys = 0;
+  valid = valid && !broken && g.keys >= 0 && g.row0 >= 0 && (long long)g.row0 + g.keys <= a.cache_rows && g.q0 >= 0 && g.nq >= 0 &&
+          g.q0 <= a.n_q && (long long)g.q0 + g.nq <= a.n_q;
+  if (!valid) g.keys = -1;
   return g;
 }
-// The offsets of a sequence's query rows, or of a group's sequences, do not ascend within their bounds.  Segments of other sequences may
-// then overlap this one's: the whole call is skipped.
-__device__ __forceinline__ bool ca_broken(const CacheArgs &a, int s) {
-  const int x0 = s < a.G ? ld_prev(a.group_cu + s) : ca_qcu(a, s - a.G), x1 = s < a.G ? ld_prev(a.group_cu + s + 1) : ca_qcu(a, s - a.G + 1);
-  return x0 < 0 || x1 < x0 || x1 > (s < a.G ? a.B : a.n_q);
-}
-// group of a sequence: -1 none, -2 one that failed validation
+// group of a sequence: -1 none
 __device__ __forceinline__ int ca_group(const CacheArgs &a, int b) {
   int lo = 0, hi = a.G;                    // the last g with group_cu[g] <= b
   if (a.G == 0 || ld_prev(a.group_cu) > b) return -1;
@@ -267,8 +266,7 @@ __device__ __forceinline__ int ca_group(const CacheArgs &a, int b) {
     if (ld_prev(a.group_cu + mid) <= b) lo = mid;
     else hi = mid;
   }
-  if (b >= ld_prev(a.group_cu + lo + 1)) return -1;
-  return ca_segment(a, lo).valid ? lo : -2;
+  return b < ld_prev(a.group_cu + lo + 1) ? lo : -1;
 }
 // Stacked row i admits the first adm0 + i / rep own keys (causal), or all of them.
 __device__ __forceinline__ int ca_admitted(int keys, int adm0, int causal, int t) { return causal ? max(0, min(keys, adm0 + t)) : keys; }
@@ -291,8 +289,9 @@ __device__ __forceinline__ int ca_numbers(int R, int keys, int adm0, int causal,
   return t;
 }
 template <typename WORK>
-__device__ __forceinline__ int ca_row_tiles(int R) {
-  return ca_streamed(R) == (WORK::INDEX == 0) ? (R + WORK::ROWS - 1) / WORK::ROWS : 0;
+__device__ __forceinline__ int ca_row_tiles(const CaSeg &g, int rep) {
+  const int R = g.nq * rep;
+  return g.keys > 0 && ca_streamed(R) == (WORK::INDEX == 0) ? (R + WORK::ROWS - 1) / WORK::ROWS : 0;
 }
 
 // An item of a block's work: a range of key tiles of one row tile.
@@ -306,16 +305,21 @@ struct __align__(16) CaJob {
 };
 __device__ __forceinline__ int ca_admitted(const CaJob &j, int t) { return ca_admitted(j.keys, j.adm0, j.causal, t); }
 
-// Walks the numbers [t, end) of a block.
+// Walks the numbers [t, end) of a piece.
 template <typename WORK>
 struct CaWalk {
-  int t, end, begin_t;
+  int t, end, begin_t, piece;
   int seg, head, rt, pos;  // pos: numbers of the row tile that lie before t
-  int R;
+  int R, causal;
   CaSeg g;
-  __device__ __forceinline__ int key_tiles(const CacheArgs &a) const { return ca_key_tiles<WORK>(R, g.keys, g.keys - g.nq + 1, g.causal, a.rep, rt); }
-  __device__ __forceinline__ void begin(const CacheArgs &a, const int *off, int n_seg, int t0, int t1) {
-    t = begin_t = t0; end = t1;
+  __device__ __forceinline__ int key_tiles(const CacheArgs &a) const { return ca_key_tiles<WORK>(R, g.keys, g.keys - g.nq + 1, causal, a.rep, rt); }
+  __device__ __forceinline__ void enter(const CacheArgs &a, const CaSeg *segs) {
+    g = segs[seg];
+    R = g.nq * a.rep;
+    causal = seg >= a.G;
+  }
+  __device__ __forceinline__ void begin(const CacheArgs &a, const int *off, const CaSeg *segs, int n_seg, int number, int t0, int t1) {
+    t = begin_t = t0; end = t1; piece = number;
     if (t >= end) return;
     int lo = 0, hi = n_seg;                // off[lo] <= t < off[hi]
     while (hi - lo > 1) {
@@ -324,8 +328,7 @@ struct CaWalk {
       else hi = mid;
     }
     seg = lo;
-    g = ca_segment(a, seg);
-    R = g.nq * a.rep;
+    enter(a, segs);
     const int per_head = (off[seg + 1] - off[seg]) / a.kv;
     int u = t - off[seg];
     head = u / per_head;
@@ -338,23 +341,22 @@ struct CaWalk {
     pos = u;
   }
   // the next item that has key tiles; false: none is left
-  __device__ __forceinline__ bool next(const CacheArgs &a, const int *off, CaJob &j) {
+  __device__ __forceinline__ bool next(const CacheArgs &a, const int *off, const CaSeg *segs, CaJob &j) {
     while (t < end) {
       const int kt = key_tiles(a), p1 = min(kt + WORK::EXTRA, pos + (end - t));
       const int k0 = max(0, pos - WORK::EXTRA), k1 = p1 - WORK::EXTRA, first = t - pos + WORK::EXTRA;
-      j.q0 = g.q0; j.R = R; j.row0 = g.row0; j.keys = g.keys; j.adm0 = g.keys - g.nq + 1; j.causal = g.causal; j.head = head; j.rt = rt;
-      j.kt0 = k0; j.n = k1 - k0; j.complete = k0 == 0 && k1 == kt; j.record = 2 * blockIdx.x + (first <= begin_t ? 0 : 1);
+      j.q0 = g.q0; j.R = R; j.row0 = g.row0; j.keys = g.keys; j.adm0 = g.keys - g.nq + 1; j.causal = causal; j.head = head; j.rt = rt;
+      j.kt0 = k0; j.n = k1 - k0; j.complete = k0 == 0 && k1 == kt; j.record = 2 * piece + (first <= begin_t ? 0 : 1);
       t += p1 - pos;
       if (t < end) {                       // the next row tile that has keys
         pos = 0;
         do {
-          if (++rt >= ca_row_tiles<WORK>(R)) {
+          if (++rt >= ca_row_tiles<WORK>(g, a.rep)) {
             rt = 0;
             if (++head >= a.kv) {
               head = 0;
               do ++seg; while (off[seg + 1] <= t);
-              g = ca_segment(a, seg);
-              R = g.nq * a.rep;
+              enter(a, segs);
             }
           }
         } while (key_tiles(a) == 0);
@@ -365,20 +367,24 @@ struct CaWalk {
   }
 };
 
-// First number of every segment into off[0 .. n_seg] (shared memory); all threads of the block.  True if the call is to be skipped.
+// Segments into segs[0 .. n_seg) and the first number of each into off[0 .. n_seg] (shared memory); all threads of the block.  True if the
+// call is to be skipped.
 template <typename WORK, int THREADS>
-__device__ __forceinline__ bool ca_plan(const CacheArgs &a, int *off, int n_seg, int *warp_part) {
+__device__ __forceinline__ bool ca_plan(const CacheArgs &a, int *off, CaSeg *segs, int n_seg, int *warp_part) {
   const int per = (n_seg + THREADS - 1) / THREADS, s0 = min(n_seg, (int)threadIdx.x * per), s1 = min(n_seg, s0 + per);
   int mine = 0;
-  bool broken = (*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) != 0;
+  bool broken = (*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) != 0, bad = false;
   for (int s = s0; s < s1; ++s) {
-    broken = broken || ca_broken(a, s);
-    const CaSeg g = ca_segment(a, s);
-    const int R = g.nq * a.rep, n = a.kv * ca_numbers<WORK>(R, g.keys, g.keys - g.nq + 1, g.causal, a.rep, ca_row_tiles<WORK>(R));
+    bool b;
+    const CaSeg g = ca_segment(a, s, b);
+    broken |= b;
+    bad |= g.keys < 0;
+    const int n = a.kv * ca_numbers<WORK>(g.nq * a.rep, g.keys, g.keys - g.nq + 1, s >= a.G, a.rep, ca_row_tiles<WORK>(g, a.rep));
+    segs[s] = g;
     off[s + 1] = n;
     mine += n;
-    if (WORK::INDEX == 0 && !g.valid && blockIdx.x == 0) atomicOr(a.status, (uint32_t)STATUS_BAD_SAMPLE);
   }
+  if (WORK::INDEX == 0 && bad && blockIdx.x == 0) atomicOr(a.status, (uint32_t)STATUS_BAD_SAMPLE);
   int scan = mine;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -402,7 +408,7 @@ __device__ __forceinline__ bool ca_plan(const CacheArgs &a, int *off, int n_seg,
   }
   return broken;
 }
-__device__ __forceinline__ int ca_chunk(int all, int blocks) { return max(1, (all + blocks - 1) / blocks); }
+__device__ __forceinline__ int ca_chunk(int all, int pieces) { return max(1, (all + pieces - 1) / pieces); }
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -447,43 +453,55 @@ struct CaBook {
   uint64_t full[CA_STAGES], empty[CA_STAGES], job_full[CA_JOBS], job_empty[CA_JOBS];
   int warp_part[8];
   int abort_flag;
-  float2 ml[CA_CONSUMERS][StreamWork::ROWS];
+  float2 ml[2][StreamWork::ROWS];
   CaJob job[CA_JOBS];
 };
 
 // The entries of the query rows, for the join: a block takes every gridDim.x-th sequence.
-__device__ __forceinline__ void ca_describe_rows(const CacheArgs &a, const int *off, int n_seg, int thread, int threads) {
+__device__ __forceinline__ void ca_describe_rows(const CacheArgs &a, const int *off, const CaSeg *segs, int n_seg, int thread, int threads) {
   for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-    const CaSeg own = ca_segment(a, a.G + b);
-    const int grp = ca_group(a, b), q0 = ca_qcu(a, b), nq = ca_qcu(a, b + 1) - q0;
+    const CaSeg own = segs[a.G + b];
+    const int grp = ca_group(a, b);
     CaRow row;
-    row.valid = own.valid && grp >= -1;
+    row.valid = own.keys >= 0 && (grp < 0 || segs[grp].keys >= 0);
     row.pad = 0;
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const int s = p == 0 ? grp : a.G + b;
       CaRowPart &part = row.part[p];
-      part.R = 0;
-      part.i0 = part.adm0 = part.causal = part.keys = part.off = part.per_head = 0;
+      part.i0 = part.R = part.adm0 = part.causal = part.keys = part.off = part.per_head = 0;
       if (s < 0 || !row.valid) continue;
-      const CaSeg g = p == 0 ? ca_segment(a, s) : own;
-      const int R = g.nq * a.rep;
+      const CaSeg g = segs[s];
       if (g.keys == 0) continue;
+      const int R = g.nq * a.rep;
       int o0 = off[s], o1 = off[s + 1];
       if (!ca_streamed(R)) {
         o0 = ld_prev(a.plan + n_seg + 1 + s);
         o1 = ld_prev(a.plan + n_seg + 2 + s);
       }
-      part.R = R; part.i0 = (own.q0 - g.q0) * a.rep; part.keys = g.keys; part.adm0 = g.keys - g.nq + 1; part.causal = g.causal;
+      part.R = R; part.i0 = (own.q0 - g.q0) * a.rep; part.keys = g.keys; part.adm0 = g.keys - g.nq + 1; part.causal = p;
       part.off = o0; part.per_head = (o1 - o0) / a.kv;
     }
-    for (int r = thread; r < nq; r += threads) {
+    for (int r = thread; r < own.nq; r += threads) {
       CaRow mine = row;
       mine.part[0].i0 += r * a.rep;
       mine.part[1].i0 += r * a.rep;
-      a.rows[q0 + r] = mine;
+      a.rows[own.q0 + r] = mine;
     }
   }
+}
+
+// Named barriers of two warps: one arrives, the other waits.
+__device__ __forceinline__ void pair_arrive(int id) { asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+
+// One (maximum, sum, values) of a fragment row and another one: factors of both.
+__device__ __forceinline__ void ca_merge(float &m, float &l, float2 other, float &f, float &g) {
+  const float top = fmaxf(m, other.x);
+  f = m == -INFINITY ? 0.f : fast_exp2(m - top);
+  g = other.x == -INFINITY ? 0.f : fast_exp2(other.x - top);
+  l = (m == -INFINITY ? 0.f : l * f) + (other.x == -INFINITY ? 0.f : other.y * g);
+  m = top;
 }
 
 template <bool F16>
@@ -494,8 +512,9 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   float *join = reinterpret_cast<float *>(ca_smem + CA_STAGES * CA_STAGE_BYTES);
   const uint32_t base = smem_u32(ca_smem), q_smem = base + CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES;
   CaBook *bk = reinterpret_cast<CaBook *>(ca_smem + CA_STAGES * CA_STAGE_BYTES + CA_JOIN_BYTES + CA_JOBS * CA_Q_BYTES);
-  int *off = reinterpret_cast<int *>(bk + 1);
   const int n_seg = a.G + a.B;
+  CaSeg *segs = reinterpret_cast<CaSeg *>(bk + 1);
+  int *off = reinterpret_cast<int *>(segs + n_seg);
   if (threadIdx.x == 0) {
     for (int s = 0; s < CA_STAGES; ++s) {
       mbar_init(smem_u32(&bk->full[s]), 1);
@@ -512,22 +531,35 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
   }
   __syncthreads();
   WaitCtx wc{&bk->abort_flag, a.status, STATUS_CACHE_TIMEOUT, a.wait_limit};
-  pdl_enter();
-  const bool stop = ca_plan<StreamWork, CA_THREADS>(a, off, n_seg, bk->warp_part);
+  // Behind the tile kernel of the same call: nothing but that kernel's plan is needed from it, and its blocks have all waited for what
+  // precedes the call before this kernel can start.  So this one fills the processors that it leaves, and waits for its end at its own.
+  const bool behind = a.pieces[1] != 0;
+  if (behind) pdl_trigger();
+  else pdl_enter();
+  const bool stop = ca_plan<StreamWork, CA_THREADS>(a, off, segs, n_seg, bk->warp_part);
 
   if (warp == CA_CONSUMERS) {
     // ------------------------------------------------------------------ items, query rows, key and value tiles
     // (the whole warp walks the loop and stays converged)
-    const int all = off[n_seg], chunk = ca_chunk(all, gridDim.x);
+    const int all = stop ? 0 : off[n_seg], chunk = ca_chunk(all, a.pieces[0]), pieces = (all + chunk - 1) / chunk;
     CaWalk<StreamWork> walk;
-    walk.begin(a, off, n_seg, stop ? 0 : min(all, (int)blockIdx.x * chunk), stop ? 0 : min(all, ((int)blockIdx.x + 1) * chunk));
+    int piece = blockIdx.x;
+    walk.begin(a, off, segs, n_seg, piece, min(all, piece * chunk), min(all, (piece + 1) * chunk));
     const uint32_t leader = warp_leader();
     RingPos pos;
     int issued = 0, used = 0;
     CaJob j;
     for (int jc = 0;; ++jc) {
       const int slot = jc % CA_JOBS;
-      const bool more = walk.next(a, off, j);
+      bool more = walk.next(a, off, segs, j);
+      while (!more && pieces > (int)gridDim.x && piece < pieces) {       // the next piece (drawn: memory does not serve all blocks alike)
+        unsigned int drawn = 0u;
+        if (lane == 0) drawn = atomicAdd(a.work, 1u);
+        piece = (int)gridDim.x + (int)__shfl_sync(0xffffffffu, drawn, 0);
+        if (piece >= pieces) break;
+        walk.begin(a, off, segs, n_seg, piece, piece * chunk, min(all, (piece + 1) * chunk));
+        more = walk.next(a, off, segs, j);
+      }
       if (!more) j.n = -1;
       // The queue of items keeps working after an abort (its waits ignore the flag and are bounded on their own): all consumers must
       // see the same sequence, ending with -1.
@@ -568,14 +600,22 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       const int fills = issued > s ? (issued - s + CA_STAGES - 1) / CA_STAGES : 0;
       if (fills > 0) mbar_wait_drain(smem_u32(&bk->full[s]), (fills - 1) & 1, CA_WAIT_LIMIT);
     }
+    // the block that leaves last puts the counters back to zero for the next launch (every block has drawn its last piece by then)
+    if (pieces > (int)gridDim.x && lane == 0 && atomicAdd(a.work + 1, 1u) == gridDim.x - 1) {
+      a.work[0] = 0u;
+      a.work[1] = 0u;
+      __threadfence();
+    }
+    if (behind) pdl_wait();
     __syncwarp();
     return;
   }
   // -------------------------------------------------------------------- consumers
-  if (!stop) ca_describe_rows(a, off, n_seg, threadIdx.x, 32 * CA_CONSUMERS);
+  if (!stop && !behind) ca_describe_rows(a, off, segs, n_seg, threadIdx.x, 32 * CA_CONSUMERS);
   const int gq = lane >> 2, tq = lane & 3;       // fragment row / column pair
   const int mi = lane >> 3, mr = lane & 7;       // matrix of an ldmatrix, row in it
   RingPos pos;
+  bool handed = false;                           // (warps 2 and 3) the buffer holds something that may not have been read yet
   for (int jc = 0;; ++jc) {
     const int slot = jc % CA_JOBS;
     const bool got = mbar_wait_drain(smem_u32(&bk->job_full[slot]), (jc / CA_JOBS) & 1, CA_WAIT_LIMIT);
@@ -717,66 +757,89 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       mbar_arrive_lane0(smem_u32(&bk->empty[pos.slot]), lane);
       pos.step(CA_STAGES);
     }
-    // ---- the four warps' sums of the item
+    // ---- the four warps' sums of the item: 2 -> 0 and 3 -> 1, then 1 -> 0, which stores.  Values stay in fragment order, and the warps that
+    // hand theirs on go on to the next item.  (Through a buffer of whole rows that all four read, with a barrier of all four before and
+    // after each piece of it, an item's end took 3700 to 4700 clocks.)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
       l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
       if (l[e] != l[e] && m[e] == -INFINITY) m[e] = 0.f;      // every logit was NaN: not an empty row
-      if (tq == 0) bk->ml[warp][gq + 8 * e] = make_float2(m[e], l[e]);
     }
-    const int pad_rows = j.R <= 4 ? 4 : j.R <= 8 ? 8 : 16, width = 256 / pad_rows;    // columns a piece
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
-    float f[2];
+    const int rows8 = min(8, j.R), in_row = gq * 4 + tq;      // rows of the lower half; a lane's place among the values of eight columns
+    const bool writes = warp == 0 && !bk->abort_flag;
+    float *buf = join + (warp & 1) * (CA_JOIN_BYTES / 8);
+    float fac[2][4];                             // factors of both sums of either step
+    // Columns 8 N0 .. 8 N1 - 1 of the rows' half e; the maxima and sums go with the first.
+    auto pass = [&](auto n0, auto n1, int e) {
+      constexpr int N0 = decltype(n0)::value, N1 = decltype(n1)::value;
+      const int lim = e == 0 ? rows8 : j.R - 8, per = e == 0 ? rows8 : 8;     // rows in use, and rows of the buffer
+      const bool on = gq < lim;
+      auto put = [&]() {
+        if (N0 == 0 && tq == 0) bk->ml[warp & 1][gq + 8 * e] = make_float2(m[e], l[e]);
+        if (on)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float top = -INFINITY;
+          for (int n = N0; n < N1; ++n) *reinterpret_cast<float2 *>(buf + ((n - N0) * per * 4 + in_row) * 2) = make_float2(o[n][2 * e], o[n][2 * e + 1]);
+      };
+      auto get = [&](const float *from, float2 other, bool first, float &f, float &g) {
+        if (first) ca_merge(m[e], l[e], other, f, g);
+        if (on)
 #pragma unroll
-      for (int w = 0; w < CA_CONSUMERS; ++w) top = fmaxf(top, bk->ml[w][gq + 8 * e].x);
-      f[e] = m[e] == -INFINITY ? 0.f : fast_exp2(m[e] - top);
+          for (int n = N0; n < N1; ++n) {
+            const float2 v = *reinterpret_cast<const float2 *>(from + ((n - N0) * per * 4 + in_row) * 2);
+            o[n][2 * e] = (f == 0.f ? 0.f : o[n][2 * e] * f) + (g == 0.f ? 0.f : v.x * g);
+            o[n][2 * e + 1] = (f == 0.f ? 0.f : o[n][2 * e + 1] * f) + (g == 0.f ? 0.f : v.y * g);
+          }
+      };
+      if (warp >= 2) {
+        if (handed) pair_sync(4 + (warp & 1));   // the buffer has been read
+        handed = true;
+        put();
+        pair_arrive(1 + (warp & 1));
+        return;
+      }
+      pair_sync(1 + warp);
+      get(buf, bk->ml[warp][gq + 8 * e], N0 == 0, fac[e][0], fac[e][1]);
+      if (warp == 0) {
+        __syncwarp();
+        pair_arrive(4);
+        pair_sync(3);
+        get(join + CA_JOIN_BYTES / 8, bk->ml[1][gq + 8 * e], N0 == 0, fac[e][2], fac[e][3]);
+        __syncwarp();
+        pair_arrive(5);
+      } else {
+        __syncwarp();                            // (the warp's own buffer: warp 3's values are in registers)
+        put();
+        pair_arrive(3);
+      }
+    };
+    using std::integral_constant;
+    if (rows8 <= 4) {
+      pass(integral_constant<int, 0>{}, integral_constant<int, 16>{}, 0);
+    } else {
+      pass(integral_constant<int, 0>{}, integral_constant<int, 8>{}, 0);
+      pass(integral_constant<int, 8>{}, integral_constant<int, 16>{}, 0);
     }
-    // threads of a piece: a float4 each for the first 64
-    const int r = (threadIdx.x & 63) / (width / 4), c4 = (threadIdx.x & 63) % (width / 4) * 4;
-    float2 *ml = nullptr;
-    float *dst = nullptr;
-    if (r < j.R && threadIdx.x < 64 && !bk->abort_flag) {
-      const int t = r / a.rep;
-      const long long e = j.complete ? (j.causal ? (long long)a.n_q * a.H : 0) + (long long)(j.q0 + t) * a.H + j.head * a.rep + (r - t * a.rep)
-                                     : (long long)j.record * StreamWork::ROWS + r;
-      ml = (j.complete ? a.full_ml : a.rec_ml[0]) + e;
-      dst = (j.complete ? a.full_o : a.rec_o[0]) + e * 128;
-      if (c4 == 0) {
-        float top = -INFINITY, sum = 0.f;
+    if (upper) {
+      pass(integral_constant<int, 0>{}, integral_constant<int, 8>{}, 1);
+      pass(integral_constant<int, 8>{}, integral_constant<int, 16>{}, 1);
+    }
+    if (writes) {
 #pragma unroll
-        for (int w = 0; w < CA_CONSUMERS; ++w) top = fmaxf(top, bk->ml[w][r].x);
+      for (int e = 0; e < 2; ++e) {
+        if (entry[e] < 0) continue;
+        const long long at = j.complete ? (j.causal ? (long long)a.n_q * a.H : 0) + entry[e] : (long long)j.record * a.rec_rows + gq + 8 * e;
+        float *dst = (j.complete ? a.full_o : a.rec_o[0]) + at * 128 + 2 * tq;
 #pragma unroll
-        for (int w = 0; w < CA_CONSUMERS; ++w)
-          if (bk->ml[w][r].x != -INFINITY) sum += bk->ml[w][r].y * fast_exp2(bk->ml[w][r].x - top);
-        *ml = make_float2(top, sum);
+        for (int n = 0; n < 16; ++n) *reinterpret_cast<float2 *>(dst + 8 * n) = make_float2(o[n][2 * e], o[n][2 * e + 1]);
+        if (tq == 0) (j.complete ? a.full_ml : a.rec_ml[0])[at] = make_float2(m[e], l[e]);
       }
     }
-    for (int c0 = 0; c0 < 128; c0 += width) {
-#pragma unroll
-      for (int n = 0; n < 16; ++n) {
-        const int c = n * 8 + 2 * tq - c0;
-        if (c < 0 || c >= width) continue;
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (gq + 8 * e < pad_rows)
-            *reinterpret_cast<float2 *>(join + (warp * pad_rows + gq + 8 * e) * width + c) = make_float2(o[n][2 * e] * f[e], o[n][2 * e + 1] * f[e]);
-      }
-      asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
-      if (dst) {
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < CA_CONSUMERS; ++w) {
-          const float4 v = *reinterpret_cast<const float4 *>(join + (w * pad_rows + r) * width + c4);
-          s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-        *reinterpret_cast<float4 *>(dst + c0 + c4) = s;
-      }
-      asm volatile("bar.sync 1, %0;" ::"n"(32 * CA_CONSUMERS) : "memory");
-    }
+  }
+  if (handed) pair_sync(4 + (warp & 1));         // (every arrival is met)
+  if (behind) {
+    pdl_wait();
+    if (!stop) ca_describe_rows(a, off, segs, n_seg, threadIdx.x, 32 * CA_CONSUMERS);
   }
 }
 
@@ -819,8 +882,9 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t base = smem_u32(ct_smem), q_smem = base, ring = base + 2 * CT_TILE_BYTES;
   CtBook *bk = reinterpret_cast<CtBook *>(ct_smem + CT_BOOK_OFF);
-  int *off = reinterpret_cast<int *>(bk + 1);
   const int n_seg = a.G + a.B;
+  CaSeg *segs = reinterpret_cast<CaSeg *>(bk + 1);
+  int *off = reinterpret_cast<int *>(segs + n_seg);
   if (threadIdx.x == 0) {
     for (int s = 0; s < CT_JOBS; ++s) {
       mbar_init(smem_u32(&bk->job_full[s]), 1);
@@ -856,7 +920,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
   const uint32_t tmem_base = bk->tmem_base;
   WaitCtx wc{&bk->abort_flag, a.status, STATUS_CACHE_TIMEOUT, a.wait_limit};
   pdl_enter();
-  const bool stop = ca_plan<TileWork, CT_THREADS>(a, off, n_seg, bk->warp_part);
+  const bool stop = ca_plan<TileWork, CT_THREADS>(a, off, segs, n_seg, bk->warp_part);
   // the next item; false: there is none
   auto take = [&](int jc, CaJob &j) {
     const int slot = jc % CT_JOBS;
@@ -875,15 +939,15 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
     if (warp == 0) {
       // ---------------------------------------------------------------- items, key / value tiles
       const uint32_t leader = warp_leader();
-      const int all = off[n_seg], chunk = ca_chunk(all, gridDim.x);
+      const int all = stop ? 0 : off[n_seg], chunk = ca_chunk(all, a.pieces[1]);        // (a piece per block)
       CaWalk<TileWork> walk;
-      walk.begin(a, off, n_seg, stop ? 0 : min(all, (int)blockIdx.x * chunk), stop ? 0 : min(all, ((int)blockIdx.x + 1) * chunk));
+      walk.begin(a, off, segs, n_seg, blockIdx.x, min(all, (int)blockIdx.x * chunk), min(all, ((int)blockIdx.x + 1) * chunk));
       CaJob j;
       int tc = 0, issued = 0;
       uint32_t raw_any = 0u, raw_odd = 0u, raw_last = 0u;     // per ring slot: copies through `raw`: any, an odd number, the latest one
       for (int jc = 0;; ++jc) {
         const int slot = jc % CT_JOBS;
-        const bool more = walk.next(a, off, j);
+        const bool more = walk.next(a, off, segs, j);
         if (more) {
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
@@ -1314,16 +1378,16 @@ __device__ __forceinline__ CaParts ca_parts_of(const CacheArgs &a, const CaRowPa
   CaParts out;
   const int i = p.i0 + sub, rt = i / WORK::ROWS, r = i - rt * WORK::ROWS;
   const int kt = ca_key_tiles<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, rt);
-  const int chunk = ca_chunk(all, a.blocks[WORK::INDEX]);
+  const int chunk = ca_chunk(all, a.pieces[WORK::INDEX]), rec_rows = WORK::INDEX == 0 ? a.rec_rows : WORK::ROWS;
   const int first = p.off + kvh * p.per_head + ca_numbers<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, rt) + WORK::EXTRA;
   const int c0 = first / chunk, c1 = (first + kt - 1) / chunk;
   const bool complete = c0 == c1;
   out.n = kt == 0 ? 0 : c1 - c0 + 1;
-  out.step = 2 * WORK::ROWS;
+  out.step = 2 * rec_rows;
   out.ml = complete ? a.full_ml : a.rec_ml[WORK::INDEX];
   out.o = complete ? a.full_o : a.rec_o[WORK::INDEX];
-  out.first = complete ? (long long)which * a.n_q * a.H + entry : (long long)(2 * c0 + (first <= c0 * chunk ? 0 : 1)) * WORK::ROWS + r;
-  out.next = (long long)(2 * c0 + 2) * WORK::ROWS + r;
+  out.first = complete ? (long long)which * a.n_q * a.H + entry : (long long)(2 * c0 + (first <= c0 * chunk ? 0 : 1)) * rec_rows + r;
+  out.next = (long long)(2 * c0 + 2) * rec_rows + r;
   return out;
 }
 
@@ -1359,7 +1423,7 @@ ca_join_kernel(const __grid_constant__ CacheArgs a) {
     CaRowPart part;
     part.i0 = ld_prev(&src->i0); part.R = ld_prev(&src->R); part.adm0 = ld_prev(&src->adm0); part.causal = ld_prev(&src->causal);
     part.keys = ld_prev(&src->keys); part.off = ld_prev(&src->off); part.per_head = ld_prev(&src->per_head);
-    const int all0 = ld_prev(a.plan + n_seg), all1 = a.blocks[1] ? ld_prev(a.plan + 2 * n_seg + 1) : 0;
+    const int all0 = ld_prev(a.plan + n_seg), all1 = a.pieces[1] ? ld_prev(a.plan + 2 * n_seg + 1) : 0;
     CaParts mine;
     mine.n = 0;
     if (h < a.H && going && valid == 1 && qr >= q0 && qr < q1 && part.R > 0) {
@@ -1445,43 +1509,57 @@ ca_join_kernel(const __grid_constant__ CacheArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------
-// weights[j] += 1 / H * sum over the segment's query rows and heads of 2^(x - lse2).  A block per 128 keys of a segment, four of them a lane; the
-// warps share the (row, head) pairs and their sums are added in the order of the warps.
+// weights[j] += 1 / H * sum over the segment's query rows and heads of 2^(x - lse2).  A thread takes four keys; `lanes` threads side by side
+// on the keys, the others below them share the (row, head) pairs, and their sums are added in order.  Few pairs (own rows of single
+// tokens): 64 threads on 256 keys, 8 pairs a thread under way together; many: 16 on 64 keys.  (64 x 870 keys, 32 pairs: 9 us
+// against 24 with 64 keys a block; a prefix with 320 pairs and 2000 keys is the other way round.)
 // ---------------------------------------------------------------------------------------
-constexpr int CA_WEIGHT_THREADS = 512, CA_WEIGHT_KEYS = 128;
+constexpr int CA_WEIGHT_THREADS = 256;
 
 __global__ void __launch_bounds__(CA_WEIGHT_THREADS)
-ca_weight_kernel(const __grid_constant__ CacheArgs a, int prefix_blocks, int own_blocks) {
-  __shared__ float4 part[CA_WEIGHT_THREADS / 32][32];
+ca_weight_kernel(const __grid_constant__ CacheArgs a, int prefix_blocks, int prefix_lanes, int own_blocks, int own_lanes) {
+  __shared__ float4 part[CA_WEIGHT_THREADS];
   pdl_enter();
   const int n_pre = a.G * prefix_blocks;
   const int s = (int)blockIdx.x < n_pre ? blockIdx.x / prefix_blocks : a.G + (blockIdx.x - n_pre) / own_blocks;
   const int kb = (int)blockIdx.x < n_pre ? blockIdx.x % prefix_blocks : (blockIdx.x - n_pre) % own_blocks;
-  const CaSeg g = ca_segment(a, s);
-  if (!g.valid || kb * CA_WEIGHT_KEYS >= g.keys || ld_prev(a.plan + 2 * (a.G + a.B + 1)) == 0) return;
-  if (*reinterpret_cast<volatile uint32_t *>(a.status) & STATUS_CACHE_TIMEOUT) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = kb * CA_WEIGHT_KEYS + lane * 4;
-  const int n = g.nq * a.H, adm0 = g.keys - g.nq + 1;
-  const float *x = a.logits + (long long)g.q0 * a.H * a.pitch + (g.causal ? a.own_off : 0) + j;
+  const uint32_t status = *reinterpret_cast<volatile uint32_t *>(a.status);
+  const int going = ld_prev(a.plan + 2 * (a.G + a.B + 1));
+  bool broken;
+  const CaSeg g = ca_segment(a, s, broken);
+  const int lanes = s < a.G ? prefix_lanes : own_lanes, shares = CA_WEIGHT_THREADS / lanes, k0 = kb * lanes * 4;
+  if (k0 >= g.keys || going == 0 || (status & STATUS_CACHE_TIMEOUT)) return;
+  const int share = threadIdx.x / lanes, j = k0 + (threadIdx.x - share * lanes) * 4;
+  const int n = g.nq * a.H, adm0 = g.keys - g.nq + 1, causal = s >= a.G;
+  const float *x = a.logits + (long long)g.q0 * a.H * a.pitch + (causal ? a.own_off : 0) + j;
   const float *lse2 = a.lse2 + (long long)g.q0 * a.H;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int e = warp; e < n; e += CA_WEIGHT_THREADS / 32) {
-    const float l2 = ld_prev(lse2 + e);
-    const int lim = ca_admitted(g.keys, adm0, g.causal, e / a.H) - j;          // keys of the lane's four that the row admits
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (lim > 0) v = ld_prev4f(x + e * a.pitch);
-    const float w[4] = {v.x, v.y, v.z, v.w};
+  for (int e0 = share; e0 < n; e0 += 8 * shares) {
+    float l2[8];
+    float4 v[8];
+    int lim[8];                                  // keys of the thread's four that the row admits
 #pragma unroll
-    for (int c = 0; c < 4; ++c) sum[c] += c < lim && l2 != INFINITY ? fast_exp2(w[c] - l2) : 0.f;
+    for (int k = 0; k < 8; ++k) {
+      const int e = e0 + k * shares;
+      lim[k] = e < n ? ca_admitted(g.keys, adm0, causal, causal ? e / a.H : 0) - j : 0;
+      l2[k] = e < n ? ld_prev(lse2 + e) : INFINITY;
+      v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (lim[k] > 0) v[k] = ld_prev4f(x + e * a.pitch);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) sum[c] += c < lim[k] && l2[k] != INFINITY ? fast_exp2(w[c] - l2[k]) : 0.f;
+    }
   }
-  part[warp][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+  part[threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
   __syncthreads();
-  const int key = kb * CA_WEIGHT_KEYS + (int)threadIdx.x;
-  if (threadIdx.x < CA_WEIGHT_KEYS && key < g.keys) {
+  const int key = k0 + (int)threadIdx.x;
+  if ((int)threadIdx.x < lanes * 4 && key < g.keys) {
     float t = 0.f;
-#pragma unroll
-    for (int w = 0; w < CA_WEIGHT_THREADS / 32; ++w) t += reinterpret_cast<const float *>(part[w])[threadIdx.x];
+#pragma unroll 4
+    for (int w = 0; w < shares; ++w) t += reinterpret_cast<const float *>(part + w * lanes)[threadIdx.x];
     float *p = a.weights + g.row0 + key;
     *p = ld_prev(p) + t / (float)a.H;
   }
