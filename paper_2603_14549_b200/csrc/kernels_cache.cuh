@@ -179,7 +179,7 @@ constexpr int CA_THREADS = 32 * (CA_CONSUMERS + 1);       // and the copying war
 constexpr int CA_STAGES = 3;
 constexpr int CA_BLOCK_BYTES = StreamWork::KEYS * 128;    // 64 keys x 64 columns
 constexpr int CA_STAGE_BYTES = 4 * CA_BLOCK_BYTES;        // K and V
-constexpr int CA_JOIN_BYTES = 4 * 4 * 64 * 4;             // the warps' sums of an item, a piece at a time
+constexpr int CA_JOIN_BYTES = 4096;                       // the warps' sums of an item, a piece at a time
 constexpr int CA_JOBS = 2;                                // items announced ahead
 constexpr int CA_Q_PITCH = 272;                           // a query row of 256 bytes; eight rows side by side meet all banks
 constexpr int CA_Q_BYTES = StreamWork::ROWS * CA_Q_PITCH;
@@ -418,6 +418,12 @@ __device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+// The 8 x 8 matrix of 16-bit values whose row `lane / 4` holds this register's two in columns 2 (lane % 4) and the next, transposed.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
 template <bool F16>
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if constexpr (F16)
@@ -495,15 +501,20 @@ __device__ __forceinline__ void ca_describe_rows(const CacheArgs &a, const int *
 __device__ __forceinline__ void pair_arrive(int id) { asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
 __device__ __forceinline__ void pair_sync(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
-// One (maximum, sum, values) of a fragment row and another one: factors of both.
+// One (maximum, sum, values) of a query row and another one: factors of both.  (What has no maximum has sums of zero.)
 __device__ __forceinline__ void ca_merge(float &m, float &l, float2 other, float &f, float &g) {
   const float top = fmaxf(m, other.x);
   f = m == -INFINITY ? 0.f : fast_exp2(m - top);
   g = other.x == -INFINITY ? 0.f : fast_exp2(other.x - top);
-  l = (m == -INFINITY ? 0.f : l * f) + (other.x == -INFINITY ? 0.f : other.y * g);
+  l = l * f + other.y * g;
   m = top;
 }
 
+// What bounds it is the memory (5.9 to 6.2 TB/s while it runs).  S^T = K Q^T and O^T = V^T P^T, with the keys and then the columns as the 16 rows of an
+// m16n8k16 instruction and up to 8 query rows as its 8 columns: a tile of 64 keys takes half the instructions, and half the
+// accumulators, of the form with (mostly empty) 16 query rows.  Rows 8 .. 15, where there are any, are a second set of columns for the
+// same key and value fragments.  A warp's logits of 16 keys x 8 rows become the second product's operand by transposing two 8 x 8
+// matrices between the lanes.  Every warp keeps its own running maximum and sums; the four meet at an item's end.
 template <bool F16>
 __global__ void __launch_bounds__(CA_THREADS, 2)
 ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CacheArgs a) {
@@ -621,91 +632,117 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     const bool got = mbar_wait_drain(smem_u32(&bk->job_full[slot]), (jc / CA_JOBS) & 1, CA_WAIT_LIMIT);
     __syncwarp();
     const CaJob j = bk->job[slot];
-    uint32_t qa[8][4];
+    const bool two = j.R > 8;                    // rows 8 .. 15 are in use
+    uint32_t qb[2][8][2];                        // the query rows as the second operand, a k-step each; [rows 0 .. 7, 8 .. 15]
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) ldsm4(q_smem + slot * CA_Q_BYTES + ((mi & 1) * 8 + mr) * CA_Q_PITCH + (kk * 2 + (mi >> 1)) * 16, qa[kk]);
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int k2 = 0; k2 < 4; ++k2) {
+        uint32_t r[4];
+        ldsm4(q_smem + slot * CA_Q_BYTES + (h * 8 + mr) * CA_Q_PITCH + (k2 * 4 + mi) * 16, r);
+        qb[h][2 * k2][0] = r[0]; qb[h][2 * k2][1] = r[1];
+        qb[h][2 * k2 + 1][0] = r[2]; qb[h][2 * k2 + 1][1] = r[3];
+      }
     __syncwarp();
     mbar_arrive_lane0(smem_u32(&bk->job_empty[slot]), lane);
     if (!got || j.n < 0) break;
-    int adm[2];                                  // admitted keys of fragment rows gq, gq + 8 (rows past the last: none, whatever the buffer held)
-    long long entry[2];                          // (query row, head)
+    int adm[2][2];                               // admitted keys of query rows 8 h + 2 tq + e (rows past the last: none, whatever the buffer held)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int i = gq + 8 * e, t = i / a.rep;
-      adm[e] = i < j.R ? ca_admitted(j, t) : 0;
-      entry[e] = i < j.R ? (long long)(j.q0 + t) * a.H + j.head * a.rep + (i - t * a.rep) : -1;
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int i = 8 * h + 2 * tq + e;
+        adm[h][e] = i < j.R ? ca_admitted(j, i / a.rep) : 0;
+      }
+    // (query row, head) of row 8 h + 2 tq + e; -1: none
+    auto entry_of = [&](int h, int e) -> long long {
+      const int i = 8 * h + 2 * tq + e, t = i / a.rep;
+      return i < j.R ? (long long)(j.q0 + t) * a.H + j.head * a.rep + (i - t * a.rep) : -1;
+    };
+    float o[2][8][4];                            // [][16 columns][column gq or gq + 8, row 2 tq or 2 tq + 1]
+    float m[2][2], l[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int n = 0; n < 8; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[h][n][e] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) { m[h][e] = -INFINITY; l[h][e] = 0.f; }
     }
-    const bool upper = j.R > 8;                  // rows 8 .. 15 are in use
-    float o[16][4];
-#pragma unroll
-    for (int n = 0; n < 16; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     for (int kt = j.kt0; kt < j.kt0 + j.n; ++kt) {
       mbar_wait_warp(smem_u32(&bk->full[pos.slot]), pos.phase, wc);
       const uint32_t ks = base + pos.slot * CA_STAGE_BYTES, vs = ks + 2 * CA_BLOCK_BYTES;
       const int j0 = kt * StreamWork::KEYS + warp * 16;      // this warp's first key
-      // ---- logits of 16 rows x 16 keys
-      float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      // ---- logits of 16 keys x 8 rows: x[][2 c + e] is key gq + 8 c, row 2 tq + e
+      float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, y[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
       {
-        const int key = warp * 16 + (mi >> 1) * 8 + mr;
+        const int key = warp * 16 + (mi & 1) * 8 + mr;
+        const uint32_t row = ks + key * 128;
 #pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-          const int c = kk * 2 + (mi & 1);
-          uint32_t b[4];
-          ldsm4(ks + (c >> 3) * CA_BLOCK_BYTES + key * 128 + (((c & 7) ^ (key & 7)) << 4), b);
-          mma16816<F16>(x[0], qa[kk], b[0], b[1]);
-          mma16816<F16>(x[1], qa[kk], b[2], b[3]);
+        for (int kk = 0; kk < 8; ++kk) {         // (two chains)
+          const int c = kk * 2 + (mi >> 1);
+          uint32_t k[4];
+          ldsm4(row + (kk >> 2) * CA_BLOCK_BYTES + (((c & 7) ^ (key & 7)) << 4), k);
+          mma16816<F16>(kk & 1 ? y[0] : x[0], k, qb[0][kk][0], qb[0][kk][1]);
+          if (two) mma16816<F16>(kk & 1 ? y[1] : x[1], k, qb[1][kk][0], qb[1][kk][1]);
         }
       }
+      uint32_t p0[2] = {0u, 0u}, p1[2] = {0u, 0u};           // probabilities of keys gq and gq + 8, rows 2 tq and 2 tq + 1
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int h = 0; h < 2; ++h) {
+        if (h == 1 && !two) continue;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int key = j0 + n * 8 + 2 * tq + (e & 1);
-          x[n][e] = key < adm[e >> 1] ? x[n][e] * a.scale_log2 : -INFINITY;
+        for (int c = 0; c < 4; ++c) {
+          const int key = j0 + gq + 8 * (c >> 1);
+          x[h][c] = key < adm[h][c & 1] ? (x[h][c] + y[h][c]) * a.scale_log2 : -INFINITY;
         }
-      if (a.logits) {
+        if (a.logits) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const long long entry = entry_of(h, e);
+            if (entry < 0) continue;
+            float *row = a.logits + entry * a.pitch + (j.causal ? a.own_off : 0) + j0 + gq;
+            row[0] = x[h][e];
+            row[8] = x[h][2 + e];
+          }
+        }
+        // ---- probabilities relative to the running maximum
+        float mx[2], p[4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) mx[e] = fmaxf(x[h][e], x[h][2 + e]);
+#pragma unroll
+        for (int s = 4; s < 32; s <<= 1)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], s));
+        if (__any_sync(0xffffffffu, mx[0] > m[h][0] || mx[1] > m[h][1])) {
+          float f[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float top = fmaxf(m[h][e], mx[e]);
+            f[e] = top == m[h][e] ? 1.f : fast_exp2(m[h][e] - top);
+            m[h][e] = top;
+            l[h][e] *= f[e];
+          }
+#pragma unroll
+          for (int n = 0; n < 8; ++n) { o[h][n][0] *= f[0]; o[h][n][1] *= f[1]; o[h][n][2] *= f[0]; o[h][n][3] *= f[1]; }
+        }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          if (entry[e] < 0) continue;
-          float *row = a.logits + entry[e] * a.pitch + (j.causal ? a.own_off : 0);
-#pragma unroll
-          for (int n = 0; n < 2; ++n)
-            *reinterpret_cast<float2 *>(row + j0 + n * 8 + 2 * tq) = make_float2(x[n][2 * e], x[n][2 * e + 1]);
+          const float ref = m[h][e] == -INFINITY ? 0.f : m[h][e];
+          p[e] = fast_exp2(x[h][e] - ref);
+          p[2 + e] = fast_exp2(x[h][2 + e] - ref);
+          l[h][e] += p[e] + p[2 + e];
         }
-      }
-      // ---- probabilities relative to the running maximum
-      uint32_t pa[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if (e == 1 && !upper) continue;
-        float mx = fmaxf(fmaxf(x[0][2 * e], x[0][2 * e + 1]), fmaxf(x[1][2 * e], x[1][2 * e + 1]));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        const float m_new = fmaxf(m[e], mx), ref = m_new == -INFINITY ? 0.f : m_new;
-        if (__any_sync(0xffffffffu, m_new != m[e])) {
-          const float f = m_new == m[e] ? 1.f : fast_exp2(m[e] - ref);
-          l[e] *= f;
-#pragma unroll
-          for (int n = 0; n < 16; ++n) { o[n][2 * e] *= f; o[n][2 * e + 1] *= f; }
-          m[e] = m_new;
-        }
-        float p[2][2];
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) p[n][c] = fast_exp2(x[n][2 * e + c] - ref);
-        l[e] += (p[0][0] + p[0][1]) + (p[1][0] + p[1][1]);
-        pa[e] = pack2_t<F16>(p[0][0], p[0][1]);
-        pa[e + 2] = pack2_t<F16>(p[1][0], p[1][1]);
+        p0[h] = pack2_t<F16>(p[0], p[1]);
+        p1[h] = pack2_t<F16>(p[2], p[3]);
       }
       // ---- values.  Rows that no query row of the tile admits are cleared (0 * NaN is NaN).  A row that only some of them
       // admit may hold infinities or NaN too: then its part is added without the matrix instruction, to the rows that admit it.
       if (j0 + 16 > (j.causal ? j.adm0 : j.keys)) {
         const int r = lane >> 1, half = lane & 1;           // two lanes per key
         const bool dead = j0 + r >= j.keys;
+        const uint8_t *values = ca_smem + pos.slot * CA_STAGE_BYTES + 2 * CA_BLOCK_BYTES;
         uint8_t *vrow = ca_smem + pos.slot * CA_STAGE_BYTES + (2 + half) * CA_BLOCK_BYTES + (warp * 16 + r) * 128;
         uint32_t hit = 0u;
         if (!dead)
@@ -722,20 +759,21 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
 #pragma unroll
           for (int e = 0; e < 16; ++e) bad |= ((who >> (2 * e)) & 3u) ? 1u << e : 0u;
           for (uint32_t left = bad; left; left &= left - 1) {
-            const int r2 = __ffs(left) - 1;      // key
-            const int src = (lane & ~3) | ((r2 & 7) >> 1);
-            const uint32_t w0 = __shfl_sync(0xffffffffu, (r2 & 8) ? pa[2] : pa[0], src), w1 = __shfl_sync(0xffffffffu, (r2 & 8) ? pa[3] : pa[1], src);
-            const float2 u0 = unpack2_t<F16>(w0), u1 = unpack2_t<F16>(w1);
-            const float p0 = (r2 & 1) ? u0.y : u0.x, p1 = (r2 & 1) ? u1.y : u1.x;
-            const bool in0 = j0 + r2 < adm[0], in1 = j0 + r2 < adm[1];
+            const int k = __ffs(left) - 1, key = warp * 16 + k;
 #pragma unroll
-            for (int n = 0; n < 16; ++n) {
-              const int key = warp * 16 + r2;
-              const uint32_t w = *reinterpret_cast<const uint32_t *>(ca_smem + pos.slot * CA_STAGE_BYTES + (2 + (n >> 3)) * CA_BLOCK_BYTES +
-                                                                     key * 128 + (((n & 7) ^ (key & 7)) << 4) + tq * 4);
-              const float2 v = unpack2_t<F16>(w);
-              if (in0) { o[n][0] += p0 * v.x; o[n][1] += p0 * v.y; }
-              if (in1) { o[n][2] += p1 * v.x; o[n][3] += p1 * v.y; }
+            for (int h = 0; h < 2; ++h) {
+              const float2 pk = unpack2_t<F16>(__shfl_sync(0xffffffffu, (k & 8) ? p1[h] : p0[h], (k & 7) * 4 + tq));
+              const bool in0 = j0 + k < adm[h][0], in1 = j0 + k < adm[h][1];
+#pragma unroll
+              for (int n = 0; n < 8; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {    // column 16 n + 8 c + gq
+                  const int chunk = 2 * n + c;
+                  const uint16_t w = *reinterpret_cast<const uint16_t *>(values + (chunk >> 3) * CA_BLOCK_BYTES + key * 128 + (((chunk & 7) ^ (key & 7)) << 4) + 2 * gq);
+                  const float v = unpack2_t<F16>(w).x;
+                  if (in0) o[h][n][2 * c] += pk.x * v;
+                  if (in1) o[h][n][2 * c + 1] += pk.y * v;
+                }
             }
           }
           __syncwarp();
@@ -745,13 +783,20 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         }
         fence_proxy_async();                     // these writes come before the next copy into the slot
       }
+      uint32_t b0[2], b1[2];
 #pragma unroll
-      for (int dt = 0; dt < 8; ++dt) {
-        const int c = dt * 2 + (mi >> 1), key = warp * 16 + (mi & 1) * 8 + mr;
-        uint32_t b[4];
-        ldsm4t(vs + (c >> 3) * CA_BLOCK_BYTES + key * 128 + (((c & 7) ^ (key & 7)) << 4), b);
-        mma16816<F16>(o[2 * dt], pa, b[0], b[1]);
-        mma16816<F16>(o[2 * dt + 1], pa, b[2], b[3]);
+      for (int h = 0; h < 2; ++h) { b0[h] = transpose8x8(p0[h]); b1[h] = transpose8x8(p1[h]); }
+      {
+        const int key = warp * 16 + (mi >> 1) * 8 + mr;
+        const uint32_t row = vs + key * 128;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+          const int c = 2 * n + (mi & 1);
+          uint32_t v[4];
+          ldsm4t(row + (n >> 2) * CA_BLOCK_BYTES + (((c & 7) ^ (key & 7)) << 4), v);
+          mma16816<F16>(o[0][n], v, b0[0], b1[0]);
+          if (two) mma16816<F16>(o[1][n], v, b0[1], b1[1]);
+        }
       }
       __syncwarp();
       mbar_arrive_lane0(smem_u32(&bk->empty[pos.slot]), lane);
@@ -761,34 +806,42 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     // hand theirs on go on to the next item.  (Through a buffer of whole rows that all four read, with a barrier of all four before and
     // after each piece of it, an item's end took 3700 to 4700 clocks.)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
-      l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
-      if (l[e] != l[e] && m[e] == -INFINITY) m[e] = 0.f;      // every logit was NaN: not an empty row
-    }
-    const int rows8 = min(8, j.R), in_row = gq * 4 + tq;      // rows of the lower half; a lane's place among the values of eight columns
-    const bool writes = warp == 0 && !bk->abort_flag;
-    float *buf = join + (warp & 1) * (CA_JOIN_BYTES / 8);
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (h == 1 && !two) continue;
+#pragma unroll
+        for (int s = 4; s < 32; s <<= 1) l[h][e] += __shfl_xor_sync(0xffffffffu, l[h][e], s);
+        if (l[h][e] != l[h][e] && m[h][e] == -INFINITY) m[h][e] = 0.f;      // every logit was NaN: not an empty row
+      }
+    float4 *buf = reinterpret_cast<float4 *>(join) + (warp & 1) * (CA_JOIN_BYTES / 32);
+    // Columns 16 N0 .. 16 N1 - 1 of rows 8 h ..; the maxima and sums go with the first.
     float fac[2][4];                             // factors of both sums of either step
-    // Columns 8 N0 .. 8 N1 - 1 of the rows' half e; the maxima and sums go with the first.
-    auto pass = [&](auto n0, auto n1, int e) {
-      constexpr int N0 = decltype(n0)::value, N1 = decltype(n1)::value;
-      const int lim = e == 0 ? rows8 : j.R - 8, per = e == 0 ? rows8 : 8;     // rows in use, and rows of the buffer
-      const bool on = gq < lim;
+    auto pass = [&](auto n0, auto n1, auto hh) {
+      constexpr int N0 = decltype(n0)::value, N1 = decltype(n1)::value, h = decltype(hh)::value;
+      const int cols = (min(8, j.R - 8 * h) + 1) >> 1;       // values of tq in use
+      const bool on = tq < cols;
       auto put = [&]() {
-        if (N0 == 0 && tq == 0) bk->ml[warp & 1][gq + 8 * e] = make_float2(m[e], l[e]);
+        if (N0 == 0 && gq == 0) {
+          bk->ml[warp & 1][8 * h + 2 * tq] = make_float2(m[h][0], l[h][0]);
+          bk->ml[warp & 1][8 * h + 2 * tq + 1] = make_float2(m[h][1], l[h][1]);
+        }
         if (on)
 #pragma unroll
-          for (int n = N0; n < N1; ++n) *reinterpret_cast<float2 *>(buf + ((n - N0) * per * 4 + in_row) * 2) = make_float2(o[n][2 * e], o[n][2 * e + 1]);
+          for (int n = N0; n < N1; ++n) buf[((n - N0) * 8 + gq) * cols + tq] = make_float4(o[h][n][0], o[h][n][1], o[h][n][2], o[h][n][3]);
       };
-      auto get = [&](const float *from, float2 other, bool first, float &f, float &g) {
-        if (first) ca_merge(m[e], l[e], other, f, g);
+      auto get = [&](const float4 *from, const float2 *other, int step) {
+        if (N0 == 0)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) ca_merge(m[h][e], l[h][e], other[8 * h + 2 * tq + e], fac[e][2 * step], fac[e][2 * step + 1]);
         if (on)
 #pragma unroll
           for (int n = N0; n < N1; ++n) {
-            const float2 v = *reinterpret_cast<const float2 *>(from + ((n - N0) * per * 4 + in_row) * 2);
-            o[n][2 * e] = (f == 0.f ? 0.f : o[n][2 * e] * f) + (g == 0.f ? 0.f : v.x * g);
-            o[n][2 * e + 1] = (f == 0.f ? 0.f : o[n][2 * e + 1] * f) + (g == 0.f ? 0.f : v.y * g);
+            const float4 v = from[((n - N0) * 8 + gq) * cols + tq];
+            o[h][n][0] = o[h][n][0] * fac[0][2 * step] + v.x * fac[0][2 * step + 1];
+            o[h][n][1] = o[h][n][1] * fac[1][2 * step] + v.y * fac[1][2 * step + 1];
+            o[h][n][2] = o[h][n][2] * fac[0][2 * step] + v.z * fac[0][2 * step + 1];
+            o[h][n][3] = o[h][n][3] * fac[1][2 * step] + v.w * fac[1][2 * step + 1];
           }
       };
       if (warp >= 2) {
@@ -799,41 +852,50 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         return;
       }
       pair_sync(1 + warp);
-      get(buf, bk->ml[warp][gq + 8 * e], N0 == 0, fac[e][0], fac[e][1]);
+      get(buf, bk->ml[warp], 0);
+      __syncwarp();
       if (warp == 0) {
-        __syncwarp();
         pair_arrive(4);
         pair_sync(3);
-        get(join + CA_JOIN_BYTES / 8, bk->ml[1][gq + 8 * e], N0 == 0, fac[e][2], fac[e][3]);
+        get(reinterpret_cast<const float4 *>(join) + CA_JOIN_BYTES / 32, bk->ml[1], 1);
         __syncwarp();
         pair_arrive(5);
       } else {
-        __syncwarp();                            // (the warp's own buffer: warp 3's values are in registers)
-        put();
+        put();                                   // (the warp's own buffer: warp 3's values are in registers)
         pair_arrive(3);
       }
     };
     using std::integral_constant;
-    if (rows8 <= 4) {
-      pass(integral_constant<int, 0>{}, integral_constant<int, 16>{}, 0);
+    constexpr integral_constant<int, 0> c0{};
+    constexpr integral_constant<int, 1> c1{};
+    constexpr integral_constant<int, 4> c4{};
+    constexpr integral_constant<int, 8> c8{};
+    if (j.R <= 4) {
+      pass(c0, c8, c0);
     } else {
-      pass(integral_constant<int, 0>{}, integral_constant<int, 8>{}, 0);
-      pass(integral_constant<int, 8>{}, integral_constant<int, 16>{}, 0);
-    }
-    if (upper) {
-      pass(integral_constant<int, 0>{}, integral_constant<int, 8>{}, 1);
-      pass(integral_constant<int, 8>{}, integral_constant<int, 16>{}, 1);
-    }
-    if (writes) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if (entry[e] < 0) continue;
-        const long long at = j.complete ? (j.causal ? (long long)a.n_q * a.H : 0) + entry[e] : (long long)j.record * a.rec_rows + gq + 8 * e;
-        float *dst = (j.complete ? a.full_o : a.rec_o[0]) + at * 128 + 2 * tq;
-#pragma unroll
-        for (int n = 0; n < 16; ++n) *reinterpret_cast<float2 *>(dst + 8 * n) = make_float2(o[n][2 * e], o[n][2 * e + 1]);
-        if (tq == 0) (j.complete ? a.full_ml : a.rec_ml[0])[at] = make_float2(m[e], l[e]);
+      pass(c0, c4, c0);
+      pass(c4, c8, c0);
+      if (two) {
+        pass(c0, c4, c1);
+        pass(c4, c8, c1);
       }
+    }
+    if (warp == 0 && !bk->abort_flag) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const long long entry = entry_of(h, e);
+          if (entry < 0) continue;
+          const long long at = j.complete ? (j.causal ? (long long)a.n_q * a.H : 0) + entry : (long long)j.record * a.rec_rows + 8 * h + 2 * tq + e;
+          float *dst = (j.complete ? a.full_o : a.rec_o[0]) + at * 128 + gq;
+#pragma unroll
+          for (int n = 0; n < 8; ++n) {
+            dst[16 * n] = o[h][n][e];
+            dst[16 * n + 8] = o[h][n][2 + e];
+          }
+          if (gq == 0) (j.complete ? a.full_ml : a.rec_ml[0])[at] = make_float2(m[h][e], l[h][e]);
+        }
     }
   }
   if (handed) pair_sync(4 + (warp & 1));         // (every arrival is met)
