@@ -87,6 +87,7 @@ CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint
   const size_t entries = (size_t)p->n_q * p->H, n_seg = (size_t)p->B + p->n_groups;
   // no more blocks than there can be key tiles; no tile kernel where no segment can have more than 16 stacked rows
   const long long rep = p->H / p->kv_heads, heads = p->kv_heads, group_rows = p->n_groups > 0 && p->max_prefix > 0 ? p->n_q * rep : 0;
+  // (heads that go together count less than the same heads one by one)
   auto numbers = [&](long long segs, long long rows, long long keys, auto work) {
     using WORK = decltype(work);
     return segs * ((rows + WORK::ROWS - 1) / WORK::ROWS) * ((keys + WORK::KEYS - 1) / WORK::KEYS + WORK::EXTRA) * heads;
@@ -101,7 +102,8 @@ CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint
   l.pieces[0] = at_most(streamed, 4LL * l.blocks[0]);
   l.pieces[1] = l.blocks[1];
   const long long group_max = group_rows > 0 ? (group_rows < S ? group_rows : S) : 0, own_max = own_rows < S ? own_rows : S;
-  l.rec_rows = (int)(group_max > own_max ? group_max : own_max);
+  const long long rows_max = group_max > own_max ? group_max : own_max;
+  l.rec_rows = (int)(4 * rows_max < S ? 4 * rows_max : S);           // (as many heads together as make up to 16 rows)
   l.too_large = streamed > CA_MAX_NUMBERS || tiled > CA_MAX_NUMBERS;
   auto carve = [&](size_t bytes) {
     const size_t o = l.bytes;
@@ -126,13 +128,14 @@ CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint
   return l;
 }
 
-// Keys or values [rows, heads, 128] with any strides; box = 64 columns x 1 head x box_rows rows, 128-byte swizzle.
-bool make_cache_map(asap_ctx *ctx, CUtensorMap *map, const void *ptr, const asap_cache_attention_args *p, uint32_t box_rows) {
-  cuuint64_t dims[3] = {128, (cuuint64_t)p->kv_heads, (cuuint64_t)p->cache_rows};
-  cuuint64_t strides[2] = {(cuuint64_t)(p->kv_heads > 1 ? p->kv_head : 128) * 2, (cuuint64_t)(p->cache_rows > 1 ? p->kv_row : 128) * 2};
-  cuuint32_t box[3] = {64, 1, box_rows};
-  cuuint32_t estr[3] = {1, 1, 1};
-  return ctx->encode(map, p->dtype == ASAP_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr),
+// Keys or values [rows, heads, 128] with any strides, as four dimensions (64 columns, row, column half, head); box = 64 columns x box_rows rows x
+// both halves x `heads`, 128-byte swizzle: in shared memory the halves of every head are blocks of box_rows x 128 bytes.
+bool make_cache_map(asap_ctx *ctx, CUtensorMap *map, const void *ptr, const asap_cache_attention_args *p, uint32_t box_rows, uint32_t heads) {
+  cuuint64_t dims[4] = {64, (cuuint64_t)p->cache_rows, 2, (cuuint64_t)p->kv_heads};
+  cuuint64_t strides[3] = {(cuuint64_t)(p->cache_rows > 1 ? p->kv_row : 128) * 2, 128, (cuuint64_t)(p->kv_heads > 1 ? p->kv_head : 128) * 2};
+  cuuint32_t box[4] = {64, box_rows, 2, heads};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return ctx->encode(map, p->dtype == ASAP_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(ptr),
                      dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -250,12 +253,15 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   if (layout.too_large) return fail(ctx, ASAP_ERR_UNSUPPORTED, "asap_cache_attention: max_q, max_len, max_prefix and the batch are too large together");
   if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0 || scratch_bytes < layout.bytes)
     return fail(ctx, ASAP_ERR_WORKSPACE, "asap_cache_attention: scratch is null, not 256-byte aligned or smaller than asap_cache_attention_scratch_bytes");
-  CUtensorMap map_k[2], map_v[2];
-  for (int w = 0; w < 2; ++w) {
-    const uint32_t box = w == 0 ? StreamWork::KEYS : TileWork::KEYS;
-    if (layout.blocks[w] && (!make_cache_map(ctx, &map_k[w], p->k, p, box) || !make_cache_map(ctx, &map_v[w], p->v, p, box)))
-      return fail(ctx, ASAP_ERR_CUDA, "cuTensorMapEncodeTiled failed for k / v");
+  CaMaps maps;
+  CUtensorMap tile_k, tile_v;
+  bool made = true;
+  for (int b = 0; b < 3; ++b) {                  // (boxes of more heads than there are stand unused)
+    const uint32_t heads = p->kv_heads >= 1 << b ? 1u << b : 1u;
+    made = made && make_cache_map(ctx, &maps.k[b], p->k, p, StreamWork::KEYS / heads, heads) && make_cache_map(ctx, &maps.v[b], p->v, p, StreamWork::KEYS / heads, heads);
   }
+  if (layout.blocks[1]) made = made && make_cache_map(ctx, &tile_k, p->k, p, TileWork::KEYS, 1) && make_cache_map(ctx, &tile_v, p->v, p, TileWork::KEYS, 1);
+  if (!made) return fail(ctx, ASAP_ERR_CUDA, "cuTensorMapEncodeTiled failed for k / v");
   a.B = p->B; a.G = p->n_groups; a.H = p->H; a.kv = p->kv_heads; a.rep = p->H / p->kv_heads;
   a.n_q = p->n_q; a.max_q = p->max_q; a.max_len = p->max_len; a.max_prefix = p->max_prefix; a.cache_rows = p->cache_rows;
   a.q_row = p->q_row; a.q_head = p->q_head; a.out_row = p->out_row; a.out_head = p->out_head;
@@ -270,12 +276,12 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   if (layout.blocks[1]) {
     mark(ctx, "cache_tile", st);
     launch_pdl(f16 ? ca_tile_kernel<true> : ca_tile_kernel<false>, dim3(layout.blocks[1]), dim3(CT_THREADS), ct_smem_bytes(p->B + p->n_groups), st,
-               map_k[1], map_v[1], a);
+               tile_k, tile_v, a);
     ASAP_TRY(after_launch(ctx, "cache_tile"));
   }
   mark(ctx, "cache_stream", st);
   launch_pdl(f16 ? ca_stream_kernel<true> : ca_stream_kernel<false>, dim3(layout.blocks[0]), dim3(CA_THREADS), ca_smem_bytes(p->B + p->n_groups), st,
-             map_k[0], map_v[0], a);
+             maps, a);
   ASAP_TRY(after_launch(ctx, "cache_stream"));
   mark(ctx, "cache_join", st);
   // (one wave of the split form: 1 x 32 heads 14 -> 8 us, 5 rows of up to 150 partial results 17 -> 8; 128 rows 21 -> 62)

@@ -166,6 +166,8 @@ rope_kernel(const __grid_constant__ RopeArgs a) {
 // the two kernels numbers its key tiles through (all row tiles, heads and segments) and cuts the numbers into equal pieces: lengths may be
 // as ragged as they like, and the host needs to know none of them.  A row tile whose key tiles lie in one piece is complete
 // there; otherwise each piece leaves a partial result (maximum, sum, weighted values) and the join adds them up in order.
+// The streaming kernel takes four or two heads side by side where their rows are few: a tile is then 16 or 32 keys of each, so that short
+// segments waste little of their last tile, and fewer warps (or none) have to add up their sums.
 // Every row tile counts EXTRA numbers more than it has key tiles, for its queries and its result: pieces of many short row tiles
 // and pieces of few long ones then take the same time.  A block's first piece is its own number, further ones are drawn.
 struct StreamWork {
@@ -186,11 +188,14 @@ constexpr int CA_Q_BYTES = StreamWork::ROWS * CA_Q_PITCH;
 constexpr int CA_MAX_SEGMENTS = 928;
 constexpr long long CA_WAIT_LIMIT = 2000000000LL;
 
+// Key / value heads that the streaming kernel takes together for segments of R stacked rows: at most 16 rows in all.
+__host__ __device__ __forceinline__ int ca_heads(int R, int kv) { return R <= 4 && kv % 4 == 0 ? 4 : R <= 8 && kv % 2 == 0 ? 2 : 1; }
+
 // What the join has to know of a query row: its place in the prefix's and in its own segment.
 struct CaRowPart {
   int i0, R;               // stacked row of its first head, stacked rows of the segment (0: no keys there)
   int adm0, causal, keys;
-  int off, per_head;       // numbers of the segment and of one of its heads
+  int off, per_head;       // numbers of the segment and of one of its heads (or of the heads that go together)
 };
 struct CaRow {
   CaRowPart part[2];
@@ -213,7 +218,7 @@ struct CacheArgs {
                                            // them 0 if the call is skipped
   int pieces[2];                           // pieces of the two kernels' work; 0: the kernel is not launched
   unsigned int *work;                      // [2] pieces drawn / blocks done; both zero between launches
-  int rec_rows;                            // rows of a streamed piece's partial result
+  int rec_rows;                            // rows of a streamed piece's partial result, those of all heads that go together
   CaRow *rows;                             // [n_q]
   float2 *rec_ml[2], *full_ml;             // partial results: two per piece and row of a row tile; [2][n_q * H] (prefix, own) complete ones
   float *rec_o[2], *full_o;                // 128 values each
@@ -271,19 +276,21 @@ __device__ __forceinline__ int ca_group(const CacheArgs &a, int b) {
 // Stacked row i admits the first adm0 + i / rep own keys (causal), or all of them.
 __device__ __forceinline__ int ca_admitted(int keys, int adm0, int causal, int t) { return causal ? max(0, min(keys, adm0 + t)) : keys; }
 __device__ __forceinline__ bool ca_streamed(int R) { return R <= StreamWork::ROWS; }
-// key tiles of row tile rt
 template <typename WORK>
-__device__ __forceinline__ int ca_key_tiles(int R, int keys, int adm0, int causal, int rep, int rt) {
-  const int last = min((rt + 1) * WORK::ROWS, R) - 1;
-  return (ca_admitted(keys, adm0, causal, causal ? last / rep : 0) + WORK::KEYS - 1) / WORK::KEYS;
+__device__ __forceinline__ int ca_together(int R, int kv) { return WORK::INDEX == 0 ? ca_heads(R, kv) : 1; }
+// key tiles of row tile rt; `hg` heads go together
+template <typename WORK>
+__device__ __forceinline__ int ca_key_tiles(int R, int keys, int adm0, int causal, int rep, int hg, int rt) {
+  const int last = min((rt + 1) * WORK::ROWS, R) - 1, tile = WORK::KEYS / hg;
+  return (ca_admitted(keys, adm0, causal, causal ? last / rep : 0) + tile - 1) / tile;
 }
 // numbers of the first `n` row tiles of a head
 template <typename WORK>
-__device__ __forceinline__ int ca_numbers(int R, int keys, int adm0, int causal, int rep, int n) {
-  if (!causal) return keys > 0 ? n * ((keys + WORK::KEYS - 1) / WORK::KEYS + WORK::EXTRA) : 0;
+__device__ __forceinline__ int ca_numbers(int R, int keys, int adm0, int causal, int rep, int hg, int n) {
+  if (!causal) return keys > 0 && n > 0 ? n * (ca_key_tiles<WORK>(R, keys, adm0, 0, rep, hg, 0) + WORK::EXTRA) : 0;
   int t = 0;
   for (int rt = 0; rt < n; ++rt) {
-    const int kt = ca_key_tiles<WORK>(R, keys, adm0, causal, rep, rt);
+    const int kt = ca_key_tiles<WORK>(R, keys, adm0, causal, rep, hg, rt);
     t += kt > 0 ? kt + WORK::EXTRA : 0;
   }
   return t;
@@ -297,11 +304,11 @@ __device__ __forceinline__ int ca_row_tiles(const CaSeg &g, int rep) {
 // An item of a block's work: a range of key tiles of one row tile.
 struct __align__(16) CaJob {
   int q0, R, row0, keys;
-  int adm0, causal, head, rt;
+  int adm0, causal, head, rt;   // head: the first of `together`
   int kt0, n;              // key tiles; n < 0: the block's work is done
   int complete, record;    // the row tile has no other items; where the result goes otherwise
   int n_act[2];            // (tile kernel) key tiles that the two row tiles of the pair look at
-  int pad[2];
+  int together, pad;
 };
 __device__ __forceinline__ int ca_admitted(const CaJob &j, int t) { return ca_admitted(j.keys, j.adm0, j.causal, t); }
 
@@ -310,13 +317,14 @@ template <typename WORK>
 struct CaWalk {
   int t, end, begin_t, piece;
   int seg, head, rt, pos;  // pos: numbers of the row tile that lie before t
-  int R, causal;
+  int R, causal, hg;
   CaSeg g;
-  __device__ __forceinline__ int key_tiles(const CacheArgs &a) const { return ca_key_tiles<WORK>(R, g.keys, g.keys - g.nq + 1, causal, a.rep, rt); }
+  __device__ __forceinline__ int key_tiles(const CacheArgs &a) const { return ca_key_tiles<WORK>(R, g.keys, g.keys - g.nq + 1, causal, a.rep, hg, rt); }
   __device__ __forceinline__ void enter(const CacheArgs &a, const CaSeg *segs) {
     g = segs[seg];
     R = g.nq * a.rep;
     causal = seg >= a.G;
+    hg = ca_together<WORK>(R, a.kv);
   }
   __device__ __forceinline__ void begin(const CacheArgs &a, const int *off, const CaSeg *segs, int n_seg, int number, int t0, int t1) {
     t = begin_t = t0; end = t1; piece = number;
@@ -329,10 +337,11 @@ struct CaWalk {
     }
     seg = lo;
     enter(a, segs);
-    const int per_head = (off[seg + 1] - off[seg]) / a.kv;
+    const int per_head = (off[seg + 1] - off[seg]) * hg / a.kv;
     int u = t - off[seg];
     head = u / per_head;
     u -= head * per_head;
+    head *= hg;
     for (rt = 0;; ++rt) {
       const int kt = key_tiles(a), n = kt > 0 ? kt + WORK::EXTRA : 0;
       if (u < n) break;
@@ -345,7 +354,7 @@ struct CaWalk {
     while (t < end) {
       const int kt = key_tiles(a), p1 = min(kt + WORK::EXTRA, pos + (end - t));
       const int k0 = max(0, pos - WORK::EXTRA), k1 = p1 - WORK::EXTRA, first = t - pos + WORK::EXTRA;
-      j.q0 = g.q0; j.R = R; j.row0 = g.row0; j.keys = g.keys; j.adm0 = g.keys - g.nq + 1; j.causal = causal; j.head = head; j.rt = rt;
+      j.q0 = g.q0; j.R = R; j.row0 = g.row0; j.keys = g.keys; j.adm0 = g.keys - g.nq + 1; j.causal = causal; j.head = head; j.rt = rt; j.together = hg;
       j.kt0 = k0; j.n = k1 - k0; j.complete = k0 == 0 && k1 == kt; j.record = 2 * piece + (first <= begin_t ? 0 : 1);
       t += p1 - pos;
       if (t < end) {                       // the next row tile that has keys
@@ -353,7 +362,7 @@ struct CaWalk {
         do {
           if (++rt >= ca_row_tiles<WORK>(g, a.rep)) {
             rt = 0;
-            if (++head >= a.kv) {
+            if ((head += hg) >= a.kv) {
               head = 0;
               do ++seg; while (off[seg + 1] <= t);
               enter(a, segs);
@@ -379,7 +388,8 @@ __device__ __forceinline__ bool ca_plan(const CacheArgs &a, int *off, CaSeg *seg
     const CaSeg g = ca_segment(a, s, b);
     broken |= b;
     bad |= g.keys < 0;
-    const int n = a.kv * ca_numbers<WORK>(g.nq * a.rep, g.keys, g.keys - g.nq + 1, s >= a.G, a.rep, ca_row_tiles<WORK>(g, a.rep));
+    const int R = g.nq * a.rep, hg = ca_together<WORK>(R, a.kv);
+    const int n = a.kv / hg * ca_numbers<WORK>(R, g.keys, g.keys - g.nq + 1, s >= a.G, a.rep, hg, ca_row_tiles<WORK>(g, a.rep));
     segs[s] = g;
     off[s + 1] = n;
     mine += n;
@@ -433,12 +443,13 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void tma_load_3d_w(uint32_t smem_dst, const void *tmap, uint32_t bar, int32_t x, int32_t y, int32_t z, uint32_t leader) {
+// Keys or values as [head][column half][row][64 columns], see make_cache_map: one copy brings the tile of all heads and both halves.
+__device__ __forceinline__ void tma_load_cache_w(uint32_t smem_dst, const void *tmap, uint32_t bar, int32_t row, int32_t head, uint32_t leader) {
   asm volatile(
       "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
-      "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%3, %4, %5}], [%2];\n\t}"
-      ::"r"(smem_dst), "l"(tmap), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(leader)
+      "@q cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %3, %5}], [%2];\n\t}"
+      ::"r"(smem_dst), "l"(tmap), "r"(bar), "r"(0), "r"(row), "r"(head), "r"(leader)
       : "memory");
 }
 // Non-zero if either half is an infinity or NaN: an exponent of all ones, plus one, carries into the sign's place.
@@ -454,6 +465,11 @@ __device__ __forceinline__ void mbar_arrive_lane0(uint32_t bar, int lane) {
   if (lane == 0) mbar_arrive(bar);
   __syncwarp();
 }
+
+// Keys and values with a tile's box for one, two and four heads together.
+struct CaMaps {
+  CUtensorMap k[3], v[3];
+};
 
 struct CaBook {
   uint64_t full[CA_STAGES], empty[CA_STAGES], job_full[CA_JOBS], job_empty[CA_JOBS];
@@ -486,7 +502,7 @@ __device__ __forceinline__ void ca_describe_rows(const CacheArgs &a, const int *
         o1 = ld_prev(a.plan + n_seg + 2 + s);
       }
       part.R = R; part.i0 = (own.q0 - g.q0) * a.rep; part.keys = g.keys; part.adm0 = g.keys - g.nq + 1; part.causal = p;
-      part.off = o0; part.per_head = (o1 - o0) / a.kv;
+      part.off = o0; part.per_head = (o1 - o0) * (ca_streamed(R) ? ca_heads(R, a.kv) : 1) / a.kv;
     }
     for (int r = thread; r < own.nq; r += threads) {
       CaRow mine = row;
@@ -517,7 +533,7 @@ __device__ __forceinline__ void ca_merge(float &m, float &l, float2 other, float
 // matrices between the lanes.  Every warp keeps its own running maximum and sums; the four meet at an item's end.
 template <bool F16>
 __global__ void __launch_bounds__(CA_THREADS, 2)
-ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CacheArgs a) {
+ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ CacheArgs a) {
   extern __shared__ __align__(1024) uint8_t ca_smem[];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   float *join = reinterpret_cast<float *>(ca_smem + CA_STAGES * CA_STAGE_BYTES);
@@ -537,8 +553,10 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     }
     bk->abort_flag = 0;
     fence_barrier_init();
-    tma_prefetch_desc(&tmap_k);
-    tma_prefetch_desc(&tmap_v);
+  }
+  if (threadIdx.x < 3) {
+    tma_prefetch_desc(&maps.k[threadIdx.x]);
+    tma_prefetch_desc(&maps.v[threadIdx.x]);
   }
   __syncthreads();
   WaitCtx wc{&bk->abort_flag, a.status, STATUS_CACHE_TIMEOUT, a.wait_limit};
@@ -580,13 +598,14 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       const uint32_t jbar = smem_u32(&bk->job_full[slot]);
       if (lane == 0) {
         bk->job[slot] = j;
-        if (going) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(jbar), "r"(j.R * 256) : "memory");
+        if (going) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(jbar), "r"(j.R * j.together * 256) : "memory");
         else mbar_arrive(jbar);
       }
       __syncwarp();
       if (!more) break;
-      if (going && lane < j.R) {
-        const uint16_t *src = a.q + (long long)(j.q0 + lane / a.rep) * a.q_row + (long long)(j.head * a.rep + lane % a.rep) * a.q_head;
+      if (going && lane < j.R * j.together) {
+        const int sub = lane / j.R, i = lane - sub * j.R, t = i / a.rep;
+        const uint16_t *src = a.q + (long long)(j.q0 + t) * a.q_row + (long long)((j.head + sub) * a.rep + (i - t * a.rep)) * a.q_head;
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];"
                      ::"r"(q_smem + slot * CA_Q_BYTES + lane * CA_Q_PITCH), "l"(src), "r"(jbar) : "memory");
       }
@@ -595,12 +614,10 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         if (used >= CA_STAGES) mbar_wait_warp(smem_u32(&bk->empty[pos.slot]), pos.phase ^ 1u, wc);
         if (!__shfl_sync(0xffffffffu, bk->abort_flag, 0)) {
           const uint32_t bar = smem_u32(&bk->full[pos.slot]), dst = base + pos.slot * CA_STAGE_BYTES;
-          const int row = j.row0 + kt * StreamWork::KEYS;
+          const int row = j.row0 + kt * (StreamWork::KEYS / j.together), box = j.together >> 1;
           mbar_expect_tx_w(bar, CA_STAGE_BYTES, leader);
-          tma_load_3d_w(dst, &tmap_k, bar, 0, j.head, row, leader);
-          tma_load_3d_w(dst + CA_BLOCK_BYTES, &tmap_k, bar, 64, j.head, row, leader);
-          tma_load_3d_w(dst + 2 * CA_BLOCK_BYTES, &tmap_v, bar, 0, j.head, row, leader);
-          tma_load_3d_w(dst + 3 * CA_BLOCK_BYTES, &tmap_v, bar, 64, j.head, row, leader);
+          tma_load_cache_w(dst, &maps.k[box], bar, row, j.head, leader);
+          tma_load_cache_w(dst + CA_STAGE_BYTES / 2, &maps.v[box], bar, row, j.head, leader);
           issued = used + 1;
         }
         pos.step(CA_STAGES);
@@ -632,20 +649,23 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     const bool got = mbar_wait_drain(smem_u32(&bk->job_full[slot]), (jc / CA_JOBS) & 1, CA_WAIT_LIMIT);
     __syncwarp();
     const CaJob j = bk->job[slot];
+    if (!got || j.n < 0) break;
     const bool two = j.R > 8;                    // rows 8 .. 15 are in use
+    // Four heads together: a warp each.  Two: warps 0 and 2, 1 and 3 share one's keys.  One: all four do.
+    const int hg = j.together, sub = warp & (hg - 1), slice = warp / hg, keys = StreamWork::KEYS / hg, head = j.head + sub;
+    const int half_bytes = keys * 128, warp_off = (2 * sub * keys + slice * 16) * 128;       // a column half; this warp's 16 keys in a tile
     uint32_t qb[2][8][2];                        // the query rows as the second operand, a k-step each; [rows 0 .. 7, 8 .. 15]
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int k2 = 0; k2 < 4; ++k2) {
-        uint32_t r[4];
-        ldsm4(q_smem + slot * CA_Q_BYTES + (h * 8 + mr) * CA_Q_PITCH + (k2 * 4 + mi) * 16, r);
+        uint32_t r[4] = {0u, 0u, 0u, 0u};
+        if (h == 0 || two) ldsm4(q_smem + slot * CA_Q_BYTES + min(sub * j.R + h * 8 + mr, 15) * CA_Q_PITCH + (k2 * 4 + mi) * 16, r);    // (past the last row: any)
         qb[h][2 * k2][0] = r[0]; qb[h][2 * k2][1] = r[1];
         qb[h][2 * k2 + 1][0] = r[2]; qb[h][2 * k2 + 1][1] = r[3];
       }
     __syncwarp();
     mbar_arrive_lane0(smem_u32(&bk->job_empty[slot]), lane);
-    if (!got || j.n < 0) break;
     int adm[2][2];                               // admitted keys of query rows 8 h + 2 tq + e (rows past the last: none, whatever the buffer held)
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -657,7 +677,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     // (query row, head) of row 8 h + 2 tq + e; -1: none
     auto entry_of = [&](int h, int e) -> long long {
       const int i = 8 * h + 2 * tq + e, t = i / a.rep;
-      return i < j.R ? (long long)(j.q0 + t) * a.H + j.head * a.rep + (i - t * a.rep) : -1;
+      return i < j.R ? (long long)(j.q0 + t) * a.H + head * a.rep + (i - t * a.rep) : -1;
     };
     float o[2][8][4];                            // [][16 columns][column gq or gq + 8, row 2 tq or 2 tq + 1]
     float m[2][2], l[2][2];
@@ -672,18 +692,18 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     }
     for (int kt = j.kt0; kt < j.kt0 + j.n; ++kt) {
       mbar_wait_warp(smem_u32(&bk->full[pos.slot]), pos.phase, wc);
-      const uint32_t ks = base + pos.slot * CA_STAGE_BYTES, vs = ks + 2 * CA_BLOCK_BYTES;
-      const int j0 = kt * StreamWork::KEYS + warp * 16;      // this warp's first key
+      const uint32_t ks = base + pos.slot * CA_STAGE_BYTES + warp_off, vs = ks + CA_STAGE_BYTES / 2;
+      const int j0 = kt * keys + slice * 16;     // this warp's first key
       // ---- logits of 16 keys x 8 rows: x[][2 c + e] is key gq + 8 c, row 2 tq + e
       float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, y[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
       {
-        const int key = warp * 16 + (mi & 1) * 8 + mr;
+        const int key = (mi & 1) * 8 + mr;
         const uint32_t row = ks + key * 128;
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) {         // (two chains)
           const int c = kk * 2 + (mi >> 1);
           uint32_t k[4];
-          ldsm4(row + (kk >> 2) * CA_BLOCK_BYTES + (((c & 7) ^ (key & 7)) << 4), k);
+          ldsm4(row + (kk >> 2) * half_bytes + (((c & 7) ^ (key & 7)) << 4), k);
           mma16816<F16>(kk & 1 ? y[0] : x[0], k, qb[0][kk][0], qb[0][kk][1]);
           if (two) mma16816<F16>(kk & 1 ? y[1] : x[1], k, qb[1][kk][0], qb[1][kk][1]);
         }
@@ -742,8 +762,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       if (j0 + 16 > (j.causal ? j.adm0 : j.keys)) {
         const int r = lane >> 1, half = lane & 1;           // two lanes per key
         const bool dead = j0 + r >= j.keys;
-        const uint8_t *values = ca_smem + pos.slot * CA_STAGE_BYTES + 2 * CA_BLOCK_BYTES;
-        uint8_t *vrow = ca_smem + pos.slot * CA_STAGE_BYTES + (2 + half) * CA_BLOCK_BYTES + (warp * 16 + r) * 128;
+        uint8_t *values = ca_smem + pos.slot * CA_STAGE_BYTES + CA_STAGE_BYTES / 2 + warp_off, *vrow = values + half * half_bytes + r * 128;
         uint32_t hit = 0u;
         if (!dead)
           for (int c = 0; c < 8; ++c) {
@@ -759,7 +778,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
 #pragma unroll
           for (int e = 0; e < 16; ++e) bad |= ((who >> (2 * e)) & 3u) ? 1u << e : 0u;
           for (uint32_t left = bad; left; left &= left - 1) {
-            const int k = __ffs(left) - 1, key = warp * 16 + k;
+            const int k = __ffs(left) - 1;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const float2 pk = unpack2_t<F16>(__shfl_sync(0xffffffffu, (k & 8) ? p1[h] : p0[h], (k & 7) * 4 + tq));
@@ -769,7 +788,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {    // column 16 n + 8 c + gq
                   const int chunk = 2 * n + c;
-                  const uint16_t w = *reinterpret_cast<const uint16_t *>(values + (chunk >> 3) * CA_BLOCK_BYTES + key * 128 + (((chunk & 7) ^ (key & 7)) << 4) + 2 * gq);
+                  const uint16_t w = *reinterpret_cast<const uint16_t *>(values + (chunk >> 3) * half_bytes + k * 128 + (((chunk & 7) ^ (k & 7)) << 4) + 2 * gq);
                   const float v = unpack2_t<F16>(w).x;
                   if (in0) o[h][n][2 * c] += pk.x * v;
                   if (in1) o[h][n][2 * c + 1] += pk.y * v;
@@ -787,13 +806,13 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
 #pragma unroll
       for (int h = 0; h < 2; ++h) { b0[h] = transpose8x8(p0[h]); b1[h] = transpose8x8(p1[h]); }
       {
-        const int key = warp * 16 + (mi >> 1) * 8 + mr;
+        const int key = (mi >> 1) * 8 + mr;
         const uint32_t row = vs + key * 128;
 #pragma unroll
         for (int n = 0; n < 8; ++n) {
           const int c = 2 * n + (mi & 1);
           uint32_t v[4];
-          ldsm4t(row + (n >> 2) * CA_BLOCK_BYTES + (((c & 7) ^ (key & 7)) << 4), v);
+          ldsm4t(row + (n >> 2) * half_bytes + (((c & 7) ^ (key & 7)) << 4), v);
           mma16816<F16>(o[0][n], v, b0[0], b1[0]);
           if (two) mma16816<F16>(o[1][n], v, b0[1], b1[1]);
         }
@@ -802,7 +821,7 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       mbar_arrive_lane0(smem_u32(&bk->empty[pos.slot]), lane);
       pos.step(CA_STAGES);
     }
-    // ---- the four warps' sums of the item: 2 -> 0 and 3 -> 1, then 1 -> 0, which stores.  Values stay in fragment order, and the warps that
+    // ---- the sums of the warps that share a head: 2 -> 0 and 3 -> 1, then (one head) 1 -> 0; the last one stores.  Values stay in fragment order, and the warps that
     // hand theirs on go on to the next item.  (Through a buffer of whole rows that all four read, with a barrier of all four before and
     // after each piece of it, an item's end took 3700 to 4700 clocks.)
 #pragma unroll
@@ -854,7 +873,9 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
       pair_sync(1 + warp);
       get(buf, bk->ml[warp], 0);
       __syncwarp();
-      if (warp == 0) {
+      if (hg == 2) {
+        pair_arrive(4 + warp);
+      } else if (warp == 0) {
         pair_arrive(4);
         pair_sync(3);
         get(reinterpret_cast<const float4 *>(join) + CA_JOIN_BYTES / 32, bk->ml[1], 1);
@@ -870,7 +891,8 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
     constexpr integral_constant<int, 1> c1{};
     constexpr integral_constant<int, 4> c4{};
     constexpr integral_constant<int, 8> c8{};
-    if (j.R <= 4) {
+    if (hg == 4) {
+    } else if (j.R <= 4) {
       pass(c0, c8, c0);
     } else {
       pass(c0, c4, c0);
@@ -880,14 +902,14 @@ ca_stream_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_consta
         pass(c4, c8, c1);
       }
     }
-    if (warp == 0 && !bk->abort_flag) {
+    if (slice == 0 && !bk->abort_flag) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const long long entry = entry_of(h, e);
           if (entry < 0) continue;
-          const long long at = j.complete ? (j.causal ? (long long)a.n_q * a.H : 0) + entry : (long long)j.record * a.rec_rows + 8 * h + 2 * tq + e;
+          const long long at = j.complete ? (j.causal ? (long long)a.n_q * a.H : 0) + entry : (long long)j.record * a.rec_rows + sub * j.R + 8 * h + 2 * tq + e;
           float *dst = (j.complete ? a.full_o : a.rec_o[0]) + at * 128 + gq;
 #pragma unroll
           for (int n = 0; n < 8; ++n) {
@@ -1039,8 +1061,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
             if (past) { raw_any |= bit; raw_odd ^= bit; }
             const int row = j.row0 + kt * 128;
             mbar_expect_tx_w(bar, CT_TILE_BYTES, leader);
-            tma_load_3d_w(dst, kv ? &tmap_v : &tmap_k, bar, 0, j.head, row, leader);
-            tma_load_3d_w(dst + CT_BLOCK_BYTES, kv ? &tmap_v : &tmap_k, bar, 64, j.head, row, leader);
+            tma_load_cache_w(dst, kv ? &tmap_v : &tmap_k, bar, row, j.head, leader);
             issued = tc + 1;
           }
         }
@@ -1438,10 +1459,11 @@ struct CaParts {
 template <typename WORK>
 __device__ __forceinline__ CaParts ca_parts_of(const CacheArgs &a, const CaRowPart &p, int which, int all, long long entry, int kvh, int sub) {
   CaParts out;
-  const int i = p.i0 + sub, rt = i / WORK::ROWS, r = i - rt * WORK::ROWS;
-  const int kt = ca_key_tiles<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, rt);
+  const int hg = ca_together<WORK>(p.R, a.kv), i = p.i0 + sub, rt = i / WORK::ROWS;
+  const int r = i - rt * WORK::ROWS + (hg > 1 ? (kvh & (hg - 1)) * p.R : 0);
+  const int kt = ca_key_tiles<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, hg, rt);
   const int chunk = ca_chunk(all, a.pieces[WORK::INDEX]), rec_rows = WORK::INDEX == 0 ? a.rec_rows : WORK::ROWS;
-  const int first = p.off + kvh * p.per_head + ca_numbers<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, rt) + WORK::EXTRA;
+  const int first = p.off + kvh / hg * p.per_head + ca_numbers<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, hg, rt) + WORK::EXTRA;
   const int c0 = first / chunk, c1 = (first + kt - 1) / chunk;
   const bool complete = c0 == c1;
   out.n = kt == 0 ? 0 : c1 - c0 + 1;
