@@ -347,20 +347,31 @@ asap_status asap_cache_evict(asap_ctx *ctx, const asap_cache_evict_args *p, void
   EvictArgs a;
   a.B = p->B; a.max_len = p->max_len; a.keep = p->keep; a.sink = p->sink; a.recent = p->recent; a.rows = p->rows; a.dst_rows = p->dst_rows;
   a.start = p->start; a.len = p->len; a.dst_start = p->dst_start; a.weights = p->weights; a.pos = p->pos; a.keep_idx = p->keep_idx;
-  a.new_len = p->new_len; a.dst_weights = p->dst_weights; a.dst_pos = p->dst_pos; a.status = ctx->status;
+  a.new_len = p->new_len; a.status = ctx->status;
+  // (where max_len <= keep every sequence stays whole, and its rows are not ranked)
+  const bool cluster = p->max_len > p->keep && p->max_len >= EV_CLUSTER_MIN;
+  const long long share = p->max_len > p->keep ? (((long long)p->max_len + (cluster ? EV_CLUSTER : 1) - 1) / (cluster ? EV_CLUSTER : 1) + 31) / 32 * 32 : 0;
+  a.cached = share * 4 <= EV_KEYS_BYTES ? (int)share : 0;
   DeviceGuard guard(ctx->device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   mark(ctx, "evict_select", st);
-  launch_pdl(evict_select_kernel, dim3(p->B), dim3(EV_THREADS), 0, st, a);
+  if (cluster)
+    launch_pdl_cluster_z(evict_select_kernel<true>, dim3(1, p->B, EV_CLUSTER), dim3(EV_THREADS), (size_t)a.cached * 4, st, EV_CLUSTER, a);
+  else
+    launch_pdl(evict_select_kernel<false>, dim3(1, p->B), dim3(EV_THREADS), (size_t)a.cached * 4, st, a);
   ASAP_TRY(after_launch(ctx, "evict_select"));
-  if (p->n_tensors > 0) {
-    mv.keep_idx = p->keep_idx; mv.start = p->start; mv.dst_start = p->dst_start; mv.keep = p->keep; mv.rows = p->rows; mv.dst_rows = p->dst_rows;
+  const bool meta = p->dst_weights || p->dst_pos;
+  if (p->n_tensors > 0 || meta) {
+    mv.keep_idx = p->keep_idx; mv.start = p->start; mv.dst_start = p->dst_start; mv.keep = p->keep; mv.n_tensors = p->n_tensors;
     mv.row_vecs = (int)(p->row_bytes / 16);
+    mv.weights = p->weights; mv.pos = p->pos; mv.dst_weights = p->dst_weights; mv.dst_pos = p->dst_pos;
+    const unsigned layers = p->n_tensors + (meta ? 1 : 0);
     mark(ctx, "evict_move", st);
+    mv.in_order = meta_in_place ? 1 : 0;
     if (in_place)
-      launch_pdl(evict_in_place_kernel, dim3((mv.row_vecs + 15) / 16, p->B, p->n_tensors), dim3(EV_MOVE_THREADS), 0, st, mv);
+      launch_pdl(evict_in_place_kernel, dim3((mv.row_vecs + 15) / 16, p->B, layers), dim3(EV_MOVE_THREADS), 0, st, mv);
     else
-      launch_pdl(evict_move_kernel, dim3((p->keep + EV_MOVE_THREADS / 32 - 1) / (EV_MOVE_THREADS / 32), p->B, p->n_tensors), dim3(EV_MOVE_THREADS), 0, st, mv);
+      launch_pdl(evict_move_kernel, dim3((p->keep + EV_MOVE_THREADS / 32 - 1) / (EV_MOVE_THREADS / 32), p->B, layers), dim3(EV_MOVE_THREADS), 0, st, mv);
     ASAP_TRY(after_launch(ctx, "evict_move"));
   }
   return finish(ctx, ASAP_OK, st);

@@ -690,12 +690,25 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
 #pragma unroll
       for (int e = 0; e < 2; ++e) { m[h][e] = -INFINITY; l[h][e] = 0.f; }
     }
-    for (int kt = j.kt0; kt < j.kt0 + j.n; ++kt) {
-      mbar_wait_warp(smem_u32(&bk->full[pos.slot]), pos.phase, wc);
+    float *lrow[2][2];                           // this lane's place in the rows of logits
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const long long entry = a.logits ? entry_of(h, e) : -1;
+        lrow[h][e] = entry < 0 ? nullptr : a.logits + entry * a.pitch + (j.causal ? a.own_off : 0) + gq;
+      }
+    // One tile; TWO: with rows 8 .. 15 (both sets step by step, so that neither waits for the other's latencies).
+    auto tile = [&](auto two_sets, int kt) {
+      constexpr int SETS = decltype(two_sets)::value;
       const uint32_t ks = base + pos.slot * CA_STAGE_BYTES + warp_off, vs = ks + CA_STAGE_BYTES / 2;
       const int j0 = kt * keys + slice * 16;     // this warp's first key
       // ---- logits of 16 keys x 8 rows: x[][2 c + e] is key gq + 8 c, row 2 tq + e
-      float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, y[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      float x[SETS][4], y[SETS][4];
+#pragma unroll
+      for (int h = 0; h < SETS; ++h)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[h][c] = y[h][c] = 0.f;
       {
         const int key = (mi & 1) * 8 + mr;
         const uint32_t row = ks + key * 128;
@@ -704,42 +717,47 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
           const int c = kk * 2 + (mi >> 1);
           uint32_t k[4];
           ldsm4(row + (kk >> 2) * half_bytes + (((c & 7) ^ (key & 7)) << 4), k);
-          mma16816<F16>(kk & 1 ? y[0] : x[0], k, qb[0][kk][0], qb[0][kk][1]);
-          if (two) mma16816<F16>(kk & 1 ? y[1] : x[1], k, qb[1][kk][0], qb[1][kk][1]);
+#pragma unroll
+          for (int h = 0; h < SETS; ++h) mma16816<F16>(kk & 1 ? y[h] : x[h], k, qb[h][kk][0], qb[h][kk][1]);
         }
       }
-      uint32_t p0[2] = {0u, 0u}, p1[2] = {0u, 0u};           // probabilities of keys gq and gq + 8, rows 2 tq and 2 tq + 1
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (h == 1 && !two) continue;
+      for (int h = 0; h < SETS; ++h)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const int key = j0 + gq + 8 * (c >> 1);
           x[h][c] = key < adm[h][c & 1] ? (x[h][c] + y[h][c]) * a.scale_log2 : -INFINITY;
         }
-        if (a.logits) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const long long entry = entry_of(h, e);
-            if (entry < 0) continue;
-            float *row = a.logits + entry * a.pitch + (j.causal ? a.own_off : 0) + j0 + gq;
-            row[0] = x[h][e];
-            row[8] = x[h][2 + e];
+      for (int h = 0; h < SETS; ++h)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (lrow[h][e]) {
+            lrow[h][e][j0] = x[h][e];
+            lrow[h][e][j0 + 8] = x[h][2 + e];
           }
-        }
-        // ---- probabilities relative to the running maximum
-        float mx[2], p[4];
+      // ---- probabilities relative to the running maximum
+      float mx[SETS][2];
+      bool up = false;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) mx[e] = fmaxf(x[h][e], x[h][2 + e]);
+      for (int h = 0; h < SETS; ++h)
 #pragma unroll
-        for (int s = 4; s < 32; s <<= 1)
+        for (int e = 0; e < 2; ++e) mx[h][e] = fmaxf(x[h][e], x[h][2 + e]);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], s));
-        if (__any_sync(0xffffffffu, mx[0] > m[h][0] || mx[1] > m[h][1])) {
+      for (int s = 4; s < 32; s <<= 1)
+#pragma unroll
+        for (int h = 0; h < SETS; ++h)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) mx[h][e] = fmaxf(mx[h][e], __shfl_xor_sync(0xffffffffu, mx[h][e], s));
+#pragma unroll
+      for (int h = 0; h < SETS; ++h) up = up || mx[h][0] > m[h][0] || mx[h][1] > m[h][1];
+      if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+        for (int h = 0; h < SETS; ++h) {
           float f[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float top = fmaxf(m[h][e], mx[e]);
+            const float top = fmaxf(m[h][e], mx[h][e]);
             f[e] = top == m[h][e] ? 1.f : fast_exp2(m[h][e] - top);
             m[h][e] = top;
             l[h][e] *= f[e];
@@ -747,6 +765,11 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
 #pragma unroll
           for (int n = 0; n < 8; ++n) { o[h][n][0] *= f[0]; o[h][n][1] *= f[1]; o[h][n][2] *= f[0]; o[h][n][3] *= f[1]; }
         }
+      }
+      uint32_t p0[SETS], p1[SETS];               // probabilities of keys gq and gq + 8, rows 2 tq and 2 tq + 1
+#pragma unroll
+      for (int h = 0; h < SETS; ++h) {
+        float p[4];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const float ref = m[h][e] == -INFINITY ? 0.f : m[h][e];
@@ -780,7 +803,7 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
           for (uint32_t left = bad; left; left &= left - 1) {
             const int k = __ffs(left) - 1;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < SETS; ++h) {
               const float2 pk = unpack2_t<F16>(__shfl_sync(0xffffffffu, (k & 8) ? p1[h] : p0[h], (k & 7) * 4 + tq));
               const bool in0 = j0 + k < adm[h][0], in1 = j0 + k < adm[h][1];
 #pragma unroll
@@ -802,9 +825,9 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
         }
         fence_proxy_async();                     // these writes come before the next copy into the slot
       }
-      uint32_t b0[2], b1[2];
+      uint32_t b0[SETS], b1[SETS];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) { b0[h] = transpose8x8(p0[h]); b1[h] = transpose8x8(p1[h]); }
+      for (int h = 0; h < SETS; ++h) { b0[h] = transpose8x8(p0[h]); b1[h] = transpose8x8(p1[h]); }
       {
         const int key = (mi >> 1) * 8 + mr;
         const uint32_t row = vs + key * 128;
@@ -813,10 +836,15 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
           const int c = 2 * n + (mi & 1);
           uint32_t v[4];
           ldsm4t(row + (n >> 2) * half_bytes + (((c & 7) ^ (key & 7)) << 4), v);
-          mma16816<F16>(o[0][n], v, b0[0], b1[0]);
-          if (two) mma16816<F16>(o[1][n], v, b0[1], b1[1]);
+#pragma unroll
+          for (int h = 0; h < SETS; ++h) mma16816<F16>(o[h][n], v, b0[h], b1[h]);
         }
       }
+    };
+    for (int kt = j.kt0; kt < j.kt0 + j.n; ++kt) {
+      mbar_wait_warp(smem_u32(&bk->full[pos.slot]), pos.phase, wc);
+      if (two) tile(std::integral_constant<int, 2>{}, kt);
+      else tile(std::integral_constant<int, 1>{}, kt);
       __syncwarp();
       mbar_arrive_lane0(smem_u32(&bk->empty[pos.slot]), lane);
       pos.step(CA_STAGES);
@@ -1653,15 +1681,17 @@ ca_weight_kernel(const __grid_constant__ CacheArgs a, int prefix_blocks, int pre
 // Eviction
 // =======================================================================================
 constexpr int EV_THREADS = 1024;
+constexpr int EV_CLUSTER = 8;                    // blocks that share a long sequence
+constexpr int EV_CLUSTER_MIN = 6144;             // rows from which they do
+constexpr int EV_KEYS_BYTES = 192 * 1024;        // a block's keys in shared memory, if its rows fit
 
 struct EvictArgs {
   int B, max_len, keep, sink, recent, rows, dst_rows;
+  int cached;                                    // rows of a block whose keys it keeps in shared memory; 0: taken again in every pass
   const int *start, *len, *dst_start;
   const float *weights;
   const int *pos;
   int *keep_idx, *new_len;
-  float *dst_weights;
-  int *dst_pos;
   uint32_t *status;
 };
 
@@ -1676,128 +1706,157 @@ __device__ __forceinline__ uint32_t row_key(float w, int row, int pos, int sink,
   return row < sink || (long long)pos > newest - recent ? 0xffffffffu : rank_key(w);
 }
 
-// A block per sequence: the keep-th largest key by radix selection, eight bits a pass; then every warp compacts a range of rows.
+// The keep-th largest key by radix selection, eight bits a pass, then every warp writes the kept rows of a range.  A block per sequence, or
+// for long ones a cluster of eight that share its rows and add their histograms through each other's shared memory.  A row's weight and
+// position are read once, its key stays in shared memory.  (One block that read both again in each of its seven passes: 2 x 30001 to
+// 60001 rows, 4096 kept 119 us.)
+template <bool CLUSTER>
 __global__ void __launch_bounds__(EV_THREADS)
 evict_select_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ int hist[256];
+  extern __shared__ uint32_t ev_keys[];
+  __shared__ int hist[2][256];
   __shared__ int warp_gt[32], warp_eq[32];
+  __shared__ int sh_pub[4];                      // what the other blocks of the cluster read: largest position, rows above and at the threshold
   __shared__ uint32_t sh_prefix;
   __shared__ int sh_need;
-  __shared__ long long sh_newest;
   pdl_enter();
-  const int b = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  constexpr int PARTS = CLUSTER ? EV_CLUSTER : 1;
+  const int b = blockIdx.y, part = CLUSTER ? (int)cluster_cta_rank() : 0, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  auto meet = [&]() {
+    if constexpr (CLUSTER) cluster_sync_all();
+    else __syncthreads();
+  };
+  auto theirs = [&](const int *p, int rank) {    // the word at p of block `rank`
+    if constexpr (CLUSTER) return ld_cluster_s32(cluster_map(smem_u32(p), (uint32_t)rank));
+    else return *reinterpret_cast<const volatile int *>(p);
+  };
   const int n = ld_prev(a.len + b), row0 = ld_prev(a.start + b), dst0 = a.dst_start ? ld_prev(a.dst_start + b) : row0;
   int *idx = a.keep_idx + (size_t)b * a.keep;
   const int m = min(n, a.keep);
+  // (all blocks of a cluster see the same sequence: they leave together)
   if (n < 0 || n > a.max_len || row0 < 0 || (long long)row0 + n > a.rows || dst0 < 0 || (long long)dst0 + m > a.dst_rows) {
-    for (int i = tid; i < a.keep; i += EV_THREADS) idx[i] = -1;
-    if (tid == 0) atomicOr(a.status, (uint32_t)STATUS_BAD_SAMPLE);
+    for (int i = part * EV_THREADS + tid; i < a.keep; i += PARTS * EV_THREADS) idx[i] = -1;
+    if (tid == 0 && part == 0) atomicOr(a.status, (uint32_t)STATUS_BAD_SAMPLE);
+    return;
+  }
+  for (int i = m + part * EV_THREADS + tid; i < a.keep; i += PARTS * EV_THREADS) idx[i] = -1;
+  if (n <= a.keep) {
+    for (int i = part * EV_THREADS + tid; i < n; i += PARTS * EV_THREADS) idx[i] = i;
+    meet();                                      // (every block has read the length, which may be new_len itself)
+    if (tid == 0 && part == 0) a.new_len[b] = m;
     return;
   }
   const float *w = a.weights + row0;
   const int *pos = a.pos ? a.pos + row0 : nullptr;
-  for (int i = m + tid; i < a.keep; i += EV_THREADS) idx[i] = -1;
-  if (n <= a.keep) {
-    for (int i = tid; i < n; i += EV_THREADS) idx[i] = i;
-  } else {
-    long long newest = n - 1;
-    if (pos) {
-      int top = INT_MIN;
-      for (int i = tid; i < n; i += EV_THREADS) top = max(top, ld_prev(pos + i));
-      top = __reduce_max_sync(0xffffffffu, top);
-      if (lane == 0) warp_gt[warp] = top;
-      __syncthreads();
-      if (warp == 0) {
-        top = __reduce_max_sync(0xffffffffu, warp_gt[lane]);
-        if (lane == 0) sh_newest = top;
-      }
-      __syncthreads();
-      newest = sh_newest;
+  const int share = ((n + PARTS - 1) / PARTS + 31) & ~31, first = min(n, part * share), last = min(n, first + share), mine = last - first;
+  const bool cached = mine <= a.cached;
+  // ---- the largest position; positions wait in the keys' place
+  long long newest = n - 1;
+  if (pos) {
+    int top = INT_MIN;
+#pragma unroll 4
+    for (int i = tid; i < mine; i += EV_THREADS) {
+      const int p = ld_prev(pos + first + i);
+      if (cached) ev_keys[i] = (uint32_t)p;
+      top = max(top, p);
     }
-    auto key = [&](int i) { return row_key(ld_prev(w + i), i, pos ? ld_prev(pos + i) : i, a.sink, a.recent, newest); };
-    uint32_t prefix = 0u;
-    int need = a.keep;                           // rows still to be taken among those that share the prefix
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int i = tid; i < n; i += EV_THREADS) {
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) warp_gt[warp] = top;
+    __syncthreads();
+    if (warp == 0) {
+      top = __reduce_max_sync(0xffffffffu, warp_gt[lane]);
+      if (lane == 0) sh_pub[0] = top;
+    }
+    meet();
+    top = INT_MIN;
+#pragma unroll
+    for (int r = 0; r < PARTS; ++r) top = max(top, theirs(&sh_pub[0], r));
+    newest = top;
+  }
+  auto fresh = [&](int i) {                      // key of this block's row i from memory
+    return row_key(ld_prev(w + first + i), first + i, pos ? ld_prev(pos + first + i) : first + i, a.sink, a.recent, newest);
+  };
+  auto key = [&](int i) { return cached ? ev_keys[i] : fresh(i); };
+  uint32_t prefix = 0u;
+  int need = a.keep;                             // rows still to be taken among those that share the prefix
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    int *h = hist[(shift >> 3) & 1];             // (the other one may still be read by other blocks)
+    if (tid < 256) h[tid] = 0;
+    __syncthreads();
+    if (shift == 24) {
+#pragma unroll 4
+      for (int i = tid; i < mine; i += EV_THREADS) {
+        uint32_t k;
+        if (cached) {
+          k = row_key(ld_prev(w + first + i), first + i, pos ? (int)ev_keys[i] : first + i, a.sink, a.recent, newest);
+          ev_keys[i] = k;
+        } else {
+          k = fresh(i);
+        }
+        atomicAdd(&h[k >> 24], 1);
+      }
+    } else {
+      for (int i = tid; i < mine; i += EV_THREADS) {
         const uint32_t k = key(i);
-        if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1);
+        if ((k >> (shift + 8)) == prefix) atomicAdd(&h[(k >> shift) & 255u], 1);
       }
-      __syncthreads();
-      if (warp == 0) {                           // from the top: lane holds bins 255 - 8 lane .. 248 - 8 lane
-        int c[8], mine = 0;
+    }
+    meet();
+    if (warp < 8) {                              // all blocks' counts, thread t has bin 255 - t
+      int c = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { c[e] = hist[255 - 8 * lane - e]; mine += c[e]; }
-        int above = mine;
+      for (int r = 0; r < PARTS; ++r) c += theirs(&h[255 - tid], r);
+      int above = c;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int v = __shfl_up_sync(0xffffffffu, above, o);
-          if (lane >= o) above += v;
-        }
-        above -= mine;
-        if (above < need && above + mine >= need) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (above < need && above + c[e] >= need) {
-              sh_prefix = (prefix << 8) | (uint32_t)(255 - 8 * lane - e);
-              sh_need = need - above;
-              above = INT_MAX / 2;
-            } else {
-              above += c[e];
-            }
-          }
-        }
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, above, o);
+        if (lane >= o) above += v;
       }
-      __syncthreads();
-      prefix = sh_prefix;
-      need = sh_need;
+      if (lane == 31) warp_eq[warp] = above;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      for (int v = 0; v < warp; ++v) above += warp_eq[v];
+      if (above >= need && above - c < need) {
+        sh_prefix = (prefix << 8) | (uint32_t)(255 - tid);
+        sh_need = need - (above - c);
+      }
     }
-    // rows above the threshold, and the first `need` equal to it
-    const int per = ((n + 1023) / 1024) * 32, lo = min(n, warp * per), hi = min(n, lo + per);
-    int gt = 0, eq = 0;
-    for (int i = lo + lane; i < hi; i += 32) {
-      const uint32_t k = key(i);
-      gt += k > prefix;
-      eq += k == prefix;
-    }
-    gt = __reduce_add_sync(0xffffffffu, gt);
-    eq = __reduce_add_sync(0xffffffffu, eq);
-    if (lane == 0) { warp_gt[warp] = gt; warp_eq[warp] = eq; }
     __syncthreads();
-    int gt0 = 0, eq0 = 0;
-    for (int v = 0; v < warp; ++v) { gt0 += warp_gt[v]; eq0 += warp_eq[v]; }
-    int at = gt0 + min(eq0, need);
-    for (int i0 = lo; i0 < hi; i0 += 32) {
-      const int i = i0 + lane;
-      const uint32_t k = i < hi ? key(i) : 0u;
-      const uint32_t beq = __ballot_sync(0xffffffffu, i < hi && k == prefix);
-      const bool take = i < hi && (k > prefix || (k == prefix && eq0 + __popc(beq & ((1u << lane) - 1u)) < need));
-      const uint32_t bt = __ballot_sync(0xffffffffu, take);
-      if (take) idx[at + __popc(bt & ((1u << lane) - 1u))] = i;
-      at += __popc(bt);
-      eq0 += __popc(beq);
-    }
+    prefix = sh_prefix;
+    need = sh_need;
   }
-  if (tid == 0) a.new_len[b] = m;
+  // ---- rows above the threshold, and the first `need` equal to it; a warp's rows lie side by side
+  const int per = ((mine + 1023) / 1024) * 32, lo = min(mine, warp * per), hi = min(mine, lo + per);
+  int gt = 0, eq = 0;
+  for (int i = lo + lane; i < hi; i += 32) {
+    const uint32_t k = key(i);
+    gt += k > prefix;
+    eq += k == prefix;
+  }
+  gt = __reduce_add_sync(0xffffffffu, gt);
+  eq = __reduce_add_sync(0xffffffffu, eq);
+  if (lane == 0) { warp_gt[warp] = gt; warp_eq[warp] = eq; }
   __syncthreads();
-  // weights and positions; a piece is read before it is written, and no later piece has its source where an earlier one goes
-  for (int i0 = 0; i0 < m; i0 += EV_THREADS) {
-    const int i = i0 + tid;
-    float wv = 0.f;
-    int pv = 0;
-    if (i < m) {
-      const int s = *reinterpret_cast<const volatile int *>(idx + i);
-      if (a.dst_weights) wv = ld_prev(w + s);
-      if (a.dst_pos) pv = pos ? ld_prev(pos + s) : s;
-    }
-    __syncthreads();
-    if (i < m) {
-      if (a.dst_weights) a.dst_weights[dst0 + i] = wv;
-      if (a.dst_pos) a.dst_pos[dst0 + i] = pv;
-    }
-    __syncthreads();
+  if (warp == 0) {
+    const int g = __reduce_add_sync(0xffffffffu, warp_gt[lane]), e = __reduce_add_sync(0xffffffffu, warp_eq[lane]);
+    if (lane == 0) { sh_pub[1] = g; sh_pub[2] = e; }
   }
+  meet();
+  int gt0 = 0, eq0 = 0;
+  for (int r = 0; r < part; ++r) { gt0 += theirs(&sh_pub[1], r); eq0 += theirs(&sh_pub[2], r); }
+  for (int v = 0; v < warp; ++v) { gt0 += warp_gt[v]; eq0 += warp_eq[v]; }
+  int at = gt0 + min(eq0, need);
+  for (int i0 = lo; i0 < hi; i0 += 32) {
+    const int i = i0 + lane;
+    const uint32_t k = i < hi ? key(i) : 0u;
+    const uint32_t beq = __ballot_sync(0xffffffffu, i < hi && k == prefix);
+    const bool take = i < hi && (k > prefix || (k == prefix && eq0 + __popc(beq & ((1u << lane) - 1u)) < need));
+    const uint32_t bt = __ballot_sync(0xffffffffu, take);
+    if (take) idx[at + __popc(bt & ((1u << lane) - 1u))] = first + i;
+    at += __popc(bt);
+    eq0 += __popc(beq);
+  }
+  if (tid == 0 && part == 0) a.new_len[b] = m;
+  if constexpr (CLUSTER) cluster_sync_all();     // nobody's shared memory goes while it may be read
 }
 
 constexpr int EV_MAX_TENSORS = 64;
@@ -1806,43 +1865,77 @@ struct EvictMoveArgs {
   const uint4 *src[EV_MAX_TENSORS];
   uint4 *dst[EV_MAX_TENSORS];
   const int *keep_idx, *start, *dst_start;
-  int keep, rows, dst_rows, row_vecs;
+  int n_tensors, keep, row_vecs;
+  int in_order;                                  // weights or positions move in place
+  const float *weights;
+  const int *pos;
+  float *dst_weights;
+  int *dst_pos;
 };
 
-// Into other tensors: a warp per kept row.
+// Weights and positions of a sequence, a piece at a time: it is read before it is written, and no later piece has its source where an earlier
+// one went.
+__device__ __forceinline__ void evict_meta_in_order(const EvictMoveArgs &a, int b, int row0, int dst0) {
+  const int *idx = a.keep_idx + (size_t)b * a.keep;
+  for (int i0 = 0; i0 < a.keep; i0 += EV_MOVE_THREADS) {
+    const int i = i0 + threadIdx.x, k = i < a.keep ? ld_prev(idx + i) : -1;
+    float w = 0.f;
+    int p = 0;
+    if (k >= 0 && a.dst_weights) w = ld_prev(a.weights + row0 + k);
+    if (k >= 0 && a.dst_pos) p = a.pos ? ld_prev(a.pos + row0 + k) : k;
+    const bool end = __syncthreads_or(k < 0);
+    if (k >= 0 && a.dst_weights) a.dst_weights[dst0 + i] = w;
+    if (k >= 0 && a.dst_pos) a.dst_pos[dst0 + i] = p;
+    if (end) break;
+  }
+}
+
+// Into other tensors: a warp per kept row.  The last grid layer moves weights and positions, a thread per row.
 __global__ void __launch_bounds__(EV_MOVE_THREADS)
 evict_move_kernel(const __grid_constant__ EvictMoveArgs a) {
   pdl_enter();
-  const int b = blockIdx.y, t = blockIdx.z, i = blockIdx.x * (EV_MOVE_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int b = blockIdx.y, t = blockIdx.z, lane = threadIdx.x & 31;
+  const int row0 = ld_prev(a.start + b), dst0 = a.dst_start ? ld_prev(a.dst_start + b) : row0;
+  if (t == a.n_tensors && a.in_order) {
+    if (blockIdx.x == 0) evict_meta_in_order(a, b, row0, dst0);
+    return;
+  }
+  const int i = t == a.n_tensors ? blockIdx.x * EV_MOVE_THREADS + threadIdx.x : blockIdx.x * (EV_MOVE_THREADS / 32) + (threadIdx.x >> 5);
   if (i >= a.keep) return;
   const int k = ld_prev(a.keep_idx + (size_t)b * a.keep + i);
-  const int row0 = ld_prev(a.start + b), dst0 = a.dst_start ? ld_prev(a.dst_start + b) : row0;
   if (k < 0) return;
+  if (t == a.n_tensors) {
+    if (a.dst_weights) a.dst_weights[dst0 + i] = ld_prev(a.weights + row0 + k);
+    if (a.dst_pos) a.dst_pos[dst0 + i] = a.pos ? ld_prev(a.pos + row0 + k) : k;
+    return;
+  }
   const uint4 *s = a.src[t] + (size_t)(row0 + k) * a.row_vecs;
   uint4 *d = a.dst[t] + (size_t)(dst0 + i) * a.row_vecs;
-  int v = lane;
-  for (; v + 7 * 32 < a.row_vecs; v += 8 * 32) {
+  for (int v = lane; v < a.row_vecs; v += 8 * 32) {
     uint4 x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ld_prev8(s + v + 32 * e, x[e]);
+    for (int e = 0; e < 8; ++e)
+      if (v + 32 * e < a.row_vecs) ld_prev8(s + v + 32 * e, x[e]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d[v + 32 * e] = x[e];
-  }
-  for (; v < a.row_vecs; v += 32) {
-    uint4 x;
-    ld_prev8(s + v, x);
-    d[v] = x;
+    for (int e = 0; e < 8; ++e)
+      if (v + 32 * e < a.row_vecs) d[v + 32 * e] = x[e];
   }
 }
 
 // In place: a block per (sequence, tensor, 256 bytes of every row) takes the kept rows in ascending order, 128 at a time, and reads a piece
-// before it writes it.  Row i of the kept ones goes to row i <= its own number, so no later piece reads what an earlier one wrote.
+// before it writes it.  Row i of the kept ones goes to row i <= its own number, so no later piece reads what an earlier one wrote.  Weights
+// and positions likewise, by one block of the last grid layer.
 __global__ void __launch_bounds__(EV_MOVE_THREADS)
 evict_in_place_kernel(const __grid_constant__ EvictMoveArgs a) {
   pdl_enter();
-  const int b = blockIdx.y, t = blockIdx.z, v = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
+  const int b = blockIdx.y, t = blockIdx.z;
   const int *idx = a.keep_idx + (size_t)b * a.keep;
-  const int row0 = ld_prev(a.start + b);
+  const int row0 = ld_prev(a.start + b), dst0 = a.dst_start ? ld_prev(a.dst_start + b) : row0;
+  if (t == a.n_tensors) {
+    if (blockIdx.x == 0) evict_meta_in_order(a, b, row0, dst0);
+    return;
+  }
+  const int v = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
   uint4 *base = a.dst[t] + v;
   const bool in = v < a.row_vecs;
   for (int i0 = 0; i0 < a.keep; i0 += 128) {
@@ -1858,14 +1951,13 @@ evict_in_place_kernel(const __grid_constant__ EvictMoveArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (in && k[e] > i0 + r0 + 16 * e) ld_prev8(base + (size_t)(row0 + k[e]) * a.row_vecs, x[e]);
-    const bool last = __syncthreads_or(end);
+    const bool done = __syncthreads_or(end);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int i = i0 + r0 + 16 * e;
       if (in && k[e] > i) base[(size_t)(row0 + i) * a.row_vecs] = x[e];
     }
-    if (last) break;
-    __syncthreads();
+    if (done) break;
   }
 }
 

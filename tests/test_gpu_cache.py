@@ -419,7 +419,8 @@ def _bits(t):
 @pytest.mark.parametrize("special", [False, True], ids=["random", "special"])
 @pytest.mark.parametrize("lens,keep,sink,recent,row", [([0, 1, 5, 40, 33], 5, 1, 2, 16), ([2000, 700, 1025, 31], 640, 4, 64, 272),
                                                        ([9000], 8999, 0, 0, 4096), ([300, 300], 1, 0, 1, 48), ([65, 64, 63], 64, 30, 34, 256),
-                                                       ([150, 400], 129, 129, 0, 768), ([70001], 4096, 4, 512, 64)])
+                                                       ([150, 400], 129, 129, 0, 768), ([70001], 4096, 4, 512, 64),
+                                                       ([6000, 20000, 5, 6144], 700, 4, 50, 16), ([400000], 3000, 2, 10, 16)])
 def test_eviction(ctx, lens, keep, sink, recent, row, special, in_place):
     start, rows, w, pos = _evict_case(len(lens) * 31 + keep, lens, special)
     B = len(lens)
@@ -464,6 +465,26 @@ def test_eviction_without_positions_or_tensors(ctx):
         e = R.evict(w[start[b]:start[b] + n].tolist(), list(range(n)), 50, 2, 10)
         assert keep_idx[b].tolist() == e + [-1] * (50 - len(e)) and int(new_len[b]) == len(e)
         assert op[start[b]:start[b] + len(e)].tolist() == e
+
+
+def test_eviction_of_weights_in_place_beside_tensors_apart(ctx):
+    lens = [300, 7, 1200]
+    start, rows, w, pos = _evict_case(9, lens)
+    dw, dp = w.to(DEV), pos.to(DEV)
+    src = torch.randn(rows, 16, device=DEV)
+    dst = torch.full((rows, 16), 9.0, device=DEV)
+    keep_idx, new_len = torch.empty(3, 90, dtype=torch.int32, device=DEV), i32([0, 0, 0])
+    A.asap_cache_evict(ctx, A.CacheEvict(i32(start), i32(lens), 1200, 90, dw, dp, keep_idx, new_len, src=[src], dst=[dst], dst_weights=dw,
+                                         dst_pos=dp, sink=1, recent=5))
+    A.asap_check(ctx)
+    want = dst.clone().fill_(9.0)
+    for s, n in zip(start, lens):
+        e = R.evict(w[s:s + n].tolist(), pos[s:s + n].tolist(), 90, 1, 5)
+        at = torch.tensor(e) + s
+        assert torch.equal(dw[s:s + len(e)].cpu(), w[at]) and torch.equal(dp[s:s + len(e)].cpu(), pos[at])
+        assert torch.equal(dw[s + len(e):s + n].cpu(), w[s + len(e):s + n])
+        want[s:s + len(e)] = src[at.to(DEV)]
+    assert torch.equal(dst, want)
 
 
 @pytest.mark.parametrize("spoil", ["len", "start", "dst"])
