@@ -278,16 +278,17 @@ __device__ __forceinline__ int ca_admitted(int keys, int adm0, int causal, int t
 __device__ __forceinline__ bool ca_streamed(int R) { return R <= StreamWork::ROWS; }
 template <typename WORK>
 __device__ __forceinline__ int ca_together(int R, int kv) { return WORK::INDEX == 0 ? ca_heads(R, kv) : 1; }
-// key tiles of row tile rt; `hg` heads go together
+// key tiles of row tile rt; `hg` heads go together.  (A streamed segment has one row tile, whose last row admits every key.)
 template <typename WORK>
 __device__ __forceinline__ int ca_key_tiles(int R, int keys, int adm0, int causal, int rep, int hg, int rt) {
-  const int last = min((rt + 1) * WORK::ROWS, R) - 1, tile = WORK::KEYS / hg;
-  return (ca_admitted(keys, adm0, causal, causal ? last / rep : 0) + tile - 1) / tile;
+  if constexpr (WORK::INDEX == 0) return (keys * hg + WORK::KEYS - hg) / WORK::KEYS;
+  const int last = min((rt + 1) * WORK::ROWS, R) - 1;
+  return (ca_admitted(keys, adm0, causal, causal ? last / rep : 0) + WORK::KEYS - 1) / WORK::KEYS;
 }
 // numbers of the first `n` row tiles of a head
 template <typename WORK>
 __device__ __forceinline__ int ca_numbers(int R, int keys, int adm0, int causal, int rep, int hg, int n) {
-  if (!causal) return keys > 0 && n > 0 ? n * (ca_key_tiles<WORK>(R, keys, adm0, 0, rep, hg, 0) + WORK::EXTRA) : 0;
+  if (!causal || WORK::INDEX == 0) return keys > 0 && n > 0 ? n * (ca_key_tiles<WORK>(R, keys, adm0, 0, rep, hg, 0) + WORK::EXTRA) : 0;
   int t = 0;
   for (int rt = 0; rt < n; ++rt) {
     const int kt = ca_key_tiles<WORK>(R, keys, adm0, causal, rep, hg, rt);
@@ -337,11 +338,17 @@ struct CaWalk {
     }
     seg = lo;
     enter(a, segs);
-    const int per_head = (off[seg + 1] - off[seg]) * hg / a.kv;
     int u = t - off[seg];
+    if constexpr (WORK::INDEX == 0) {
+      const int per_head = key_tiles(a) + WORK::EXTRA, group = u / per_head;
+      pos = u - group * per_head;
+      head = group * hg;
+      rt = 0;
+      return;
+    }
+    const int per_head = (off[seg + 1] - off[seg]) / a.kv;
     head = u / per_head;
     u -= head * per_head;
-    head *= hg;
     for (rt = 0;; ++rt) {
       const int kt = key_tiles(a), n = kt > 0 ? kt + WORK::EXTRA : 0;
       if (u < n) break;
@@ -352,12 +359,7 @@ struct CaWalk {
   // the next item that has key tiles; false: none is left
   __device__ __forceinline__ bool next(const CacheArgs &a, const int *off, const CaSeg *segs, CaJob &j) {
     while (t < end) {
-      const int kt = key_tiles(a), p1 = min(kt + WORK::EXTRA, pos + (end - t));
-      const int k0 = max(0, pos - WORK::EXTRA), k1 = p1 - WORK::EXTRA, first = t - pos + WORK::EXTRA;
-      j.q0 = g.q0; j.R = R; j.row0 = g.row0; j.keys = g.keys; j.adm0 = g.keys - g.nq + 1; j.causal = causal; j.head = head; j.rt = rt; j.together = hg;
-      j.kt0 = k0; j.n = k1 - k0; j.complete = k0 == 0 && k1 == kt; j.record = 2 * piece + (first <= begin_t ? 0 : 1);
-      t += p1 - pos;
-      if (t < end) {                       // the next row tile that has keys
+      if (pos < 0) {                       // the row tile is done: the next one that has keys
         pos = 0;
         do {
           if (++rt >= ca_row_tiles<WORK>(g, a.rep)) {
@@ -370,7 +372,14 @@ struct CaWalk {
           }
         } while (key_tiles(a) == 0);
       }
-      if (k1 > k0) return true;
+      const int kt = key_tiles(a), p1 = min(kt + WORK::EXTRA, pos + (end - t));
+      const int k0 = max(0, pos - WORK::EXTRA), k1 = p1 - WORK::EXTRA, first = t - pos + WORK::EXTRA;
+      t += p1 - pos;
+      pos = -1;
+      if (k1 <= k0) continue;
+      j.q0 = g.q0; j.R = R; j.row0 = g.row0; j.keys = g.keys; j.adm0 = g.keys - g.nq + 1; j.causal = causal; j.head = head; j.rt = rt; j.together = hg;
+      j.kt0 = k0; j.n = k1 - k0; j.complete = k0 == 0 && k1 == kt; j.record = 2 * piece + (first <= begin_t ? 0 : 1);
+      return true;
     }
     return false;
   }
@@ -603,14 +612,7 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
       }
       __syncwarp();
       if (!more) break;
-      if (going && lane < j.R * j.together) {
-        const int sub = lane / j.R, i = lane - sub * j.R, t = i / a.rep;
-        const uint16_t *src = a.q + (long long)(j.q0 + t) * a.q_row + (long long)((j.head + sub) * a.rep + (i - t * a.rep)) * a.q_head;
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];"
-                     ::"r"(q_smem + slot * CA_Q_BYTES + lane * CA_Q_PITCH), "l"(src), "r"(jbar) : "memory");
-      }
-      __syncwarp();
-      for (int kt = j.kt0; kt < j.kt0 + j.n; ++kt, ++used) {
+      auto load_tile = [&](int kt) {
         if (used >= CA_STAGES) mbar_wait_warp(smem_u32(&bk->empty[pos.slot]), pos.phase ^ 1u, wc);
         if (!__shfl_sync(0xffffffffu, bk->abort_flag, 0)) {
           const uint32_t bar = smem_u32(&bk->full[pos.slot]), dst = base + pos.slot * CA_STAGE_BYTES;
@@ -620,8 +622,19 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
           tma_load_cache_w(dst + CA_STAGE_BYTES / 2, &maps.v[box], bar, row, j.head, leader);
           issued = used + 1;
         }
+        ++used;
         pos.step(CA_STAGES);
+      };
+      const bool early = used < CA_STAGES;       // (nothing to wait for)
+      if (early) load_tile(j.kt0);
+      if (going && lane < j.R * j.together) {
+        const int sub = lane / j.R, i = lane - sub * j.R, t = i / a.rep;
+        const uint16_t *src = a.q + (long long)(j.q0 + t) * a.q_row + (long long)((j.head + sub) * a.rep + (i - t * a.rep)) * a.q_head;
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];"
+                     ::"r"(q_smem + slot * CA_Q_BYTES + lane * CA_Q_PITCH), "l"(src), "r"(jbar) : "memory");
       }
+      __syncwarp();
+      for (int kt = j.kt0 + (early ? 1 : 0); kt < j.kt0 + j.n; ++kt) load_tile(kt);
     }
     // every copy issued has landed before the block leaves (the consumers wait for the query rows whatever happens)
     for (int s = 0; s < CA_STAGES; ++s) {

@@ -623,8 +623,10 @@ def test_prune_then_decode_with_eviction(ctx):
     A.asap_check(ctx)
 
 
-def test_a_wait_that_runs_out_is_reported_and_the_context_recovers(ctx):
-    c = Case(lens=[3000, 2000], nq=[1, 1], H=8, kv=8, dtype=torch.bfloat16, seed=16, weights=False)
+@pytest.mark.parametrize("nq", [[1, 1], [20, 40]], ids=["streamed", "tiles"])
+def test_a_wait_that_runs_out_is_reported_and_the_context_recovers(ctx, nq):
+    # (long enough that every block has more tiles than its ring holds: some wait cannot be satisfied at once)
+    c = Case(lens=[30000, 20000], nq=nq, H=32, kv=32, dtype=torch.bfloat16, seed=16, weights=False)
     c.run(ctx)
     good = c.out.clone()
     A.asap_debug_wait_limit(ctx, 1)
