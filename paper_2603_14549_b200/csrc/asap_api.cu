@@ -856,7 +856,7 @@ asap_status asap_init(asap_ctx **ctx_out, int device, size_t max_total_tokens, i
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_KEYS_BYTES);
   for (auto kernel : {ca_stream_kernel<false>, ca_stream_kernel<true>})
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ca_smem_bytes(CA_MAX_SEGMENTS));
-  for (auto kernel : {ca_tile_kernel<false>, ca_tile_kernel<true>})
+  for (auto kernel : {ca_tile_kernel<false, false>, ca_tile_kernel<false, true>, ca_tile_kernel<true, false>, ca_tile_kernel<true, true>})
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ct_smem_bytes(CA_MAX_SEGMENTS));
   if (e == cudaSuccess && ctx->sim_cluster) {
     // the cluster form of the sliced similarity launch needs eight co-resident blocks of up to 195 KB each in one

@@ -104,7 +104,7 @@ CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint
   const long long group_max = group_rows > 0 ? (group_rows < S ? group_rows : S) : 0, own_max = own_rows < S ? own_rows : S;
   const long long rows_max = group_max > own_max ? group_max : own_max;
   l.rec_rows = (int)(4 * rows_max < S ? 4 * rows_max : S);           // (as many heads together as make up to 16 rows)
-  l.too_large = streamed > CA_MAX_NUMBERS || tiled > CA_MAX_NUMBERS;
+  l.too_large = streamed > CA_MAX_NUMBERS || tiled > CA_MAX_NUMBERS || (long long)entries > CA_MAX_NUMBERS / 2;
   auto carve = [&](size_t bytes) {
     const size_t o = l.bytes;
     l.bytes = align_up(l.bytes + bytes, 256);
@@ -275,7 +275,7 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (layout.blocks[1]) {
     mark(ctx, "cache_tile", st);
-    launch_pdl(f16 ? ca_tile_kernel<true> : ca_tile_kernel<false>, dim3(layout.blocks[1]), dim3(CT_THREADS), ct_smem_bytes(p->B + p->n_groups), st,
+    launch_pdl(f16 ? (p->weights ? ca_tile_kernel<true, true> : ca_tile_kernel<true, false>) : (p->weights ? ca_tile_kernel<false, true> : ca_tile_kernel<false, false>), dim3(layout.blocks[1]), dim3(CT_THREADS), ct_smem_bytes(p->B + p->n_groups), st,
                tile_k, tile_v, a);
     ASAP_TRY(after_launch(ctx, "cache_tile"));
   }

@@ -188,8 +188,13 @@ constexpr int CA_Q_BYTES = StreamWork::ROWS * CA_Q_PITCH;
 constexpr int CA_MAX_SEGMENTS = 928;
 constexpr long long CA_WAIT_LIMIT = 2000000000LL;
 
-// Key / value heads that the streaming kernel takes together for segments of R stacked rows: at most 16 rows in all.
-__host__ __device__ __forceinline__ int ca_heads(int R, int kv) { return R <= 4 && kv % 4 == 0 ? 4 : R <= 8 && kv % 2 == 0 ? 2 : 1; }
+// Key / value heads that the streaming kernel takes together for segments of R stacked rows: at most 16 rows in all.  Long segments are taken
+// head by head: there is nothing to gain, and the heads of a piece would be spread over as many times more pieces for the join to add
+// up (5 sequences of 2000 to 60000 rows, four heads together 109 us, one 104).
+constexpr int CA_TOGETHER_KEYS = 4096;
+__device__ __forceinline__ int ca_heads(int R, int kv, int keys) {
+  return keys > CA_TOGETHER_KEYS ? 1 : R <= 4 && kv % 4 == 0 ? 4 : R <= 8 && kv % 2 == 0 ? 2 : 1;
+}
 
 // What the join has to know of a query row: its place in the prefix's and in its own segment.
 struct CaRowPart {
@@ -277,7 +282,7 @@ __device__ __forceinline__ int ca_group(const CacheArgs &a, int b) {
 __device__ __forceinline__ int ca_admitted(int keys, int adm0, int causal, int t) { return causal ? max(0, min(keys, adm0 + t)) : keys; }
 __device__ __forceinline__ bool ca_streamed(int R) { return R <= StreamWork::ROWS; }
 template <typename WORK>
-__device__ __forceinline__ int ca_together(int R, int kv) { return WORK::INDEX == 0 ? ca_heads(R, kv) : 1; }
+__device__ __forceinline__ int ca_together(int R, int kv, int keys) { return WORK::INDEX == 0 ? ca_heads(R, kv, keys) : 1; }
 // key tiles of row tile rt; `hg` heads go together.  (A streamed segment has one row tile, whose last row admits every key.)
 template <typename WORK>
 __device__ __forceinline__ int ca_key_tiles(int R, int keys, int adm0, int causal, int rep, int hg, int rt) {
@@ -325,7 +330,7 @@ struct CaWalk {
     g = segs[seg];
     R = g.nq * a.rep;
     causal = seg >= a.G;
-    hg = ca_together<WORK>(R, a.kv);
+    hg = ca_together<WORK>(R, a.kv, g.keys);
   }
   __device__ __forceinline__ void begin(const CacheArgs &a, const int *off, const CaSeg *segs, int n_seg, int number, int t0, int t1) {
     t = begin_t = t0; end = t1; piece = number;
@@ -397,7 +402,7 @@ __device__ __forceinline__ bool ca_plan(const CacheArgs &a, int *off, CaSeg *seg
     const CaSeg g = ca_segment(a, s, b);
     broken |= b;
     bad |= g.keys < 0;
-    const int R = g.nq * a.rep, hg = ca_together<WORK>(R, a.kv);
+    const int R = g.nq * a.rep, hg = ca_together<WORK>(R, a.kv, g.keys);
     const int n = a.kv / hg * ca_numbers<WORK>(R, g.keys, g.keys - g.nq + 1, s >= a.G, a.rep, hg, ca_row_tiles<WORK>(g, a.rep));
     segs[s] = g;
     off[s + 1] = n;
@@ -511,7 +516,7 @@ __device__ __forceinline__ void ca_describe_rows(const CacheArgs &a, const int *
         o1 = ld_prev(a.plan + n_seg + 2 + s);
       }
       part.R = R; part.i0 = (own.q0 - g.q0) * a.rep; part.keys = g.keys; part.adm0 = g.keys - g.nq + 1; part.causal = p;
-      part.off = o0; part.per_head = (o1 - o0) * (ca_streamed(R) ? ca_heads(R, a.kv) : 1) / a.kv;
+      part.off = o0; part.per_head = (o1 - o0) * (ca_streamed(R) ? ca_heads(R, a.kv, g.keys) : 1) / a.kv;
     }
     for (int r = thread; r < own.nq; r += threads) {
       CaRow mine = row;
@@ -1000,7 +1005,7 @@ __device__ __forceinline__ bool ct_passed(const CaJob &j, int rep, int kt) {
   return (kt + 1) * 128 > ca_admitted(j, j.causal ? j.rt * TileWork::ROWS / rep : 0);
 }
 
-template <bool F16>
+template <bool F16, bool WEIGHTS>
 __global__ void __launch_bounds__(CT_THREADS, 1)
 ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CacheArgs a) {
   extern __shared__ __align__(1024) uint8_t ct_smem[];
@@ -1282,7 +1287,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       const bool live = i_lo < j.R;               // the warp has rows
       const int qt = i / a.rep;
       const int adm = i < j.R ? ca_admitted(j, qt) : 0, adm_lo = live ? ca_admitted(j, i_lo / a.rep) : 0;
-      const long long entry = i < j.R ? (long long)(j.q0 + qt) * a.H + j.head * a.rep + (i - qt * a.rep) : -1;
+      const int entry = i < j.R ? (j.q0 + qt) * a.H + j.head * a.rep + (i - qt * a.rep) : -1;
       // p = 2^(x * scale - ref).  The reference is the maximum of the row's first key tile and then stays: one below the running
       // maximum only scales the sums.  Should a tile's sum outgrow the limit in some row of the warp, that tile is done again with the
       // row's true maximum as the new reference (O and the sum so far are rescaled).
@@ -1311,7 +1316,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
           for (int c = 0; c < 128; ++c)
             if (c >= lim) xr[c] = __float_as_uint(-INFINITY);
         }
-        if (a.logits) {
+        if constexpr (WEIGHTS) {
           // through shared memory, 16 columns at a time (16-byte chunk c of row r at c ^ ((r >> 1) & 3)): a store covers eight pieces of 64 bytes
 #pragma unroll
           for (int c0 = 0; c0 < 128; c0 += 16) {
@@ -1327,9 +1332,9 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
 #pragma unroll
             for (int r8 = 0; r8 < 32; r8 += 8) {
               const int rr = r8 + (lane >> 2), c = lane & 3;
-              const long long e = __shfl_sync(0xffffffffu, entry, rr);
+              const int e = __shfl_sync(0xffffffffu, entry, rr);
               const float4 v = *reinterpret_cast<const float4 *>(stage + rr * 64 + ((c ^ ((rr >> 1) & 3)) << 4));
-              if (e >= 0) *reinterpret_cast<float4 *>(a.logits + e * a.pitch + (j.causal ? a.own_off : 0) + j0 + c0 + 4 * c) = v;
+              if (e >= 0) *reinterpret_cast<float4 *>(a.logits + (long long)e * a.pitch + (j.causal ? a.own_off : 0) + j0 + c0 + 4 * c) = v;
             }
           }
           __syncwarp();
@@ -1406,7 +1411,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       if (!live) continue;
       // NaN in every logit leaves no maximum, but the row is not an empty one
       const bool none = n_act == 0 || (unset && l_run == 0.f), complete = j.complete != 0;
-      const long long at = i >= j.R ? -1 : complete ? (j.causal ? (long long)a.n_q * a.H : 0) + entry : (long long)j.record * TileWork::ROWS + g * 128 + lrow;
+      const int at = entry < 0 ? -1 : complete ? (j.causal ? a.n_q * a.H : 0) + entry : j.record * TileWork::ROWS + g * 128 + lrow;
       const bool write = !bk->abort_flag;
       if (at >= 0 && write) (complete ? a.full_ml : a.rec_ml[1])[at] = none ? make_float2(-INFINITY, 0.f) : make_float2(-neg_ref, l_run);
       if (n_act == 0) continue;
@@ -1440,9 +1445,9 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
 #pragma unroll
         for (int r8 = 0; r8 < 32; r8 += 8) {
           const int rr = r8 + (lane >> 2), c = lane & 3;
-          const long long e = __shfl_sync(0xffffffffu, at, rr);
+          const int e = __shfl_sync(0xffffffffu, at, rr);
           const uint4 x = *reinterpret_cast<const uint4 *>(stage + rr * 64 + ((c ^ ((rr >> 1) & 3)) << 4));
-          if (e >= 0 && write) *reinterpret_cast<uint4 *>(dst + e * 128 + c0 + 4 * c) = x;
+          if (e >= 0 && write) *reinterpret_cast<uint4 *>(dst + (long long)e * 128 + c0 + 4 * c) = x;
         }
       }
       tc_fence_before();                            // the next item's first P (and so its first P V) comes after these loads
@@ -1500,7 +1505,7 @@ struct CaParts {
 template <typename WORK>
 __device__ __forceinline__ CaParts ca_parts_of(const CacheArgs &a, const CaRowPart &p, int which, int all, long long entry, int kvh, int sub) {
   CaParts out;
-  const int hg = ca_together<WORK>(p.R, a.kv), i = p.i0 + sub, rt = i / WORK::ROWS;
+  const int hg = ca_together<WORK>(p.R, a.kv, p.keys), i = p.i0 + sub, rt = i / WORK::ROWS;
   const int r = i - rt * WORK::ROWS + (hg > 1 ? (kvh & (hg - 1)) * p.R : 0);
   const int kt = ca_key_tiles<WORK>(p.R, p.keys, p.adm0, p.causal, a.rep, hg, rt);
   const int chunk = ca_chunk(all, a.pieces[WORK::INDEX]), rec_rows = WORK::INDEX == 0 ? a.rec_rows : WORK::ROWS;
