@@ -140,6 +140,20 @@ bool make_cache_map(asap_ctx *ctx, CUtensorMap *map, const void *ptr, const asap
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Queries [n_q, H, 128] as five dimensions (64 columns, head of a key / value head, query row, column half, key / value head); box = a row
+// tile of 128 stacked rows.  For H / kv_heads a divisor of 128.
+bool make_query_map(asap_ctx *ctx, CUtensorMap *map, const asap_cache_attention_args *p) {
+  const cuuint64_t rep = p->H / p->kv_heads;
+  cuuint64_t dims[5] = {64, rep, (cuuint64_t)p->n_q, 2, (cuuint64_t)p->kv_heads};
+  const cuuint64_t row = p->n_q > 1 ? p->q_row : 128, head = p->H > 1 ? p->q_head : 128;
+  cuuint64_t strides[4] = {head * 2, row * 2, 128, rep * head * 2};
+  cuuint32_t box[5] = {64, (cuuint32_t)rep, 128 / (cuuint32_t)rep, 2, 1};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  return ctx->encode(map, p->dtype == ASAP_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(p->q),
+                     dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace
 
 extern "C" {
@@ -254,13 +268,18 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0 || scratch_bytes < layout.bytes)
     return fail(ctx, ASAP_ERR_WORKSPACE, "asap_cache_attention: scratch is null, not 256-byte aligned or smaller than asap_cache_attention_scratch_bytes");
   CaMaps maps;
-  CUtensorMap tile_k, tile_v;
+  CUtensorMap tile_k = {}, tile_v = {}, tile_q = {};
   bool made = true;
   for (int b = 0; b < 3; ++b) {                  // (boxes of more heads than there are stand unused)
     const uint32_t heads = p->kv_heads >= 1 << b ? 1u << b : 1u;
     made = made && make_cache_map(ctx, &maps.k[b], p->k, p, StreamWork::KEYS / heads, heads) && make_cache_map(ctx, &maps.v[b], p->v, p, StreamWork::KEYS / heads, heads);
   }
   if (layout.blocks[1]) made = made && make_cache_map(ctx, &tile_k, p->k, p, TileWork::KEYS, 1) && make_cache_map(ctx, &tile_v, p->v, p, TileWork::KEYS, 1);
+  // (rows or heads that share an address, as a broadcast view has them, are gathered)
+  const int rep = p->H / p->kv_heads;
+  a.q_tiled = layout.blocks[1] && 128 % rep == 0 && (p->n_q == 1 || p->q_row >= 128) && (p->H == 1 || p->q_head >= 128);
+  tile_q = tile_k;
+  if (a.q_tiled) made = made && make_query_map(ctx, &tile_q, p);
   if (!made) return fail(ctx, ASAP_ERR_CUDA, "cuTensorMapEncodeTiled failed for k / v");
   a.B = p->B; a.G = p->n_groups; a.H = p->H; a.kv = p->kv_heads; a.rep = p->H / p->kv_heads;
   a.n_q = p->n_q; a.max_q = p->max_q; a.max_len = p->max_len; a.max_prefix = p->max_prefix; a.cache_rows = p->cache_rows;
@@ -276,7 +295,7 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   if (layout.blocks[1]) {
     mark(ctx, "cache_tile", st);
     launch_pdl(f16 ? (p->weights ? ca_tile_kernel<true, true> : ca_tile_kernel<true, false>) : (p->weights ? ca_tile_kernel<false, true> : ca_tile_kernel<false, false>), dim3(layout.blocks[1]), dim3(CT_THREADS), ct_smem_bytes(p->B + p->n_groups), st,
-               tile_k, tile_v, a);
+               tile_k, tile_v, tile_q, a);
     ASAP_TRY(after_launch(ctx, "cache_tile"));
   }
   mark(ctx, "cache_stream", st);

@@ -174,7 +174,7 @@ struct StreamWork {
   static constexpr int ROWS = 16, KEYS = 64, EXTRA = 2, INDEX = 0;
 };
 struct TileWork {
-  static constexpr int ROWS = 256, KEYS = 128, EXTRA = 3, INDEX = 1;
+  static constexpr int ROWS = 256, KEYS = 128, EXTRA = 4, INDEX = 1;
 };
 constexpr int CA_CONSUMERS = 4;                           // warps; each takes 16 keys of a tile
 constexpr int CA_THREADS = 32 * (CA_CONSUMERS + 1);       // and the copying warp
@@ -223,6 +223,7 @@ struct CacheArgs {
                                            // them 0 if the call is skipped
   int pieces[2];                           // pieces of the two kernels' work; 0: the kernel is not launched
   unsigned int *work;                      // [2] pieces drawn / blocks done; both zero between launches
+  int q_tiled;                             // rep divides 128: a row tile of query rows is one tiled copy
   int rec_rows;                            // rows of a streamed piece's partial result, those of all heads that go together
   CaRow *rows;                             // [n_q]
   float2 *rec_ml[2], *full_ml;             // partial results: two per piece and row of a row tile; [2][n_q * H] (prefix, own) complete ones
@@ -466,6 +467,16 @@ __device__ __forceinline__ void tma_load_cache_w(uint32_t smem_dst, const void *
       ::"r"(smem_dst), "l"(tmap), "r"(bar), "r"(0), "r"(row), "r"(head), "r"(leader)
       : "memory");
 }
+// A row tile of stacked query rows as [column half][query row][head of the key / value head][64 columns].
+__device__ __forceinline__ void tma_load_query_w(uint32_t smem_dst, const void *tmap, uint32_t bar, int32_t row, int32_t head, uint32_t leader) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %3, %4, %3, %5}], [%2];\n\t}"
+      ::"r"(smem_dst), "l"(tmap), "r"(bar), "r"(0), "r"(row), "r"(head), "r"(leader)
+      : "memory");
+}
+
 // Non-zero if either half is an infinity or NaN: an exponent of all ones, plus one, carries into the sign's place.
 template <bool F16>
 __device__ __forceinline__ uint32_t not_finite_bits(uint32_t w) {
@@ -1007,7 +1018,8 @@ __device__ __forceinline__ bool ct_passed(const CaJob &j, int rep, int kt) {
 
 template <bool F16, bool WEIGHTS>
 __global__ void __launch_bounds__(CT_THREADS, 1)
-ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CacheArgs a) {
+ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CUtensorMap tmap_q,
+               const __grid_constant__ CacheArgs a) {
   extern __shared__ __align__(1024) uint8_t ct_smem[];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t base = smem_u32(ct_smem), q_smem = base, ring = base + 2 * CT_TILE_BYTES;
@@ -1229,8 +1241,11 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       }
     } else {
       // ---------------------------------------------------------------- query rows
-      // (gathered: stacked row i is query row i / rep, head i % rep of the key / value head; rows past the last one keep whatever the
-      // buffer holds, nothing of theirs is used).  A lane works out the addresses of four rows; sixteen lanes copy a row.
+      // Stacked row i is query row i / rep, head i % rep of the key / value head; rows past the last one hold anything (other sequences' query
+      // rows, or what the buffer held), nothing of theirs is used.  One tiled copy where rep divides 128 (see make_query_map); otherwise
+      // gathered, a lane working out the addresses of four rows and sixteen lanes copying a row, which takes about 4000 clocks.
+      const uint32_t leader = warp_leader();
+      int tiled[2] = {0, 0};                      // tiled copies issued
       int qc[2] = {0, 0};
       CaJob j;
       for (int jc = 0; take(jc, j); ++jc) {
@@ -1241,6 +1256,15 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
           if (g) ++qc[1];
           else ++qc[0];
           const int i0 = j.rt * TileWork::ROWS + g * 128, n = min(128, j.R - i0);
+          if (a.q_tiled) {
+            if (!__shfl_sync(0xffffffffu, bk->abort_flag, 0)) {
+              mbar_expect_tx_w(smem_u32(&bk->q_full[g]), CT_TILE_BYTES, leader);
+              tma_load_query_w(q_smem + g * CT_TILE_BYTES, &tmap_q, smem_u32(&bk->q_full[g]), j.q0 + i0 / a.rep, j.head, leader);
+              if (g) tiled[1] = qc[1];
+              else tiled[0] = qc[0];
+            }
+            continue;
+          }
           const int c = lane & 15;                // 16-byte piece of a row
           long long from[4];
 #pragma unroll
@@ -1266,6 +1290,10 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
           mbar_arrive_lane0(smem_u32(&bk->q_full[g]), lane);
         }
       }
+      // every copy issued has landed before the block leaves
+      for (int g = 0; g < 2; ++g)
+        if ((g ? tiled[1] : tiled[0]) > 0) mbar_wait_drain(smem_u32(&bk->q_full[g]), ((g ? tiled[1] : tiled[0]) - 1) & 1, CA_WAIT_LIMIT);
+      __syncwarp();
     }
   } else {
     reg_inc<216>();
@@ -1417,17 +1445,19 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       if (n_act == 0) continue;
       float *dst = complete ? a.full_o : a.rec_o[1];
       const bool bad = *reinterpret_cast<volatile int *>(&bk->bad[jc & 3]) != 0;
+      // (A thread stores its own row, 32 bytes at a time: whole sectors.  Through shared memory in pieces of 32 rows x 16 columns it took half as
+      // long again.)
 #pragma unroll 1
-      for (int c0 = 0; c0 < 128; c0 += 16) {
-        uint32_t r[16];
-        tmem_ld16(o_addr + c0, r);
+      for (int c0 = 0; c0 < 128; c0 += 32) {
+        uint32_t r[32];
+        tmem_ld32(o_addr + c0, r);
         tmem_wait_ld();
         if (bad) {                                  // what warp 2 left out
           const int from = max(j.kt0 * 128, ca_admitted(j, j.causal ? j.rt * TileWork::ROWS / a.rep : 0)), to = min((j.kt0 + j.n) * 128, adm);
           for (int key = from; key < to; ++key) {
             const uint16_t *v = a.v + (long long)(j.row0 + key) * a.kv_row + (long long)j.head * a.kv_head + c0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 16; ++e) {
               uint32_t w;
               asm volatile("ld.global.u32 %0, [%1];" : "=r"(w) : "l"(v + 2 * e));
               const float2 x = unpack2_t<F16>(w);
@@ -1437,18 +1467,15 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
           }
           __syncwarp();
         }
-        __syncwarp();                               // the previous piece has been read
+        if (at >= 0 && write) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          *reinterpret_cast<uint4 *>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(r[4 * c], r[4 * c + 1], r[4 * c + 2], r[4 * c + 3]);
-        __syncwarp();
-#pragma unroll
-        for (int r8 = 0; r8 < 32; r8 += 8) {
-          const int rr = r8 + (lane >> 2), c = lane & 3;
-          const int e = __shfl_sync(0xffffffffu, at, rr);
-          const uint4 x = *reinterpret_cast<const uint4 *>(stage + rr * 64 + ((c ^ ((rr >> 1) & 3)) << 4));
-          if (e >= 0 && write) *reinterpret_cast<uint4 *>(dst + (long long)e * 128 + c0 + 4 * c) = x;
+          for (int c = 0; c < 32; c += 8)
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                         ::"l"(dst + (long long)at * 128 + c0 + c), "r"(r[c]), "r"(r[c + 1]), "r"(r[c + 2]), "r"(r[c + 3]), "r"(r[c + 4]), "r"(r[c + 5]),
+                           "r"(r[c + 6]), "r"(r[c + 7])
+                         : "memory");
         }
+        __syncwarp();
       }
       tc_fence_before();                            // the next item's first P (and so its first P V) comes after these loads
     }
