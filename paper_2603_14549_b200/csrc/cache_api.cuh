@@ -306,8 +306,11 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   // (one wave of the split form: 1 x 32 heads 14 -> 8 us, 5 rows of up to 150 partial results 17 -> 8; 128 rows 21 -> 62)
   const bool split = (long long)p->n_q * ((p->H + CA_JOIN_SPLIT_HEADS - 1) / CA_JOIN_SPLIT_HEADS) <= 2LL * ctx->num_sms;
   const int heads = split ? CA_JOIN_SPLIT_HEADS : CA_JOIN_HEADS;
-  launch_pdl(f16 ? (split ? ca_join_kernel<true, true> : ca_join_kernel<true, false>) : (split ? ca_join_kernel<false, true> : ca_join_kernel<false, false>),
-             dim3(p->n_q, (p->H + heads - 1) / heads), dim3(CA_JOIN_THREADS), 0, st, a);
+  const bool many = !split && p->n_q >= 4 * ctx->num_sms;
+  const int rows = many ? 4 : 1;
+  launch_pdl(f16 ? (split ? ca_join_kernel<true, true, 1> : many ? ca_join_kernel<true, false, 4> : ca_join_kernel<true, false, 1>)
+                 : (split ? ca_join_kernel<false, true, 1> : many ? ca_join_kernel<false, false, 4> : ca_join_kernel<false, false, 1>),
+             dim3((p->n_q + rows - 1) / rows, (p->H + heads - 1) / heads), dim3(CA_JOIN_THREADS), 0, st, a);
   ASAP_TRY(after_launch(ctx, "cache_join"));
   if (p->weights) {
     const int own_lanes = (long long)p->max_q * p->H <= 64 ? 64 : 16, pre_lanes = 16;

@@ -71,7 +71,8 @@ rope_kernel(const __grid_constant__ RopeArgs a) {
   pdl_enter();
   const int row0 = blockIdx.x * a.rows_per_block;
   const int rows = min(a.rows_per_block, a.n_rows - row0);
-  for (int i = threadIdx.x; i < rows * a.n_pairs; i += ROPE_THREADS) {
+  const RopeTensor &t = a.t[blockIdx.y];
+  for (int i = threadIdx.x; t.rotate && i < rows * a.n_pairs; i += ROPE_THREADS) {
     const int r = i / a.n_pairs, p = i - r * a.n_pairs;
     const long long pos = ld_prev(a.pos + row0 + r);
     const unsigned long long turn = (unsigned long long)pos * a.turns[p];
@@ -91,7 +92,6 @@ rope_kernel(const __grid_constant__ RopeArgs a) {
   }
   __syncthreads();
   const int P = a.n_pairs, rot = 2 * P;
-  const RopeTensor &t = a.t[blockIdx.y];
   // tasks of a head: rotated pieces first, then pieces that pass through
   const int n_rot = t.rotate ? (VEC ? (a.interleaved ? P / 4 : P / 8) : P) : 0;
   const int n_pass = VEC ? (a.head_dim - (t.rotate ? rot : 0)) / 8 : a.head_dim - (t.rotate ? rot : 0);
@@ -1491,8 +1491,9 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
 // ---------------------------------------------------------------------------------------
 // Partial results of a (query row, head) -> output, four of the 128 values a lane.  A thread works out where the partial results of one (head,
 // prefix or own rows) lie.  (With the addresses worked out by every warp for itself the kernel was bound by those instructions: 2254
-// rows x 32 heads 67 us.)  Two forms: with many rows a block takes 32 heads of a query row, a warp two of them; with few (SPLIT) a
-// block takes two heads and eight warps share the partial results of one, of which a long sequence has a hundred or more.
+// rows x 32 heads 67 us.)  Three forms: a block takes 32 heads of ROWS query rows, a warp two at a time (four rows where there are enough of
+// them: 2254 x 32 heads 41 us -> 25); with few rows (SPLIT) it takes two heads, and eight warps share the partial results of one, of which
+// a long sequence has a hundred or more.
 // ---------------------------------------------------------------------------------------
 constexpr int CA_JOIN_THREADS = 512, CA_JOIN_WARPS = CA_JOIN_THREADS / 32;
 constexpr int CA_JOIN_HEADS = 32, CA_JOIN_SPLIT_HEADS = 2;
@@ -1561,40 +1562,49 @@ __device__ __forceinline__ void ca_finish_row(const CacheArgs &a, const CaSum &s
   }
 }
 
-template <bool F16, bool SPLIT>
-__global__ void __launch_bounds__(CA_JOIN_THREADS)
+template <bool F16, bool SPLIT, int ROWS>
+__global__ void __launch_bounds__(CA_JOIN_THREADS, 2)
 ca_join_kernel(const __grid_constant__ CacheArgs a) {
   constexpr int HEADS = SPLIT ? CA_JOIN_SPLIT_HEADS : CA_JOIN_HEADS;
-  __shared__ CaParts sh_parts[HEADS][2];
+  __shared__ CaParts sh_parts[ROWS * HEADS][2];
+  __shared__ int sh_valid[ROWS];
   __shared__ float4 sh_acc[SPLIT ? CA_JOIN_WARPS : 1][32];
   __shared__ float2 sh_ml[SPLIT ? CA_JOIN_WARPS : 1];
   pdl_enter();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, qr = blockIdx.x, n_seg = a.G + a.B, h0 = blockIdx.y * HEADS;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_seg = a.G + a.B, h0 = blockIdx.y * HEADS;
   // every query row of [q_cu[0], q_cu[B]) has an entry of this call unless the call is skipped
   const uint32_t status = *reinterpret_cast<volatile uint32_t *>(a.status);
   const int q0 = a.q_cu ? ld_prev(a.q_cu) : 0, q1 = a.q_cu ? ld_prev(a.q_cu + a.B) : a.n_q, going = ld_prev(a.plan + 2 * (n_seg + 1));
-  const int valid = ld_prev(&a.rows[qr].valid);
-  if (threadIdx.x < 2 * HEADS) {
-    const int h = h0 + (threadIdx.x >> 1), p = threadIdx.x & 1;
-    const CaRowPart *src = &a.rows[qr].part[p];
-    CaRowPart part;
-    part.i0 = ld_prev(&src->i0); part.R = ld_prev(&src->R); part.adm0 = ld_prev(&src->adm0); part.causal = ld_prev(&src->causal);
-    part.keys = ld_prev(&src->keys); part.off = ld_prev(&src->off); part.per_head = ld_prev(&src->per_head);
-    const int all0 = ld_prev(a.plan + n_seg), all1 = a.pieces[1] ? ld_prev(a.plan + 2 * n_seg + 1) : 0;
+  static_assert(ROWS * HEADS * 2 <= CA_JOIN_THREADS, "a thread per (query row, head, part)");
+  if (threadIdx.x < ROWS * HEADS * 2) {
+    const int qr = blockIdx.x * ROWS + threadIdx.x / (2 * HEADS), h = h0 + (threadIdx.x >> 1) % HEADS, p = threadIdx.x & 1;
     CaParts mine;
     mine.n = 0;
-    if (h < a.H && going && valid == 1 && qr >= q0 && qr < q1 && part.R > 0) {
-      const int kvh = h / a.rep, sub = h - kvh * a.rep;
-      const long long entry = (long long)qr * a.H + h;
-      mine = ca_streamed(part.R) ? ca_parts_of<StreamWork>(a, part, p, all0, entry, kvh, sub) : ca_parts_of<TileWork>(a, part, p, all1, entry, kvh, sub);
+    int valid = -1;                              // not this call's row
+    if (qr < a.n_q) {
+      const CaRowPart *src = &a.rows[qr].part[p];
+      const int entry_valid = ld_prev(&a.rows[qr].valid);
+      CaRowPart part;
+      part.i0 = ld_prev(&src->i0); part.R = ld_prev(&src->R); part.adm0 = ld_prev(&src->adm0); part.causal = ld_prev(&src->causal);
+      part.keys = ld_prev(&src->keys); part.off = ld_prev(&src->off); part.per_head = ld_prev(&src->per_head);
+      const int all0 = ld_prev(a.plan + n_seg), all1 = a.pieces[1] ? ld_prev(a.plan + 2 * n_seg + 1) : 0;
+      if (going && qr >= q0 && qr < q1 && !(status & STATUS_CACHE_TIMEOUT)) {
+        valid = entry_valid;
+        if (h < a.H && valid == 1 && part.R > 0) {
+          const int kvh = h / a.rep, sub = h - kvh * a.rep;
+          const long long entry = (long long)qr * a.H + h;
+          mine = ca_streamed(part.R) ? ca_parts_of<StreamWork>(a, part, p, all0, entry, kvh, sub) : ca_parts_of<TileWork>(a, part, p, all1, entry, kvh, sub);
+        }
+      }
     }
     sh_parts[threadIdx.x >> 1][p] = mine;
+    if (threadIdx.x % (2 * HEADS) == 0) sh_valid[threadIdx.x / (2 * HEADS)] = valid;
   }
   __syncthreads();
-  if ((status & STATUS_CACHE_TIMEOUT) || !going || qr < q0 || qr >= q1) return;
-  if (valid != 1) {                              // a row of a sequence that is skipped
-    if (threadIdx.x < HEADS && h0 + (int)threadIdx.x < a.H) a.lse2[(long long)qr * a.H + h0 + threadIdx.x] = INFINITY;
-    return;
+  // a row of a sequence that is skipped adds no weight
+  if (threadIdx.x < ROWS * HEADS) {
+    const int r = threadIdx.x / HEADS, h = h0 + threadIdx.x % HEADS;
+    if (sh_valid[r] == 0 && h < a.H) a.lse2[(long long)(blockIdx.x * ROWS + r) * a.H + h] = INFINITY;
   }
   if constexpr (SPLIT) {
     constexpr int SHARE = CA_JOIN_WARPS / HEADS;
@@ -1620,47 +1630,50 @@ ca_join_kernel(const __grid_constant__ CacheArgs a) {
     sh_acc[warp][lane] = s.acc;
     if (lane == 0) sh_ml[warp] = make_float2(s.top, s.sum);
     __syncthreads();
-    if (w != 0 || h0 + e >= a.H) return;
+    if (w != 0 || h0 + e >= a.H || sh_valid[0] != 1) return;
     for (int k = 1; k < SHARE; ++k) s.add(sh_ml[warp + k], sh_acc[warp + k][lane]);
-    ca_finish_row<F16>(a, s, qr, h0 + e, lane);
+    ca_finish_row<F16>(a, s, blockIdx.x, h0 + e, lane);
   } else {
-    constexpr int MINE = HEADS / CA_JOIN_WARPS;
-    float2 ml[MINE][2];
-    float4 o[MINE][2];
+    constexpr int MINE = 2;                      // (query row, head) pairs of a warp whose first loads are under way together
+#pragma unroll 1
+    for (int e0 = warp * MINE; e0 < ROWS * HEADS; e0 += CA_JOIN_WARPS * MINE) {
+      float2 ml[MINE][2];
+      float4 o[MINE][2];
 #pragma unroll
-    for (int x = 0; x < MINE; ++x)
+      for (int x = 0; x < MINE; ++x)
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const CaParts &c = sh_parts[warp + x * CA_JOIN_WARPS][p];
-        if (c.n == 0) continue;
-        ml[x][p] = ld_prev2f(c.ml + c.first);
-        o[x][p] = ld_prev4f(c.o + c.first * 128 + lane * 4);
-      }
-#pragma unroll
-    for (int x = 0; x < MINE; ++x) {
-      const int e = warp + x * CA_JOIN_WARPS;
-      if (h0 + e >= a.H) break;
-      CaSum s;
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const CaParts &c = sh_parts[e][p];
-        if (c.n == 0) continue;
-        s.add(ml[x][p], o[x][p]);
-        for (int k0 = 1; k0 < c.n; k0 += 4) {
-          float2 m4[4];
-          float4 o4[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const long long at = c.at(min(k0 + k, c.n - 1));
-            m4[k] = ld_prev2f(c.ml + at);
-            o4[k] = ld_prev4f(c.o + at * 128 + lane * 4);
-          }
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (k0 + k < c.n) s.add(m4[k], o4[k]);
+        for (int p = 0; p < 2; ++p) {
+          const CaParts &c = sh_parts[e0 + x][p];
+          if (c.n == 0) continue;
+          ml[x][p] = ld_prev2f(c.ml + c.first);
+          o[x][p] = ld_prev4f(c.o + c.first * 128 + lane * 4);
         }
+#pragma unroll
+      for (int x = 0; x < MINE; ++x) {
+        const int e = e0 + x, r = e / HEADS, h = h0 + e % HEADS;
+        if (h >= a.H || sh_valid[r] != 1) continue;
+        CaSum s;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const CaParts &c = sh_parts[e][p];
+          if (c.n == 0) continue;
+          s.add(ml[x][p], o[x][p]);
+          for (int k0 = 1; k0 < c.n; k0 += 4) {
+            float2 m4[4];
+            float4 o4[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const long long at = c.at(min(k0 + k, c.n - 1));
+              m4[k] = ld_prev2f(c.ml + at);
+              o4[k] = ld_prev4f(c.o + at * 128 + lane * 4);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (k0 + k < c.n) s.add(m4[k], o4[k]);
+          }
+        }
+        ca_finish_row<F16>(a, s, blockIdx.x * ROWS + r, h, lane);
       }
-      ca_finish_row<F16>(a, s, qr, h0 + e, lane);
     }
   }
 }
