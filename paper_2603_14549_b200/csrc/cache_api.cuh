@@ -302,6 +302,14 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   launch_pdl(f16 ? ca_stream_kernel<true> : ca_stream_kernel<false>, dim3(layout.blocks[0]), dim3(CA_THREADS), ca_smem_bytes(p->B + p->n_groups), st,
              maps, a);
   ASAP_TRY(after_launch(ctx, "cache_stream"));
+  const bool few = p->weights && p->n_groups == 0 && (long long)p->max_q * p->H <= CA_FEW_PAIRS && p->max_len > 0;
+  a.join_behind = few ? 1 : 0;
+  if (few) {
+    const long long own = (p->max_len + 4 * CA_FEW_LANES - 1) / (4 * CA_FEW_LANES);
+    mark(ctx, "cache_weight", st);
+    launch_pdl(ca_weight_few_kernel, dim3((unsigned)(own * p->B)), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)own);
+    ASAP_TRY(after_launch(ctx, "cache_weight"));
+  }
   mark(ctx, "cache_join", st);
   // (one wave of the split form: 1 x 32 heads 14 -> 8 us, 5 rows of up to 150 partial results 17 -> 8; 128 rows 21 -> 62)
   const bool split = (long long)p->n_q * ((p->H + CA_JOIN_SPLIT_HEADS - 1) / CA_JOIN_SPLIT_HEADS) <= 2LL * ctx->num_sms;
@@ -312,7 +320,7 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
                  : (split ? ca_join_kernel<false, true, 1> : many ? ca_join_kernel<false, false, 4> : ca_join_kernel<false, false, 1>),
              dim3((p->n_q + rows - 1) / rows, (p->H + heads - 1) / heads), dim3(CA_JOIN_THREADS), 0, st, a);
   ASAP_TRY(after_launch(ctx, "cache_join"));
-  if (p->weights) {
+  if (p->weights && !few) {
     const int own_lanes = (long long)p->max_q * p->H <= 64 ? 64 : 16, pre_lanes = 16;
     const long long pre = (p->max_prefix + 4 * pre_lanes - 1) / (4 * pre_lanes), own = (p->max_len + 4 * own_lanes - 1) / (4 * own_lanes);
     const long long blocks = pre * p->n_groups + own * p->B;
