@@ -196,6 +196,12 @@ CASES = {
     "prefix_only": dict(lens=[0, 0, 0], nq=[1, 3, 1], H=4, kv=1, groups=[(0, 3, 129)]),
     "many_items": dict(lens=[150, 40, 70, 200, 33, 256], nq=[150, 33, 70, 181, 33, 130], H=24, kv=24, groups=[(0, 2, 300), (2, 6, 1000)]),
     "many_items_gqa": dict(lens=[100] * 30, nq=[17] * 30, H=32, kv=8, groups=[(0, 30, 700)]),
+    "tiles_of_an_odd_ratio": dict(lens=[60, 200], nq=[5, 9], H=14, kv=2, groups=[(0, 2, 400)]),
+    "sixteen_rows": dict(lens=[30] * 16, nq=[1] * 16, H=4, kv=4, groups=[(0, 16, 3000)]),
+    "nine_rows_each": dict(lens=[700, 45, 9], nq=[9, 9, 9], H=4, kv=4),
+    "two_heads_together": dict(lens=[500, 17, 4500], nq=[2, 3, 1], H=12, kv=4),
+    "four_heads_together": dict(lens=[500, 33, 15, 16, 17, 5000], nq=[1] * 6, H=16, kv=8),
+    "sixty_four_pairs": dict(lens=[300, 1, 64, 1025], nq=[2, 1, 2, 2], H=32, kv=8),
     "late_rows": dict(lens=[2, 1], nq=[9, 5], H=2, kv=2, groups=[(0, 2, 70)]),
 }
 
@@ -363,6 +369,87 @@ def test_capture_replay_and_another_stream(ctx):
     A.asap_cache_attention(ctx, args, scratch, other)
     other.synchronize()
     assert torch.equal(first, c.out)
+
+
+def test_a_padded_batch(ctx):
+    """Query rows behind the last sequence's, as a batch of fixed size has them, stay as they are, whatever they hold."""
+    c = Case(lens=[100, 31, 64], nq=[1, 2, 20], H=4, kv=2, dtype=torch.bfloat16, seed=21, groups=[(0, 2, 90)])
+    c.run(ctx)
+    first = (c.out.clone(), c.lse.clone())
+    d = Case(lens=[100, 31, 64], nq=[1, 2, 20], H=4, kv=2, dtype=torch.bfloat16, seed=21, groups=[(0, 2, 90)])
+    pad = torch.full((5, 4, HEAD), float("nan"), dtype=torch.bfloat16, device=DEV)
+    d.q = torch.cat([c.q, pad])
+    d.out, d.lse = torch.full((28, 4, HEAD), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((28, 4), 7.0, device=DEV)
+    d.run(ctx)
+    A.asap_check(ctx)
+    assert torch.equal(d.out[:23], first[0]) and torch.equal(d.lse[:23], first[1]) and torch.equal(d.weights, c.weights)
+    assert (d.out[23:] == 7).all() and (d.lse[23:] == 7).all()
+
+
+@pytest.mark.parametrize("spoil", ["q_cu", "group_cu"])
+def test_offsets_that_do_not_ascend_skip_the_call(ctx, spoil):
+    c = Case(lens=[100, 31, 64, 20], nq=[2, 3, 1, 40], H=4, kv=2, dtype=torch.bfloat16, seed=22, groups=[(0, 1, 50), (1, 4, 70)])
+    base = c.weights.clone()
+    if spoil == "q_cu":
+        c.dev["q_cu"][2] = 1
+    else:
+        c.dev["group_cu"].copy_(i32([2, 1, 4]))
+    c.run(ctx)
+    with pytest.raises(A.AsapError) as e:
+        A.asap_check(ctx)
+    assert e.value.status == -6
+    assert (c.out == 7).all() and (c.lse == 7).all() and torch.equal(c.weights, base)
+
+
+def test_two_contexts_on_two_streams(ctx):
+    """Calls on contexts and scratch of their own may overlap."""
+    other = A.asap_init(0, 64, 1, 1, HEAD)
+    try:
+        cases = [Case(lens=[900, 70, 400], nq=[1, 1, 1], H=32, kv=8, dtype=torch.bfloat16, seed=s, groups=[(0, 3, 800)]) for s in (23, 24)]
+        for c in cases:
+            c.run(ctx)
+        A.asap_check(ctx)
+        want = [(c.out.clone(), c.lse.clone()) for c in cases]
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        work = []
+        for c, x in zip(cases, (ctx, other)):
+            args = c.args()
+            work.append((args, torch.empty(A.asap_cache_attention_scratch_bytes(x, args), dtype=torch.uint8, device=DEV), x))
+            c.out.fill_(7)
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for (args, scratch, x), s in zip(work, streams):
+                A.asap_cache_attention(x, args, scratch, s)
+        for (_, _, x), s in zip(work, streams):
+            A.asap_check(x, s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(c.out, w[0]) and torch.equal(c.lse, w[1]) for c, w in zip(cases, want))
+    finally:
+        A.asap_free(other)
+
+
+def test_back_to_back_calls_of_different_shapes(ctx):
+    """Calls that follow each other without a wait, through the same scratch: each launch sequence keeps out of the way of the one before."""
+    cases = [Case(**CASES[n], dtype=torch.bfloat16, seed=30 + i) for i, n in enumerate(["many_items", "groups", "many_splits", "one_row", "sixteen_rows",
+                                                                                       "four_heads_together", "whole_prompt", "prefix_only"])]
+    args = [c.args() for c in cases]
+    scratch = torch.empty(max(A.asap_cache_attention_scratch_bytes(ctx, a) for a in args), dtype=torch.uint8, device=DEV)
+    want = []
+    for c, a in zip(cases, args):
+        A.asap_cache_attention(ctx, a, scratch)
+        A.asap_check(ctx)
+        want.append((c.out.clone(), c.lse.clone()))
+    rng = random.Random(31)
+    for _ in range(6):
+        order = list(range(len(cases)))
+        rng.shuffle(order)
+        for c in cases:
+            c.out.fill_(7)
+        for i in order:
+            A.asap_cache_attention(ctx, args[i], scratch)
+        torch.cuda.synchronize()
+        assert all(torch.equal(c.out, w[0]) and torch.equal(c.lse, w[1]) for c, w in zip(cases, want))
+    A.asap_check(ctx)
 
 
 def test_offsets_past_32_bits(ctx):
