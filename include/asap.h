@@ -303,7 +303,7 @@ typedef struct {
   int32_t B, H, kv_heads, head_dim, dtype;  /* head_dim must be 128; kv_heads divides H */
   int32_t n_q;                              /* rows of q and out; q_cu[B] may be smaller, the rows behind it stay as they are */
   int32_t max_q, max_len, max_prefix;       /* host-known bounds of the query rows, own rows and prefix rows */
-  int32_t n_groups;                         /* 0: no prefixes.  B + n_groups <= 928 */
+  int32_t n_groups;                         /* 0: no prefixes.  B + n_groups <= 1024 */
   int32_t cache_rows;                       /* rows of k and v */
   float scale;                              /* 0: 1 / sqrt(head_dim) */
   int64_t q_row, q_head, out_row, out_head, kv_row, kv_head;  /* strides, multiples of 8; k and v have the same */

@@ -240,14 +240,22 @@ asap_status asap_rope(asap_ctx *ctx, const asap_rope_plan *plan, const asap_rope
   a.n_tensors = p->n_tensors; a.n_rows = p->n_rows; a.head_dim = p->head_dim; a.n_pairs = plan->n_pairs; a.interleaved = plan->interleaved ? 1 : 0;
   a.dst_rows = p->dst_rows; a.magnitude = plan->magnitude; a.sign = p->inverse ? -1.f : 1.f; a.pos = p->pos; a.map = p->dst_map;
   memcpy(a.turns, plan->turns, sizeof(a.turns));
-  a.rows_per_block = p->n_rows >= 16 * ctx->num_sms ? ROPE_MAX_ROWS : 1;
+  long long blocks = 0;
+  for (int i = 0; i < p->n_tensors; ++i) {
+    RopeTensor &t = a.t[i];
+    t.rows = 1;
+    if (p->n_rows >= 16 * ctx->num_sms) t.rows = t.heads >= 128 ? 1 : t.heads > 128 / ROPE_MAX_ROWS ? 128 / t.heads : ROPE_MAX_ROWS;
+    t.first_block = (int)blocks;
+    blocks += (p->n_rows + t.rows - 1) / t.rows;
+  }
+  if (blocks > 0x7fffffffLL) return fail(ctx, ASAP_ERR_UNSUPPORTED, "%s: too many rows", who);
   const bool vec = plan->n_pairs % (plan->interleaved ? 4 : 8) == 0;
   DeviceGuard guard(ctx->device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool f16 = p->dtype == ASAP_FP16;
   mark(ctx, "rope", st);
   launch_pdl(f16 ? (vec ? rope_kernel<true, true> : rope_kernel<true, false>) : (vec ? rope_kernel<false, true> : rope_kernel<false, false>),
-             dim3((p->n_rows + a.rows_per_block - 1) / a.rows_per_block, p->n_tensors), dim3(ROPE_THREADS), 0, st, a);
+             dim3((unsigned)blocks), dim3(ROPE_THREADS), 0, st, a);
   return finish(ctx, after_launch(ctx, "rope"), st);
 }
 
@@ -321,7 +329,8 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
              dim3((p->n_q + rows - 1) / rows, (p->H + heads - 1) / heads), dim3(CA_JOIN_THREADS), 0, st, a);
   ASAP_TRY(after_launch(ctx, "cache_join"));
   if (p->weights && !few) {
-    const int own_lanes = (long long)p->max_q * p->H <= 64 ? 64 : 16, pre_lanes = 16;
+    const auto lanes_of = [](long long pairs) { return pairs <= 64 ? 64 : pairs <= 512 ? 16 : 4; };
+    const int own_lanes = lanes_of((long long)p->max_q * p->H), pre_lanes = lanes_of((long long)p->n_q * p->H / (p->n_groups ? p->n_groups : 1));
     const long long pre = (p->max_prefix + 4 * pre_lanes - 1) / (4 * pre_lanes), own = (p->max_len + 4 * own_lanes - 1) / (4 * own_lanes);
     const long long blocks = pre * p->n_groups + own * p->B;
     if (blocks > 0) {
@@ -393,15 +402,19 @@ asap_status asap_cache_evict(asap_ctx *ctx, const asap_cache_evict_args *p, void
   const bool meta = p->dst_weights || p->dst_pos;
   if (p->n_tensors > 0 || meta) {
     mv.keep_idx = p->keep_idx; mv.start = p->start; mv.dst_start = p->dst_start; mv.keep = p->keep; mv.n_tensors = p->n_tensors;
-    mv.row_vecs = (int)(p->row_bytes / 16);
+    mv.row_vecs = p->n_tensors > 0 ? (int)(p->row_bytes / 16) : 1;
     mv.weights = p->weights; mv.pos = p->pos; mv.dst_weights = p->dst_weights; mv.dst_pos = p->dst_pos;
     const unsigned layers = p->n_tensors + (meta ? 1 : 0);
     mark(ctx, "evict_move", st);
     mv.in_order = meta_in_place ? 1 : 0;
     if (in_place)
       launch_pdl(evict_in_place_kernel, dim3((mv.row_vecs + 15) / 16, p->B, layers), dim3(EV_MOVE_THREADS), 0, st, mv);
-    else
-      launch_pdl(evict_move_kernel, dim3((p->keep + EV_MOVE_THREADS / 32 - 1) / (EV_MOVE_THREADS / 32), p->B, layers), dim3(EV_MOVE_THREADS), 0, st, mv);
+    else {
+      mv.warp_rows = mv.row_vecs < 256 ? 256 / mv.row_vecs : 1;
+      const int block_rows = mv.warp_rows * (EV_MOVE_THREADS / 32);
+      const int move_blocks = (p->keep + block_rows - 1) / block_rows, meta_blocks = meta ? (p->keep + EV_MOVE_THREADS - 1) / EV_MOVE_THREADS : 0;
+      launch_pdl(evict_move_kernel, dim3(p->n_tensors == 0 || meta_blocks > move_blocks ? meta_blocks : move_blocks, p->B, layers), dim3(EV_MOVE_THREADS), 0, st, mv);
+    }
     ASAP_TRY(after_launch(ctx, "evict_move"));
   }
   return finish(ctx, ASAP_OK, st);

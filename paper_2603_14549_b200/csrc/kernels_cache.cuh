@@ -44,17 +44,18 @@ __device__ __forceinline__ float2 unpack2_t(uint32_t w) {
 // =======================================================================================
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_MAX_PAIRS = 128;
-constexpr int ROPE_MAX_ROWS = 4;       // rows of a block
+constexpr int ROPE_MAX_ROWS = 16;      // rows of a block
 
 struct RopeTensor {
   const uint16_t *src;
   uint16_t *dst;
   int heads, rotate, mapped;
+  int rows, first_block;               // rows of a block, and the tensor's first block
   long long src_row, src_head, dst_row, dst_head;
 };
 struct RopeArgs {
   RopeTensor t[4];
-  int n_tensors, n_rows, rows_per_block, head_dim, n_pairs, interleaved, dst_rows;
+  int n_tensors, n_rows, head_dim, n_pairs, interleaved, dst_rows;
   float magnitude, sign;
   const int *pos, *map;
   unsigned long long turns[ROPE_MAX_PAIRS];
@@ -62,16 +63,21 @@ struct RopeArgs {
 
 // One element pair, or eight elements at a time (VEC) where the pairs allow it: half layout n_pairs % 8 == 0, interleaved
 // n_pairs % 4 == 0.  The angles of a row are taken once for all its heads: pos * turns modulo 2^64 is the fraction of a turn, whose
-// upper 32 bits, as a signed number, are the angle in (-1/2, 1/2] turns (2^-32 turns off at most); sincospi takes it in fp32.
+// upper 32 bits, as a signed number, are the angle in [-1/2, 1/2) turns (2^-32 turns off at most); sincospi takes it in fp32.
+// What bounds it on prompts is the memory, kept busy by many warps with little in hand: 24531 rows of 32 + 2 x 32 heads 208 us, 89 % of a
+// copy's rate.  (Four rows of a piece under way together per thread, 74 registers, 237 us; warps with angles of their own, 94 registers, 315.)
+// A block takes about 128 heads of one tensor: four rows of 32 heads, sixteen of 8 or fewer.
 template <bool F16, bool VEC>
 __global__ void __launch_bounds__(ROPE_THREADS)
 rope_kernel(const __grid_constant__ RopeArgs a) {
   __shared__ __align__(16) float cs[ROPE_MAX_ROWS][2][ROPE_MAX_PAIRS];
   __shared__ int dst_of[ROPE_MAX_ROWS];
   pdl_enter();
-  const int row0 = blockIdx.x * a.rows_per_block;
-  const int rows = min(a.rows_per_block, a.n_rows - row0);
-  const RopeTensor &t = a.t[blockIdx.y];
+  int ti = 0;
+  while (ti + 1 < a.n_tensors && (int)blockIdx.x >= a.t[ti + 1].first_block) ++ti;
+  const RopeTensor &t = a.t[ti];
+  const int row0 = (blockIdx.x - t.first_block) * t.rows;
+  const int rows = min(t.rows, a.n_rows - row0);
   for (int i = threadIdx.x; t.rotate && i < rows * a.n_pairs; i += ROPE_THREADS) {
     const int r = i / a.n_pairs, p = i - r * a.n_pairs;
     const long long pos = ld_prev(a.pos + row0 + r);
@@ -105,21 +111,21 @@ rope_kernel(const __grid_constant__ RopeArgs a) {
     if (d < 0) continue;
     const uint16_t *src = t.src + (long long)(row0 + r) * t.src_row + (long long)h * t.src_head;
     uint16_t *dst = t.dst + (long long)d * t.dst_row + (long long)h * t.dst_head;
-    if (v >= n_rot) {
-      const int e = (t.rotate ? rot : 0) + (v - n_rot) * (VEC ? 8 : 1);
-      if constexpr (VEC) {
-        uint4 x;
-        ld_prev8(src + e, x);
-        *reinterpret_cast<uint4 *>(dst + e) = x;
-      } else {
-        dst[e] = *reinterpret_cast<const volatile uint16_t *>(src + e);
-      }
+    // (pieces that pass through and rotated ones lie in the same warp: their loads are one instruction)
+    const bool turned = v < n_rot;
+    const int e0 = turned ? v * 8 : (t.rotate ? rot : 0) + (v - n_rot) * (VEC ? 8 : 1);
+    uint4 x, y;
+    if constexpr (VEC) {
+      ld_prev8(src + e0, x);
+      if (turned && !a.interleaved) ld_prev8(src + P + e0, y);
+    }
+    if (!turned) {
+      if constexpr (VEC) *reinterpret_cast<uint4 *>(dst + e0) = x;
+      else dst[e0] = *reinterpret_cast<const volatile uint16_t *>(src + e0);
       continue;
     }
     if constexpr (VEC) {
       if (a.interleaved) {
-        uint4 x;
-        ld_prev8(src + v * 8, x);
         uint32_t w[4] = {x.x, x.y, x.z, x.w};
         const float4 c = *reinterpret_cast<const float4 *>(&cs[r][0][v * 4]), s = *reinterpret_cast<const float4 *>(&cs[r][1][v * 4]);
         const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
@@ -130,9 +136,6 @@ rope_kernel(const __grid_constant__ RopeArgs a) {
         }
         *reinterpret_cast<uint4 *>(dst + v * 8) = make_uint4(w[0], w[1], w[2], w[3]);
       } else {
-        uint4 x, y;
-        ld_prev8(src + v * 8, x);
-        ld_prev8(src + P + v * 8, y);
         uint32_t wx[4] = {x.x, x.y, x.z, x.w}, wy[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -185,7 +188,7 @@ constexpr int CA_JOIN_BYTES = 4096;                       // the warps' sums of 
 constexpr int CA_JOBS = 2;                                // items announced ahead
 constexpr int CA_Q_PITCH = 272;                           // a query row of 256 bytes; eight rows side by side meet all banks
 constexpr int CA_Q_BYTES = StreamWork::ROWS * CA_Q_PITCH;
-constexpr int CA_MAX_SEGMENTS = 928;
+constexpr int CA_MAX_SEGMENTS = 1024;
 constexpr long long CA_WAIT_LIMIT = 2000000000LL;
 
 // Key / value heads that the streaming kernel takes together for segments of R stacked rows: at most 16 rows in all.  Long segments are taken
@@ -994,9 +997,7 @@ constexpr int CT_THREADS = 384;                 // warp 0: key / value copies, 1
 constexpr int CT_TILE_BYTES = 128 * 128 * 2;
 constexpr int CT_BLOCK_BYTES = CT_TILE_BYTES / 2;
 constexpr int CT_SLOTS = 4;                     // ring of key and value tiles in the order K0 V0 K1 V1 ...
-constexpr int CT_STAGE_BYTES = 32 * 64;         // per softmax warp: 32 rows x 16 floats
-constexpr int CT_STAGE_OFF = (2 + CT_SLOTS) * CT_TILE_BYTES;
-constexpr int CT_BOOK_OFF = CT_STAGE_OFF + 8 * CT_STAGE_BYTES;
+constexpr int CT_BOOK_OFF = (2 + CT_SLOTS) * CT_TILE_BYTES;
 constexpr int CT_JOBS = 4;                      // items announced ahead
 constexpr uint32_t CT_TMEM_COLS = 512, CT_S_COL = 256, CT_P_COL = 384;   // O of both row tiles, one S that they use in turn, P of both
 // A tile's sum relative to the reference at which the reference moves: no probability may leave the element type's range.
@@ -1306,7 +1307,6 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
     const uint32_t s_addr = lane_addr + CT_S_COL, p_addr = lane_addr + CT_P_COL + g * 64, o_addr = lane_addr + g * 128;
     const float scale = a.scale_log2;
     const uint64_t scale2 = f2_pack(scale, scale);
-    uint8_t *stage = ct_smem + CT_STAGE_OFF + (warp - 4) * CT_STAGE_BYTES;
     int sc = 0;                                   // key tiles so far
     CaJob j;
     for (int jc = 0; take(jc, j); ++jc) {
@@ -1346,24 +1346,15 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
             if (c >= lim) xr[c] = __float_as_uint(-INFINITY);
         }
         if constexpr (WEIGHTS) {
-          // through shared memory, 16 columns at a time (16-byte chunk c of row r at c ^ ((r >> 1) & 3)): a store covers eight pieces of 64 bytes
+          if (entry >= 0) {
+            float *row = a.logits + (long long)entry * a.pitch + (j.causal ? a.own_off : 0) + j0;
 #pragma unroll
-          for (int c0 = 0; c0 < 128; c0 += 16) {
-            __syncwarp();
+            for (int c = 0; c < 128; c += 8) {
+              float v[8];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              float4 v;
-              v.x = __uint_as_float(xr[c0 + 4 * c]) * scale; v.y = __uint_as_float(xr[c0 + 4 * c + 1]) * scale;
-              v.z = __uint_as_float(xr[c0 + 4 * c + 2]) * scale; v.w = __uint_as_float(xr[c0 + 4 * c + 3]) * scale;
-              *reinterpret_cast<float4 *>(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = v;
-            }
-            __syncwarp();
-#pragma unroll
-            for (int r8 = 0; r8 < 32; r8 += 8) {
-              const int rr = r8 + (lane >> 2), c = lane & 3;
-              const int e = __shfl_sync(0xffffffffu, entry, rr);
-              const float4 v = *reinterpret_cast<const float4 *>(stage + rr * 64 + ((c ^ ((rr >> 1) & 3)) << 4));
-              if (e >= 0) *reinterpret_cast<float4 *>(a.logits + (long long)e * a.pitch + (j.causal ? a.own_off : 0) + j0 + c0 + 4 * c) = v;
+              for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(xr[c + e]) * scale;
+              asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                           ::"l"(row + c), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
             }
           }
           __syncwarp();
@@ -1687,8 +1678,8 @@ ca_join_kernel(const __grid_constant__ CacheArgs a) {
 // ---------------------------------------------------------------------------------------
 // weights[j] += 1 / H * sum over the segment's query rows and heads of 2^(x - lse2).  A thread takes four keys; `lanes` threads side by side
 // on the keys, the others below them share the (row, head) pairs, and their sums are added in order.  Few pairs (own rows of single
-// tokens): 64 threads on 256 keys, 8 pairs a thread under way together; many: 16 on 64 keys.  (64 x 870 keys, 32 pairs: 9 us
-// against 24 with 64 keys a block; a prefix with 320 pairs and 2000 keys is the other way round.)
+// tokens): 64 threads on 256 keys, 8 pairs a thread under way together; many: 16 on 64 keys; more than 512: 4 on 16 keys.  (64 x 870 keys, 32
+// pairs: 9 us against 24 with 64 keys a block; a prefix with 320 pairs and 2000 keys is the other way round.)
 // ---------------------------------------------------------------------------------------
 constexpr int CA_WEIGHT_THREADS = 256;
 
@@ -2008,7 +1999,7 @@ struct EvictMoveArgs {
   const uint4 *src[EV_MAX_TENSORS];
   uint4 *dst[EV_MAX_TENSORS];
   const int *keep_idx, *start, *dst_start;
-  int n_tensors, keep, row_vecs;
+  int n_tensors, keep, row_vecs, warp_rows;
   int in_order;                                  // weights or positions move in place
   const float *weights;
   const int *pos;
@@ -2033,35 +2024,43 @@ __device__ __forceinline__ void evict_meta_in_order(const EvictMoveArgs &a, int 
   }
 }
 
-// Into other tensors: a warp per kept row.  The last grid layer moves weights and positions, a thread per row.
+// Into other tensors: a warp takes as many kept rows as make up 4 KB, or one long one, eight loads of a lane under way together (with a row per
+// warp 19 x 1875 rows of 1 KB took a third longer).  The last grid layer moves weights and positions, a thread per row.
 __global__ void __launch_bounds__(EV_MOVE_THREADS)
 evict_move_kernel(const __grid_constant__ EvictMoveArgs a) {
   pdl_enter();
   const int b = blockIdx.y, t = blockIdx.z, lane = threadIdx.x & 31;
   const int row0 = ld_prev(a.start + b), dst0 = a.dst_start ? ld_prev(a.dst_start + b) : row0;
-  if (t == a.n_tensors && a.in_order) {
-    if (blockIdx.x == 0) evict_meta_in_order(a, b, row0, dst0);
-    return;
-  }
-  const int i = t == a.n_tensors ? blockIdx.x * EV_MOVE_THREADS + threadIdx.x : blockIdx.x * (EV_MOVE_THREADS / 32) + (threadIdx.x >> 5);
-  if (i >= a.keep) return;
-  const int k = ld_prev(a.keep_idx + (size_t)b * a.keep + i);
-  if (k < 0) return;
+  const int *idx = a.keep_idx + (size_t)b * a.keep;
   if (t == a.n_tensors) {
+    if (a.in_order) {
+      if (blockIdx.x == 0) evict_meta_in_order(a, b, row0, dst0);
+      return;
+    }
+    const int i = blockIdx.x * EV_MOVE_THREADS + threadIdx.x, k = i < a.keep ? ld_prev(idx + i) : -1;
+    if (k < 0) return;
     if (a.dst_weights) a.dst_weights[dst0 + i] = ld_prev(a.weights + row0 + k);
     if (a.dst_pos) a.dst_pos[dst0 + i] = a.pos ? ld_prev(a.pos + row0 + k) : k;
     return;
   }
-  const uint4 *s = a.src[t] + (size_t)(row0 + k) * a.row_vecs;
-  uint4 *d = a.dst[t] + (size_t)(dst0 + i) * a.row_vecs;
-  for (int v = lane; v < a.row_vecs; v += 8 * 32) {
+  const int i0 = (blockIdx.x * (EV_MOVE_THREADS / 32) + (threadIdx.x >> 5)) * a.warp_rows;
+  const int n = min(a.warp_rows, a.keep - i0) * a.row_vecs;      // vectors of this warp's rows
+  for (int v0 = 0; v0 < n; v0 += 8 * 32) {
     uint4 x[8];
+    long long to[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int f = v0 + 32 * e + lane, r = a.warp_rows == 1 ? 0 : f / a.row_vecs, v = f - r * a.row_vecs;
+      to[e] = -1;
+      if (f >= n) continue;
+      const int k = ld_prev(idx + i0 + r);
+      if (k < 0) continue;
+      to[e] = (long long)(dst0 + i0 + r) * a.row_vecs + v;
+      ld_prev8(a.src[t] + (size_t)(row0 + k) * a.row_vecs + v, x[e]);
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (v + 32 * e < a.row_vecs) ld_prev8(s + v + 32 * e, x[e]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (v + 32 * e < a.row_vecs) d[v + 32 * e] = x[e];
+      if (to[e] >= 0) a.dst[t][to[e]] = x[e];
   }
 }
 

@@ -116,7 +116,7 @@ def _attend(**kw):
 @pytest.mark.parametrize("status,kw", [
     (-1, dict(B=0)), (-1, dict(n_q=0)), (-1, dict(max_q=0)), (-1, dict(max_q=3)), (-5, dict(head_dim=64)), (-5, dict(dtype=7)),
     (-1, dict(kv_heads=3)), (-1, dict(max_len=1001)), (-1, dict(max_len=-1)), (-1, dict(n_groups=1)), (-1, dict(n_groups=3)),
-    (-5, dict(B=929, n_q=929)), (-1, dict(scale=-1.0)), (-1, dict(scale=float("nan"))), (-1, dict(q=None)), (-1, dict(len=None)),
+    (-5, dict(B=1025, n_q=1025)), (-1, dict(scale=-1.0)), (-1, dict(scale=float("nan"))), (-1, dict(q=None)), (-1, dict(len=None)),
     (-1, dict(n_q=3)), (-2, dict(k=(1 << 21) + 8)), (-2, dict(kv_row=260)), (-1, dict(kv_row=64)), (-1, dict(kv_head=0)),
     (-1, dict(out_row=1000)), (-1, dict(out=1 << 20)), (-1, dict(out=1 << 21)), (-1, dict(q_row=-8)), (-1, dict(kv_row=1 << 40))])
 def test_attention_that_is_refused(lib, ctx, status, kw):
