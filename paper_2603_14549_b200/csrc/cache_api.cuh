@@ -388,7 +388,8 @@ asap_status asap_cache_evict(asap_ctx *ctx, const asap_cache_evict_args *p, void
   a.start = p->start; a.len = p->len; a.dst_start = p->dst_start; a.weights = p->weights; a.pos = p->pos; a.keep_idx = p->keep_idx;
   a.new_len = p->new_len; a.status = ctx->status;
   // (where max_len <= keep every sequence stays whole, and its rows are not ranked)
-  const bool cluster = p->max_len > p->keep && p->max_len >= EV_CLUSTER_MIN;
+  const long long rounds = ((long long)p->B * EV_CLUSTER + ctx->num_sms - 1) / ctx->num_sms;
+  const bool cluster = p->max_len > p->keep && p->max_len >= (rounds == 1 ? EV_CLUSTER_MIN : rounds * EV_CLUSTER_MIN_ROUND);
   const long long share = p->max_len > p->keep ? (((long long)p->max_len + (cluster ? EV_CLUSTER : 1) - 1) / (cluster ? EV_CLUSTER : 1) + 31) / 32 * 32 : 0;
   a.cached = share * 4 <= EV_KEYS_BYTES ? (int)share : 0;
   DeviceGuard guard(ctx->device);

@@ -1816,7 +1816,10 @@ ca_weight_few_kernel(const __grid_constant__ CacheArgs a, int own_blocks) {
 // =======================================================================================
 constexpr int EV_THREADS = 1024;
 constexpr int EV_CLUSTER = 8;                    // blocks that share a long sequence
-constexpr int EV_CLUSTER_MIN = 6144;             // rows from which they do
+// Rows from which they do, if the device takes all sequences' clusters at once, or per round of them if it does not.  (One block: 7.4 us for 2048
+// rows, 12.5 for 8192, 32 for 32768, for 64 sequences as for one.  Clusters: 11 to 14 us for up to 8 sequences, 22 to 29 for 19, 53 to 70
+// for 64.)
+constexpr int EV_CLUSTER_MIN = 6144, EV_CLUSTER_MIN_ROUND = 12288;
 constexpr int EV_KEYS_BYTES = 192 * 1024;        // a block's keys in shared memory, if its rows fit
 
 struct EvictArgs {
