@@ -319,14 +319,16 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
     ASAP_TRY(after_launch(ctx, "cache_weight"));
   }
   mark(ctx, "cache_join", st);
-  // (one wave of the split form: 1 x 32 heads 14 -> 8 us, 5 rows of up to 150 partial results 17 -> 8; 128 rows 21 -> 62)
-  const bool split = (long long)p->n_q * ((p->H + CA_JOIN_SPLIT_HEADS - 1) / CA_JOIN_SPLIT_HEADS) <= 2LL * ctx->num_sms;
-  const int heads = split ? CA_JOIN_SPLIT_HEADS : CA_JOIN_HEADS;
-  const bool many = !split && p->n_q >= 4 * ctx->num_sms;
-  const int rows = many ? 4 : 1;
-  launch_pdl(f16 ? (split ? ca_join_kernel<true, true, 1> : many ? ca_join_kernel<true, false, 4> : ca_join_kernel<true, false, 1>)
-                 : (split ? ca_join_kernel<false, true, 1> : many ? ca_join_kernel<false, false, 4> : ca_join_kernel<false, false, 1>),
-             dim3((p->n_q + rows - 1) / rows, (p->H + heads - 1) / heads), dim3(CA_JOIN_THREADS), 0, st, a);
+  // (the form with as many blocks as the device holds at a time: 1 x 32 heads 14 -> 8 us, 5 rows of up to 150 partial results 17 -> 8 with eight
+  // warps a head; with those 128 rows 21 -> 62)
+  const auto blocks_of = [&](int heads) { return (long long)p->n_q * ((p->H + heads - 1) / heads); };
+  const int share = blocks_of(2) <= 2LL * ctx->num_sms ? 8 : blocks_of(8) <= 2LL * ctx->num_sms ? 2 : 1;
+  const int heads = share > 1 ? CA_JOIN_WARPS / share : CA_JOIN_HEADS, rows = share == 1 && p->n_q >= 4 * ctx->num_sms ? 4 : 1;
+  void (*join)(CacheArgs) = share == 8 ? (f16 ? ca_join_kernel<true, 8, 1> : ca_join_kernel<false, 8, 1>)
+                          : share == 2 ? (f16 ? ca_join_kernel<true, 2, 1> : ca_join_kernel<false, 2, 1>)
+                          : rows == 4  ? (f16 ? ca_join_kernel<true, 1, 4> : ca_join_kernel<false, 1, 4>)
+                                       : (f16 ? ca_join_kernel<true, 1, 1> : ca_join_kernel<false, 1, 1>);
+  launch_pdl(join, dim3((p->n_q + rows - 1) / rows, (p->H + heads - 1) / heads), dim3(CA_JOIN_THREADS), 0, st, a);
   ASAP_TRY(after_launch(ctx, "cache_join"));
   if (p->weights && !few) {
     const auto lanes_of = [](long long pairs) { return pairs <= 64 ? 64 : pairs <= 512 ? 16 : 4; };

@@ -1484,11 +1484,11 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
 // Partial results of a (query row, head) -> output, four of the 128 values a lane.  A thread works out where the partial results of one (head,
 // prefix or own rows) lie.  (With the addresses worked out by every warp for itself the kernel was bound by those instructions: 2254
 // rows x 32 heads 67 us.)  Three forms: a block takes 32 heads of ROWS query rows, a warp two at a time (four rows where there are enough of
-// them: 2254 x 32 heads 41 us -> 25); with few rows (SPLIT) it takes two heads, and eight warps share the partial results of one, of which
-// a long sequence has a hundred or more.
+// them, and two blocks on an SM: 2254 x 32 heads 41 us -> 37); with fewer rows it takes eight heads or two, and two or eight warps share the
+// partial results of one head, of which a long sequence has a hundred or more.
 // ---------------------------------------------------------------------------------------
 constexpr int CA_JOIN_THREADS = 512, CA_JOIN_WARPS = CA_JOIN_THREADS / 32;
-constexpr int CA_JOIN_HEADS = 32, CA_JOIN_SPLIT_HEADS = 2;
+constexpr int CA_JOIN_HEADS = 32;
 
 __device__ __forceinline__ float2 ld_prev2f(const float2 *p) {
   float2 v;
@@ -1554,10 +1554,11 @@ __device__ __forceinline__ void ca_finish_row(const CacheArgs &a, const CaSum &s
   }
 }
 
-template <bool F16, bool SPLIT, int ROWS>
+template <bool F16, int SHARE, int ROWS>
 __global__ void __launch_bounds__(CA_JOIN_THREADS, 2)
 ca_join_kernel(const __grid_constant__ CacheArgs a) {
-  constexpr int HEADS = SPLIT ? CA_JOIN_SPLIT_HEADS : CA_JOIN_HEADS;
+  constexpr bool SPLIT = SHARE > 1;              // warps that share a head
+  constexpr int HEADS = SPLIT ? CA_JOIN_WARPS / SHARE : CA_JOIN_HEADS;
   __shared__ CaParts sh_parts[ROWS * HEADS][2];
   __shared__ int sh_valid[ROWS];
   __shared__ float4 sh_acc[SPLIT ? CA_JOIN_WARPS : 1][32];
@@ -1602,7 +1603,6 @@ ca_join_kernel(const __grid_constant__ CacheArgs a) {
     if (sh_valid[r] == 0 && h < a.H) a.lse2[(long long)(blockIdx.x * ROWS + r) * a.H + h] = INFINITY;
   }
   if constexpr (SPLIT) {
-    constexpr int SHARE = CA_JOIN_WARPS / HEADS;
     const int e = warp / SHARE, w = warp - e * SHARE;
     CaSum s;
 #pragma unroll
