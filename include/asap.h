@@ -286,7 +286,9 @@ typedef struct {
 
 /* Rotates (and copies) up to four tensors with the same positions in one launch: the queries, the keys into their cache rows,
  * the values into theirs.  src == dst with the same strides, unmapped, rotates in place; other overlaps of a tensor's source and
- * destination are refused.  n_rows == 0 does nothing. */
+ * destination are refused.  A call's tensors may lie between each other's rows or heads (the parts of a packed projection), but no
+ * element of a destination may belong to another of its tensors; equal pointers are refused.  At most 65536 heads.  n_rows == 0 does
+ * nothing. */
 asap_status asap_rope(asap_ctx *ctx, const asap_rope_plan *plan, const asap_rope_args *args, void *stream);
 
 /* Attention of new rows over a cache.  Sequence b owns rows start[b] .. start[b] + len[b] - 1 of the cache, its nq = q_cu[b + 1] -
@@ -330,8 +332,8 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
  * Rows rank: held rows first (the first `sink` rows of the sequence, and those with pos > newest - recent, newest = the largest
  * position of the sequence), then by weight, largest first (-0 equals +0, NaN is below everything); lower row first among
  * equals.  For row i of the kept ones, each of the n_tensors (0 .. 64) tensors moves row start[b] + keep_idx[b][i] to row
- * dst_start[b] + i, and weights and pos likewise.  dst[t] == src[t] moves in place (dst_start NULL then); partly overlapping tensors are
- * refused. */
+ * dst_start[b] + i, and weights and pos likewise.  dst[t] == src[t] moves in place (dst_start NULL then; the sequences must not overlap);
+ * partly overlapping tensors are refused.  keep and max_len are at most 2^30. */
 typedef struct {
   int32_t B, max_len, keep, sink, recent;  /* 0 <= sink, 0 <= recent, sink + recent <= keep, 0 < keep */
   int32_t rows, dst_rows;                  /* rows of the sources / of the destinations */
@@ -355,7 +357,7 @@ asap_status asap_cache_evict(asap_ctx *ctx, const asap_cache_evict_args *args, v
  * pos[row] new_pos[b].  row[] is what asap_rope takes as dst_map.  Once a row has been reused the rows of a sequence are no longer in
  * the order of their positions: a call of asap_cache_attention with more than one query row per sequence needs them in order. */
 typedef struct {
-  int32_t B, capacity, sink, recent;       /* sink + recent < capacity */
+  int32_t B, capacity, sink, recent;       /* sink + recent < capacity <= 2^30 */
   int32_t rows;                            /* rows of weights and pos */
   const int32_t *start;                    /* [B] */
   int32_t *len;                            /* [B] */

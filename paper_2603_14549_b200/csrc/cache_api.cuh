@@ -36,6 +36,7 @@ bool strides_disjoint(long long rows, long long heads, long long dim, long long 
   if (rows == 1) return head >= dim;
   return (head >= dim && row >= (heads - 1) * head + dim) || (row >= dim && head >= (rows - 1) * row + dim);
 }
+constexpr int MAX_ROWS = 1 << 30;              // rows that 32-bit counters walk in strides
 constexpr long long MAX_STRIDE = 1LL << 39;    // elements of two bytes (a tensor map's strides are below 2^40 bytes)
 
 asap_status check_cache_attention(asap_ctx *ctx, const asap_cache_attention_args *p) {
@@ -80,6 +81,9 @@ struct CaLayout {
   int pieces[2] = {0, 0};        // pieces of their work
   int rec_rows = 0;
   bool too_large = false;
+  bool few = false;              // weights by ca_weight_few_kernel
+  int own_lanes = 0, pre_lanes = 0;          // threads side by side on the keys
+  long long own_blocks = 0, pre_blocks = 0;  // blocks of a sequence and of a prefix
 };
 constexpr long long CA_MAX_NUMBERS = 1LL << 30;    // key tiles are numbered in 32 bits
 CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint8_t *at, CacheArgs *a) {
@@ -105,6 +109,15 @@ CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint
   const long long rows_max = group_max > own_max ? group_max : own_max;
   l.rec_rows = (int)(4 * rows_max < S ? 4 * rows_max : S);           // (as many heads together as make up to 16 rows)
   l.too_large = streamed > CA_MAX_NUMBERS || tiled > CA_MAX_NUMBERS || (long long)entries > CA_MAX_NUMBERS / 2;
+  if (p->weights) {
+    const auto lanes_of = [](long long pairs) { return pairs <= 64 ? 64 : pairs <= 512 ? 16 : 4; };
+    l.few = p->n_groups == 0 && (long long)p->max_q * p->H <= CA_FEW_PAIRS && p->max_len > 0;
+    l.own_lanes = l.few ? CA_FEW_LANES : lanes_of((long long)p->max_q * p->H);
+    l.pre_lanes = lanes_of((long long)p->n_q * p->H / (p->n_groups ? p->n_groups : 1));
+    l.own_blocks = ((long long)p->max_len + 4 * l.own_lanes - 1) / (4 * l.own_lanes);
+    l.pre_blocks = ((long long)p->max_prefix + 4 * l.pre_lanes - 1) / (4 * l.pre_lanes);
+    l.too_large = l.too_large || l.own_blocks * p->B + l.pre_blocks * p->n_groups > CA_MAX_NUMBERS;
+  }
   auto carve = [&](size_t bytes) {
     const size_t o = l.bytes;
     l.bytes = align_up(l.bytes + bytes, 256);
@@ -215,6 +228,7 @@ asap_status asap_rope(asap_ctx *ctx, const asap_rope_plan *plan, const asap_rope
   for (int i = 0; i < p->n_tensors; ++i) {
     const asap_rope_tensor &t = p->tensors[i];
     if (t.heads <= 0) return fail(ctx, ASAP_ERR_INVALID, "%s: heads of tensor %d must be positive", who, i);
+    if (t.heads > 65536) return fail(ctx, ASAP_ERR_UNSUPPORTED, "%s: heads of tensor %d above 65536", who, i);
     if (p->n_rows > 0 && (!t.src || !t.dst)) return fail(ctx, ASAP_ERR_INVALID, "%s: null tensor %d", who, i);
     if (t.mapped && p->n_rows > 0 && (!p->dst_map || p->dst_rows <= 0)) return fail(ctx, ASAP_ERR_INVALID, "%s: tensor %d is mapped: dst_map and dst_rows are needed", who, i);
     if (!aligned16(t.src) || !aligned16(t.dst)) return fail(ctx, ASAP_ERR_ALIGN, "%s: tensor %d is not 16-byte aligned", who, i);
@@ -230,6 +244,11 @@ asap_status asap_rope(asap_ctx *ctx, const asap_rope_plan *plan, const asap_rope
       if (!same && ranges_overlap(t.src, 2 * span_of(p->n_rows, t.heads, p->head_dim, t.src_row, t.src_head), t.dst,
                                   2 * span_of(dst_rows, t.heads, p->head_dim, t.dst_row, t.dst_head)))
         return fail(ctx, ASAP_ERR_INVALID, "%s: source and destination %d overlap without being the same", who, i);
+    }
+    // (others may interleave with this one, as the parts of a packed projection do; the same start is no layout)
+    for (int j = 0; j < i && p->n_rows > 0; ++j) {
+      const asap_rope_tensor &u = p->tensors[j];
+      if (u.dst == t.dst || u.src == t.dst || u.dst == t.src) return fail(ctx, ASAP_ERR_INVALID, "%s: destination of tensor %d or %d is a tensor of the other", who, j, i);
     }
     RopeTensor &r = a.t[i];
     r.src = static_cast<const uint16_t *>(t.src); r.dst = static_cast<uint16_t *>(t.dst);
@@ -310,12 +329,10 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   launch_pdl(f16 ? ca_stream_kernel<true> : ca_stream_kernel<false>, dim3(layout.blocks[0]), dim3(CA_THREADS), ca_smem_bytes(p->B + p->n_groups), st,
              maps, a);
   ASAP_TRY(after_launch(ctx, "cache_stream"));
-  const bool few = p->weights && p->n_groups == 0 && (long long)p->max_q * p->H <= CA_FEW_PAIRS && p->max_len > 0;
-  a.join_behind = few ? 1 : 0;
-  if (few) {
-    const long long own = (p->max_len + 4 * CA_FEW_LANES - 1) / (4 * CA_FEW_LANES);
+  a.join_behind = layout.few ? 1 : 0;
+  if (layout.few) {
     mark(ctx, "cache_weight", st);
-    launch_pdl(ca_weight_few_kernel, dim3((unsigned)(own * p->B)), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)own);
+    launch_pdl(ca_weight_few_kernel, dim3((unsigned)(layout.own_blocks * p->B)), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)layout.own_blocks);
     ASAP_TRY(after_launch(ctx, "cache_weight"));
   }
   mark(ctx, "cache_join", st);
@@ -330,17 +347,12 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
                                        : (f16 ? ca_join_kernel<true, 1, 1> : ca_join_kernel<false, 1, 1>);
   launch_pdl(join, dim3((p->n_q + rows - 1) / rows, (p->H + heads - 1) / heads), dim3(CA_JOIN_THREADS), 0, st, a);
   ASAP_TRY(after_launch(ctx, "cache_join"));
-  if (p->weights && !few) {
-    const auto lanes_of = [](long long pairs) { return pairs <= 64 ? 64 : pairs <= 512 ? 16 : 4; };
-    const int own_lanes = lanes_of((long long)p->max_q * p->H), pre_lanes = lanes_of((long long)p->n_q * p->H / (p->n_groups ? p->n_groups : 1));
-    const long long pre = (p->max_prefix + 4 * pre_lanes - 1) / (4 * pre_lanes), own = (p->max_len + 4 * own_lanes - 1) / (4 * own_lanes);
-    const long long blocks = pre * p->n_groups + own * p->B;
-    if (blocks > 0) {
-      mark(ctx, "cache_weight", st);
-      launch_pdl(ca_weight_kernel, dim3((unsigned)blocks), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)(pre > 0 ? pre : 1), pre_lanes,
-                 (int)(own > 0 ? own : 1), own_lanes);
-      ASAP_TRY(after_launch(ctx, "cache_weight"));
-    }
+  const long long weight_blocks = layout.pre_blocks * p->n_groups + layout.own_blocks * p->B;
+  if (p->weights && !layout.few && weight_blocks > 0) {
+    mark(ctx, "cache_weight", st);
+    launch_pdl(ca_weight_kernel, dim3((unsigned)weight_blocks), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)(layout.pre_blocks > 0 ? layout.pre_blocks : 1),
+               layout.pre_lanes, (int)(layout.own_blocks > 0 ? layout.own_blocks : 1), layout.own_lanes);
+    ASAP_TRY(after_launch(ctx, "cache_weight"));
   }
   return finish(ctx, ASAP_OK, st);
 }
@@ -352,6 +364,7 @@ asap_status asap_cache_evict(asap_ctx *ctx, const asap_cache_evict_args *p, void
   if (!p) return fail(ctx, ASAP_ERR_INVALID, "%s: null arguments", who);
   if (p->B <= 0 || p->max_len <= 0 || p->keep <= 0 || p->rows <= 0 || p->dst_rows <= 0)
     return fail(ctx, ASAP_ERR_INVALID, "%s: B, max_len, keep, rows and dst_rows must be positive", who);
+  if (p->keep > MAX_ROWS || p->max_len > MAX_ROWS) return fail(ctx, ASAP_ERR_UNSUPPORTED, "%s: keep and max_len at most 2^30", who);
   if (p->sink < 0 || p->recent < 0 || (long long)p->sink + p->recent > p->keep)
     return fail(ctx, ASAP_ERR_INVALID, "%s: need 0 <= sink, recent and sink + recent <= keep", who);
   if (p->B > 65535) return fail(ctx, ASAP_ERR_UNSUPPORTED, "%s: at most 65535 sequences", who);
@@ -429,6 +442,7 @@ asap_status asap_cache_slot(asap_ctx *ctx, const asap_cache_slot_args *p, void *
   ctx->err[0] = 0;
   if (!p) return fail(ctx, ASAP_ERR_INVALID, "%s: null arguments", who);
   if (p->B <= 0 || p->capacity <= 0 || p->rows <= 0) return fail(ctx, ASAP_ERR_INVALID, "%s: B, capacity and rows must be positive", who);
+  if (p->capacity > MAX_ROWS) return fail(ctx, ASAP_ERR_UNSUPPORTED, "%s: capacity at most 2^30", who);
   if (p->sink < 0 || p->recent < 0 || (long long)p->sink + p->recent >= p->capacity)
     return fail(ctx, ASAP_ERR_INVALID, "%s: need 0 <= sink, recent and sink + recent < capacity", who);
   if (!p->start || !p->len || !p->weights || !p->pos || !p->new_pos || !p->row)

@@ -99,6 +99,18 @@ def test_rotations_that_are_refused(lib, ctx, status, kw):
     _refused(lib, ctx, "asap_rope", _rope(**kw), status, C.byref(plan))
 
 
+@pytest.mark.parametrize("status,src,dst", [(-1, 3 << 20, 2 << 20), (-1, 2 << 20, 4 << 20), (-1, 3 << 20, 1 << 20)])
+def test_two_tensors_of_a_rotation_that_meet_are_refused(lib, ctx, status, src, dst):
+    a = _rope(n_tensors=2)
+    a.owner = t = (A.CRopeTensor * 2)(a.owner[0], A.CRopeTensor(src, dst, 4, 1, 0, 0, 512, 128, 512, 128))
+    a.tensors = t
+    _refused(lib, ctx, "asap_rope", a, status, C.byref(A.asap_rope_make(128)))
+
+
+def test_heads_beyond_the_counters_are_refused(lib, ctx):
+    _refused(lib, ctx, "asap_rope", _rope(t_heads=65537, n_rows=1), -5, C.byref(A.asap_rope_make(128)))
+
+
 def test_a_rotation_without_rows_does_nothing(lib, ctx):
     plan = A.asap_rope_make(128)
     assert lib.asap_rope(ctx, C.byref(plan), C.byref(_rope(n_rows=0, pos=None, t_src=None, t_dst=None)), None) == 0
@@ -155,6 +167,22 @@ def _evict(**kw):
     (-1, dict(pos=1 << 30, dst_pos=(1 << 30) + 4)), (-5, dict(B=65536))])
 def test_evictions_that_are_refused(lib, ctx, status, kw):
     _refused(lib, ctx, "asap_cache_evict", _evict(**kw), status)
+
+
+@pytest.mark.parametrize("kw", [dict(keep=2 ** 30 + 1), dict(max_len=2 ** 31 - 1)])
+def test_evictions_beyond_the_counters_are_refused(lib, ctx, kw):
+    _refused(lib, ctx, "asap_cache_evict", _evict(**kw), -5)
+
+
+def test_slots_beyond_the_counters_are_refused(lib, ctx):
+    a = A.CCacheSlotArgs(B=2, capacity=2 ** 31 - 1, sink=4, recent=10, rows=1000, start=4096, len=4096, weights=8192, pos=8192, new_pos=4096, row=4096)
+    _refused(lib, ctx, "asap_cache_slot", a, -5)
+
+
+def test_attention_weights_of_more_blocks_than_a_launch_has_are_refused(lib, ctx):
+    # 1023 sequences of up to 38,600,000 keys, 16 keys a block: 2,467,987,500 blocks
+    _refused(lib, ctx, "asap_cache_attention", _attend(B=1023, H=513, kv_heads=1, n_q=1, max_q=1, max_len=38_600_000, cache_rows=38_600_000, q_cu=4096,
+                                                       q_row=513 * 128, out_row=513 * 128, kv_row=128, k=1 << 40, v=1 << 41, weights=4096), -5)
 
 
 @pytest.mark.parametrize("kw", [dict(B=0), dict(capacity=0), dict(sink=90, recent=10), dict(sink=-1), dict(weights=None), dict(row=None)])
