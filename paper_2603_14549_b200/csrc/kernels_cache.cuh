@@ -1,13 +1,16 @@
 // New tokens over a key / value cache: rotary positions with the rows appended, attention of the new rows over a shared prefix
 // and their own rows, accumulated attention weights, and eviction by those weights.
 //
-//   rope_kernel         (a, b) -> m (a cos f - b sin f, b cos f + a sin f) for up to four tensors of the same rows
-//   ca_stream_kernel    partial softmax sums of (query rows x a range of keys), keys and values streamed once
-//   ca_join_kernel      partial sums of a row -> output and ln of the sum
-//   ca_weight_kernel    probabilities summed over query rows and heads, per key
-//   evict_select_kernel rows kept by rank, their weights and positions
-//   evict_move_kernel   kept rows of the cache tensors
-//   slot_kernel         the row of every sequence's next token
+//   rope_kernel           (a, b) -> m (a cos f - b sin f, b cos f + a sin f) for up to four tensors of the same rows
+//   ca_stream_kernel      partial softmax sums of up to 16 stacked query rows over a range of keys, keys and values streamed once
+//   ca_tile_kernel        the same for more rows, 256 at a time on the tensor cores
+//   ca_join_kernel        partial sums of a row -> output and ln of the sum
+//   ca_weight_kernel      probabilities summed over query rows and heads, per key
+//   ca_weight_few_kernel  the same for few rows, from the partial sums, without waiting for the join
+//   evict_select_kernel   rows kept by rank
+//   evict_move_kernel     kept rows of the cache tensors, their weights and positions
+//   evict_in_place_kernel the same within the same tensors
+//   slot_kernel           the row of every sequence's next token
 #pragma once
 
 #include <cuda_fp16.h>
@@ -555,7 +558,9 @@ __device__ __forceinline__ void ca_merge(float &m, float &l, float2 other, float
   m = top;
 }
 
-// What bounds it is the memory (5.9 to 6.2 TB/s while it runs).  S^T = K Q^T and O^T = V^T P^T, with the keys and then the columns as the 16 rows of an
+// What bounds it is the memory where the cache is long: 64 sequences of 643 to 1100 rows of 32 heads, 0.89 GB, 152 us a call with its join and
+// weights (5.8 TB/s), 5 sequences of 2000 to 60000 rows of 8 heads, 0.63 GB, 106 us (5.9 TB/s).  A short call is the sum of its launches'
+// latencies: one token over 267 rows 12.5 us.  S^T = K Q^T and O^T = V^T P^T, with the keys and then the columns as the 16 rows of an
 // m16n8k16 instruction and up to 8 query rows as its 8 columns: a tile of 64 keys takes half the instructions, and half the
 // accumulators, of the form with (mostly empty) 16 query rows.  Rows 8 .. 15, where there are any, are a second set of columns for the
 // same key and value fragments.  A warp's logits of 16 keys x 8 rows become the second product's operand by transposing two 8 x 8
@@ -992,6 +997,11 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
 // Segments of more than 16 stacked rows.  Persistent blocks; two row tiles of 128 rows share every key and value tile of 128 keys and take
 // turns on the tensor pipe: S = Q K^T into tensor memory, one thread per row turns it into probabilities relative to a reference
 // maximum, P goes back to tensor memory in the element type, O += P V accumulates there.
+// What bounds it: a pair of key tiles takes 2300 to 2750 clocks, near the products' own rate, but an item's ends cost 8000 to 10000 more (the
+// first tile's maximum, 128 KB of results a block, nothing for the tensor pipe to do meanwhile) and a launch 11 us before its first
+// product: 13 sequences of 16 to 256 query rows over prefixes of 2915 rows, 32 heads: 146 us of the call's 193, where the
+// products alone are 69 at the measured rate.  (Results through shared memory, queries gathered and items counted two tiles longer
+// than their keys, in place of four: 175.)
 // ---------------------------------------------------------------------------------------
 constexpr int CT_THREADS = 384;                 // warp 0: key / value copies, 1: MMA issue, 2: value rows to be cleared, 3: query rows, 4-11: softmax
 constexpr int CT_TILE_BYTES = 128 * 128 * 2;
@@ -1245,7 +1255,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       // ---------------------------------------------------------------- query rows
       // Stacked row i is query row i / rep, head i % rep of the key / value head; rows past the last one hold anything (other sequences' query
       // rows, or what the buffer held), nothing of theirs is used.  One tiled copy where rep divides 128 (see make_query_map); otherwise
-      // gathered, a lane working out the addresses of four rows and sixteen lanes copying a row, which takes about 4000 clocks.
+      // gathered, a lane working out the addresses of four rows and sixteen lanes copying a row.
       const uint32_t leader = warp_leader();
       int tiled[2] = {0, 0};                      // tiled copies issued
       int qc[2] = {0, 0};
@@ -1437,8 +1447,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       if (n_act == 0) continue;
       float *dst = complete ? a.full_o : a.rec_o[1];
       const bool bad = *reinterpret_cast<volatile int *>(&bk->bad[jc & 3]) != 0;
-      // (A thread stores its own row, 32 bytes at a time: whole sectors.  Through shared memory in pieces of 32 rows x 16 columns it took half as
-      // long again.)
+      // (A thread stores its own row, 32 bytes at a time: whole sectors.)
 #pragma unroll 1
       for (int c0 = 0; c0 < 128; c0 += 32) {
         uint32_t r[32];
@@ -1733,7 +1742,7 @@ ca_weight_kernel(const __grid_constant__ CacheArgs a, int prefix_blocks, int pre
 }
 
 // The same for batches without prefixes whose sequences have at most 64 (row, head) pairs each: a block works out ln of their sums itself, from the
-// partial results, and so need not wait for the join (1 x 267 keys 15.7 us a call, with the join between 3 us more).
+// partial results, and so need not wait for the join, which runs beside it (1 x 267 keys: the call 15.7 -> 12.5 us).
 constexpr int CA_FEW_PAIRS = 64, CA_FEW_LANES = 64;
 
 __global__ void __launch_bounds__(CA_WEIGHT_THREADS)
@@ -2027,8 +2036,9 @@ __device__ __forceinline__ void evict_meta_in_order(const EvictMoveArgs &a, int 
   }
 }
 
-// Into other tensors: a warp takes as many kept rows as make up 4 KB, or one long one, eight loads of a lane under way together (with a row per
-// warp 19 x 1875 rows of 1 KB took a third longer).  The last grid layer moves weights and positions, a thread per row.
+// Into other tensors: a warp takes as many kept rows as make up 4 KB, or one long one, eight loads of a lane under way together (19
+// sequences, 1875 rows of 1 KB kept: the whole call 54 -> 50 us against a row per warp).  What bounds it is the memory: 24 x 640 rows of 8 KB,
+// keys and values, 87 us with the selection, 5.7 TB/s.  The last grid layer moves weights and positions, a thread per row.
 __global__ void __launch_bounds__(EV_MOVE_THREADS)
 evict_move_kernel(const __grid_constant__ EvictMoveArgs a) {
   pdl_enter();
@@ -2106,7 +2116,8 @@ evict_in_place_kernel(const __grid_constant__ EvictMoveArgs a) {
   }
 }
 
-// The lowest ranked row of a full cache: smallest key, the last row among equals.
+// The lowest ranked row of a full cache: smallest key, the last row among equals.  A block per sequence reads its weights and positions once; 64 x
+// 1152 rows 3.7 us, the call's own cost and one round trip to the memory.
 constexpr int SLOT_THREADS = 512;
 struct SlotArgs {
   int B, capacity, sink, recent, rows;
