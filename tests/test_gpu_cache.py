@@ -93,6 +93,18 @@ def test_rotation_in_place_and_back(ctx, layout, rot):
     assert ((z.double() - x.double()).abs() <= 2.0 ** -9 * (x.double().abs().amax(-1, keepdim=True) * 1.5)).all()
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_parts_of_a_packed_projection_turn_in_place(ctx, layout):
+    """Queries and keys between each other's rows, the values beside them as they were."""
+    packed = torch.randn(37, 6 + 2 + 2, HEAD, device=DEV, generator=gen(7)).to(torch.bfloat16)
+    before, pos, plan = packed.clone(), i32(list(range(37))), A.asap_rope_make(64, layout=layout)
+    q, k = packed[:, :6], packed[:, 6:8]
+    A.asap_rope(ctx, plan, A.RopeArgs(pos, [A.RopeTensor(q, q), A.RopeTensor(k, k)]))
+    A.asap_check(ctx)
+    _close_rotation(packed[:, :8], R.rotate(before[:, :8], pos, 64, layout, _freq(plan)), before[:, :8], packed.dtype, 1.0)
+    assert torch.equal(packed[:, 8:], before[:, 8:])
+
+
 def test_far_positions_keep_their_angles(ctx):
     """Positions up to the last int32, where an angle taken in 32 bits would be off by whole turns."""
     x = torch.randn(6, 2, HEAD, device=DEV, generator=gen(2)).to(torch.bfloat16)
@@ -252,6 +264,22 @@ def test_out_may_be_a_strided_view(ctx):
     c.out = wide[:, 2:6]
     c.run(ctx)
     assert torch.equal(first, c.out) and (wide[:, :2] == 7).all() and (wide[:, 6:] == 7).all()
+
+
+@pytest.mark.parametrize("nq", [[1, 2], [40, 90]], ids=["streamed", "tiles"])
+@pytest.mark.parametrize("what", ["rows", "heads"])
+def test_queries_may_be_a_broadcast_view(ctx, nq, what):
+    c = Case(lens=[100, 131], nq=nq, H=4, kv=2, dtype=torch.bfloat16, seed=8)
+    one = torch.randn(1 if what == "rows" else sum(nq), 4 if what == "rows" else 1, HEAD, device=DEV, generator=gen(8)).to(torch.bfloat16)
+    c.q = one.expand(sum(nq), 4, HEAD)
+    c.check(ctx)
+
+
+@pytest.mark.parametrize("weights", [False, True], ids=["", "weights"])
+def test_many_partial_results_of_many_rows(ctx, weights):
+    """Enough rows for two warps a head in the join, and long sequences cut into more pieces than those take at a time."""
+    c = Case(lens=[30000] + [20] * 49, nq=[1] * 50, H=24, kv=4, dtype=torch.float16, seed=16, weights=weights, groups=[(1, 3, 9000)])
+    c.check(ctx)
 
 
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")], ids=["nan", "inf", "-inf"])
@@ -540,6 +568,20 @@ def test_eviction(ctx, lens, keep, sink, recent, row, special, in_place):
         want_w[to], want_p[to] = w.to(DEV)[at], pos.to(DEV)[at]
     assert all(torch.equal(t, x) for t, x in zip(dst, want))          # and every other row as it was
     assert torch.equal(_bits(ow), _bits(want_w)) and torch.equal(op, want_p)
+
+
+def test_eviction_of_a_large_batch_with_one_long_sequence(ctx):
+    """A block per sequence, and one whose keys do not fit its shared memory."""
+    lens = [55000] + [60 + i for i in range(79)]
+    start, rows, w, pos = _evict_case(21, lens)
+    dw, dp, new_len = w.to(DEV), pos.to(DEV), i32(lens)
+    keep_idx, ow = torch.empty(80, 64, dtype=torch.int32, device=DEV), torch.full((rows,), 9.0, device=DEV)
+    A.asap_cache_evict(ctx, A.CacheEvict(i32(start), new_len, 55000, 64, dw, dp, keep_idx, new_len, dst_weights=ow, sink=2, recent=10))
+    A.asap_check(ctx)
+    for b, n in enumerate(lens):
+        e = R.evict(w[start[b]:start[b] + n].tolist(), pos[start[b]:start[b] + n].tolist(), 64, 2, 10)
+        assert keep_idx[b].tolist() == e + [-1] * (64 - len(e)) and int(new_len[b]) == len(e), b
+        assert torch.equal(ow[start[b]:start[b] + len(e)].cpu(), w[torch.tensor(e) + start[b]]), b
 
 
 def test_eviction_without_positions_or_tensors(ctx):
