@@ -336,16 +336,19 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
     ASAP_TRY(after_launch(ctx, "cache_weight"));
   }
   mark(ctx, "cache_join", st);
-  // (the form with as many blocks as the device holds at a time: 1 x 32 heads 14 -> 8 us, 5 rows of up to 150 partial results 17 -> 8 with eight
-  // warps a head; with those 128 rows 21 -> 62)
+  // (the form with the most blocks that the device holds at a time.  Two heads: 1 x 32 heads 14 -> 8 us, 5 rows of up to 150 partial results 17 ->
+  // 8, but 128 rows 21 -> 62; eight: 61 rows 16 -> 12; sixteen: 128 rows 18.5 -> 16.5)
   const auto blocks_of = [&](int heads) { return (long long)p->n_q * ((p->H + heads - 1) / heads); };
-  const int share = blocks_of(2) <= 2LL * ctx->num_sms ? 8 : blocks_of(8) <= 2LL * ctx->num_sms ? 2 : 1;
-  const int heads = share > 1 ? CA_JOIN_WARPS / share : CA_JOIN_HEADS, rows = share == 1 && p->n_q >= 4 * ctx->num_sms ? 4 : 1;
-  void (*join)(CacheArgs) = share == 8 ? (f16 ? ca_join_kernel<true, 8, 1> : ca_join_kernel<false, 8, 1>)
-                          : share == 2 ? (f16 ? ca_join_kernel<true, 2, 1> : ca_join_kernel<false, 2, 1>)
-                          : rows == 4  ? (f16 ? ca_join_kernel<true, 1, 4> : ca_join_kernel<false, 1, 4>)
-                                       : (f16 ? ca_join_kernel<true, 1, 1> : ca_join_kernel<false, 1, 1>);
-  launch_pdl(join, dim3((p->n_q + rows - 1) / rows, (p->H + heads - 1) / heads), dim3(CA_JOIN_THREADS), 0, st, a);
+  int heads = CA_JOIN_HEADS;
+  for (int few_heads : {16, 8, 2})
+    if (blocks_of(few_heads) <= 2LL * ctx->num_sms) heads = few_heads;
+  const int rows = heads == CA_JOIN_HEADS && p->n_q >= 4 * ctx->num_sms ? 4 : 1;
+  void (*join)(CacheArgs) = heads == 2    ? (f16 ? ca_join_kernel<true, 2, 1> : ca_join_kernel<false, 2, 1>)
+                          : heads == 8    ? (f16 ? ca_join_kernel<true, 8, 1> : ca_join_kernel<false, 8, 1>)
+                          : heads == 16   ? (f16 ? ca_join_kernel<true, 16, 1> : ca_join_kernel<false, 16, 1>)
+                          : rows == 1     ? (f16 ? ca_join_kernel<true, 32, 1> : ca_join_kernel<false, 32, 1>)
+                                          : (f16 ? ca_join_kernel<true, 32, 4> : ca_join_kernel<false, 32, 4>);
+  launch_pdl(join, dim3((p->n_q + rows - 1) / rows, (p->H + heads - 1) / heads), dim3(rows > 1 ? CA_JOIN_MANY_THREADS : CA_JOIN_THREADS), 0, st, a);
   ASAP_TRY(after_launch(ctx, "cache_join"));
   const long long weight_blocks = layout.pre_blocks * p->n_groups + layout.own_blocks * p->B;
   if (p->weights && !layout.few && weight_blocks > 0) {

@@ -1492,12 +1492,14 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
 // ---------------------------------------------------------------------------------------
 // Partial results of a (query row, head) -> output, four of the 128 values a lane.  A thread works out where the partial results of one (head,
 // prefix or own rows) lie.  (With the addresses worked out by every warp for itself the kernel was bound by those instructions: 2254
-// rows x 32 heads 67 us.)  Three forms: a block takes 32 heads of ROWS query rows, a warp two at a time (four rows where there are enough of
-// them, and two blocks on an SM: 2254 x 32 heads 41 us -> 37); with fewer rows it takes eight heads or two, and two or eight warps share the
-// partial results of one head, of which a long sequence has a hundred or more.
+// rows x 32 heads 67 us.)  Many rows: a block takes 32 heads of four, a warp two at a time, small blocks that hide each other's beginnings (2254
+// rows x 32 heads: 41 us with a row and 512 threads a block, 35 with four rows, 33 with four rows and 256 threads,
+// of which the whole call shows nothing, 193 and 194).  With fewer rows it takes
+// 16, 8 or 2 heads, and one, two or eight warps share the partial results of a head, eight of which are under way together; a long sequence has a
+// hundred or more.
 // ---------------------------------------------------------------------------------------
 constexpr int CA_JOIN_THREADS = 512, CA_JOIN_WARPS = CA_JOIN_THREADS / 32;
-constexpr int CA_JOIN_HEADS = 32;
+constexpr int CA_JOIN_HEADS = 32, CA_JOIN_MANY_THREADS = 256;
 
 __device__ __forceinline__ float2 ld_prev2f(const float2 *p) {
   float2 v;
@@ -1563,11 +1565,12 @@ __device__ __forceinline__ void ca_finish_row(const CacheArgs &a, const CaSum &s
   }
 }
 
-template <bool F16, int SHARE, int ROWS>
-__global__ void __launch_bounds__(CA_JOIN_THREADS, 2)
+template <bool F16, int HEADS, int ROWS>
+__global__ void __launch_bounds__(ROWS > 1 ? CA_JOIN_MANY_THREADS : CA_JOIN_THREADS, ROWS > 1 ? 4 : 2)
 ca_join_kernel(const __grid_constant__ CacheArgs a) {
-  constexpr bool SPLIT = SHARE > 1;              // warps that share a head
-  constexpr int HEADS = SPLIT ? CA_JOIN_WARPS / SHARE : CA_JOIN_HEADS;
+  constexpr int THREADS = ROWS > 1 ? CA_JOIN_MANY_THREADS : CA_JOIN_THREADS, WARPS = THREADS / 32;
+  constexpr int SHARE = WARPS / HEADS;           // warps that share a head
+  constexpr bool SPLIT = ROWS == 1 && SHARE >= 1;
   __shared__ CaParts sh_parts[ROWS * HEADS][2];
   __shared__ int sh_valid[ROWS];
   __shared__ float4 sh_acc[SPLIT ? CA_JOIN_WARPS : 1][32];
@@ -1580,7 +1583,7 @@ ca_join_kernel(const __grid_constant__ CacheArgs a) {
   // every query row of [q_cu[0], q_cu[B]) has an entry of this call unless the call is skipped
   const uint32_t status = *reinterpret_cast<volatile uint32_t *>(a.status);
   const int q0 = a.q_cu ? ld_prev(a.q_cu) : 0, q1 = a.q_cu ? ld_prev(a.q_cu + a.B) : a.n_q, going = ld_prev(a.plan + 2 * (n_seg + 1));
-  static_assert(ROWS * HEADS * 2 <= CA_JOIN_THREADS, "a thread per (query row, head, part)");
+  static_assert(ROWS * HEADS * 2 <= THREADS, "a thread per (query row, head, part)");
   if (threadIdx.x < ROWS * HEADS * 2) {
     const int qr = blockIdx.x * ROWS + threadIdx.x / (2 * HEADS), h = h0 + (threadIdx.x >> 1) % HEADS, p = threadIdx.x & 1;
     CaParts mine;
@@ -1641,7 +1644,7 @@ ca_join_kernel(const __grid_constant__ CacheArgs a) {
   } else {
     constexpr int MINE = 2;                      // (query row, head) pairs of a warp whose first loads are under way together
 #pragma unroll 1
-    for (int e0 = warp * MINE; e0 < ROWS * HEADS; e0 += CA_JOIN_WARPS * MINE) {
+    for (int e0 = warp * MINE; e0 < ROWS * HEADS; e0 += WARPS * MINE) {
       float2 ml[MINE][2];
       float4 o[MINE][2];
 #pragma unroll
