@@ -2138,6 +2138,7 @@ slot_kernel(const __grid_constant__ SlotArgs a) {
   pdl_enter();
   const int b = blockIdx.x, tid = threadIdx.x;
   const int n = ld_prev(a.len + b), row0 = ld_prev(a.start + b), np = ld_prev(a.new_pos + b);
+  __syncthreads();                               // (every thread has read the length, which the first one writes below)
   if (n < 0 || n > a.capacity || row0 < 0 || (long long)row0 + min(n + 1, a.capacity) > a.rows) {
     if (tid == 0) {
       a.row[b] = -1;

@@ -673,6 +673,28 @@ def test_slot_skips_a_bad_sequence(ctx):
     assert row.tolist() == [-1, -1, -1] and dl.tolist() == [11, 10, -1] and (dw == 1).all()
 
 
+def test_slots_of_caches_about_to_be_full(ctx):
+    """The call fills the last free row: the length that it writes is the one that tells a full cache, and no thread may take it for the
+    length before.  Row 0 is the lowest ranked one, which a thread that saw a full cache would choose."""
+    B, cap = 3000, 700
+    dw, dp = torch.rand(B * cap, device=DEV, generator=gen(3)) + 1, torch.arange(cap, dtype=torch.int32, device=DEV).repeat(B)
+    dw[::cap] = 0.5
+    start, dl, row = torch.arange(B, dtype=torch.int32, device=DEV) * cap, torch.empty(B, dtype=torch.int32, device=DEV), torch.empty(B, dtype=torch.int32, device=DEV)
+    args = A.CacheSlot(start, dl, cap, dw, dp, i32([cap + 5] * B), row)
+    want_w, want_p = dw.clone(), dp.clone()
+    want_w[cap - 1::cap], want_p[cap - 1::cap] = 0.0, cap + 5
+    for _ in range(30):
+        dl.fill_(cap - 1)
+        row.fill_(-9)
+        A.asap_cache_slot(ctx, args)
+        assert torch.equal(row, start + cap - 1) and (dl == cap).all() and torch.equal(dw, want_w) and torch.equal(dp, want_p)
+    want_w[cap - 1::cap] = 2.0                          # now they are full, and row 0 goes
+    dw.copy_(want_w)
+    A.asap_cache_slot(ctx, args)
+    A.asap_check(ctx)
+    assert torch.equal(row, start) and (dl == cap).all() and (dw[::cap] == 0).all() and (dp[::cap] == cap + 5).all()
+
+
 # ------------------------------------------------------------------------------------------------ all of them together
 def test_prune_then_decode_with_eviction(ctx):
     """A pruned prompt's cache is compacted, then questions are answered token by token: every new row is rotated into its slot, attends
