@@ -353,8 +353,8 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   const long long weight_blocks = layout.pre_blocks * p->n_groups + layout.own_blocks * p->B;
   if (p->weights && !layout.few && weight_blocks > 0) {
     mark(ctx, "cache_weight", st);
-    launch_pdl(ca_weight_kernel, dim3((unsigned)weight_blocks), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)(layout.pre_blocks > 0 ? layout.pre_blocks : 1),
-               layout.pre_lanes, (int)(layout.own_blocks > 0 ? layout.own_blocks : 1), layout.own_lanes);
+    launch_pdl(ca_weight_kernel, dim3((unsigned)weight_blocks), dim3(CA_WEIGHT_THREADS), 0, st, a, (int)layout.pre_blocks, layout.pre_lanes,
+               (int)layout.own_blocks, layout.own_lanes);
     ASAP_TRY(after_launch(ctx, "cache_weight"));
   }
   return finish(ctx, ASAP_OK, st);

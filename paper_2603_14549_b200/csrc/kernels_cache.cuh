@@ -1699,7 +1699,7 @@ __global__ void __launch_bounds__(CA_WEIGHT_THREADS)
 ca_weight_kernel(const __grid_constant__ CacheArgs a, int prefix_blocks, int prefix_lanes, int own_blocks, int own_lanes) {
   __shared__ float4 part[CA_WEIGHT_THREADS];
   pdl_enter();
-  const int n_pre = a.G * prefix_blocks;
+  const int n_pre = a.G * prefix_blocks;         // (no blocks for rows that the bounds rule out: then no block divides by that number either)
   const int s = (int)blockIdx.x < n_pre ? blockIdx.x / prefix_blocks : a.G + (blockIdx.x - n_pre) / own_blocks;
   const int kb = (int)blockIdx.x < n_pre ? blockIdx.x % prefix_blocks : (blockIdx.x - n_pre) % own_blocks;
   const uint32_t status = *reinterpret_cast<volatile uint32_t *>(a.status);

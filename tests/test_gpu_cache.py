@@ -246,6 +246,21 @@ def test_without_query_offsets_weights_and_lse(ctx):
     assert torch.equal(first, c.out)
 
 
+@pytest.mark.parametrize("nq", [1, 20], ids=["streamed", "tiles"])
+def test_weights_where_every_prefix_is_empty(ctx, nq):
+    """Groups whose prefixes have no rows (yet): the bound of the prefixes is zero, and the own rows get their weights all the same."""
+    c = Case(lens=[900, 300, 31, 700], nq=[nq] * 4, H=8, kv=2, dtype=torch.bfloat16, seed=40, groups=[(0, 1, 0), (1, 3, 0), (3, 4, 0)])
+    assert c.bounds["max_prefix"] == 0
+    c.check(ctx)
+
+
+@pytest.mark.parametrize("nq", [1, 20], ids=["streamed", "tiles"])
+def test_weights_where_no_sequence_has_rows_of_its_own(ctx, nq):
+    c = Case(lens=[0, 0, 0], nq=[nq] * 3, H=8, kv=2, dtype=torch.bfloat16, seed=41, groups=[(0, 1, 500), (1, 3, 77)])
+    assert c.bounds["max_len"] == 0
+    c.check(ctx)
+
+
 def test_scale_and_loose_bounds(ctx):
     c = Case(lens=[100, 31], nq=[1, 2], H=4, kv=2, dtype=torch.bfloat16, seed=5, slack=5000)
     before = c.weights.clone()
