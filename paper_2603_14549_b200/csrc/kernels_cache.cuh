@@ -498,6 +498,52 @@ __device__ __forceinline__ void mbar_arrive_lane0(uint32_t bar, int lane) {
   __syncwarp();
 }
 
+// The whole (converged) warp waits and knows whether all its lanes saw the phase complete: it goes on as one, or gives up as one.
+__device__ __forceinline__ bool mbar_wait_all(uint32_t bar, uint32_t parity, const WaitCtx &w) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, w));
+}
+// A block's last wait for copies that it issued itself (the abort flag does not end it); giving up is recorded.
+__device__ __forceinline__ void mbar_settle(uint32_t bar, uint32_t parity, const WaitCtx &w) {
+  if (!mbar_wait_drain(bar, parity, CA_WAIT_LIMIT)) atomicOr(w.status, w.status_bit);
+}
+
+// The waits in the streaming kernel's queue of items, by a whole (converged) warp.  The consumers meet in barriers without a limit at every item's
+// end, so all of them have to see the same items, after an abort too.  A wait past the limit raises the abort flag, which ends every wait but those
+// in the queue, so whoever has to be waited for comes then.  Only should that not happen either, for a second and more of looking, is the wait lost: 0.
+// 1: in time.  2: late.  (Bounded mbarriers in place of the barriers at an item's end: 61 sequences under 6 prefixes 90.0 us for 87.9.)
+constexpr int CA_QUEUE_LOOKS = 1 << 20;                   // of a microsecond at least
+__device__ __forceinline__ int ca_wait_on(uint32_t bar, uint32_t parity, volatile int *abort_flag, uint32_t *status, long long limit) {
+  const long long t0 = clock64();
+  bool ok;
+  while (!(ok = mbar_try_wait(bar, parity)) && clock64() - t0 <= limit) {}
+  if (__all_sync(0xffffffffu, ok)) return 1;
+  *abort_flag = 1;
+  atomicOr(status, (uint32_t)STATUS_CACHE_TIMEOUT);
+  for (int i = 0; !(ok = mbar_test_wait(bar, parity)) && i < CA_QUEUE_LOOKS; ++i) __nanosleep(1000);
+  return __all_sync(0xffffffffu, ok) ? 2 : 0;
+}
+// A consumer warp: whether it takes item n.  The first late warp decides for all of them (`verdict`: 2 n + 2 none takes it, 2 n + 3 all do), and a
+// warp that is in time has seen an item that no other one has given up yet.
+__device__ __forceinline__ bool ca_wait_on_item(unsigned int *verdict, int n, uint32_t bar, uint32_t parity, volatile int *abort_flag, uint32_t *status,
+                                             long long limit) {
+  const int how = ca_wait_on(bar, parity, abort_flag, status, limit);
+  if (how == 1) return true;
+  const unsigned int mine = 2u * n + 2u + (how == 2 ? 1u : 0u);
+  unsigned int said = 0u;
+  if ((threadIdx.x & 31) == 0) {
+    said = *reinterpret_cast<volatile unsigned int *>(verdict);
+    while (said >> 1 != mine >> 1) {
+      const unsigned int before = atomicCAS(verdict, said, mine);
+      said = before == said ? mine : before;
+    }
+  }
+  if (!(__shfl_sync(0xffffffffu, said, 0) & 1u)) return false;
+  mbar_wait_drain(bar, parity, CA_WAIT_LIMIT);            // (complete: another warp has seen it)
+  __syncwarp();
+  return true;
+}
+__device__ __forceinline__ bool mbar_try_all(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)); }
+
 // Keys and values with a tile's box for one, two and four heads together.
 struct CaMaps {
   CUtensorMap k[3], v[3];
@@ -505,11 +551,16 @@ struct CaMaps {
 
 struct CaBook {
   uint64_t full[CA_STAGES], empty[CA_STAGES], job_full[CA_JOBS], job_empty[CA_JOBS];
-  int warp_part[8];
+  int warp_part[7];
+  unsigned int verdict;                    // see ca_wait_on_item
   int abort_flag;
   float2 ml[2][StreamWork::ROWS];
   CaJob job[CA_JOBS];
 };
+
+// Named barriers of two warps: one arrives, the other waits.
+__device__ __forceinline__ void pair_arrive(int id) { asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void pair_sync(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
 // The entries of the query rows, for the join: a block takes every gridDim.x-th sequence.
 __device__ __forceinline__ void ca_describe_rows(const CacheArgs &a, const int *off, const CaSeg *segs, int n_seg, int thread, int threads) {
@@ -544,10 +595,6 @@ __device__ __forceinline__ void ca_describe_rows(const CacheArgs &a, const int *
     }
   }
 }
-
-// Named barriers of two warps: one arrives, the other waits.
-__device__ __forceinline__ void pair_arrive(int id) { asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
-__device__ __forceinline__ void pair_sync(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
 // One (maximum, sum, values) of a query row and another one: factors of both.  (What has no maximum has sums of zero.)
 __device__ __forceinline__ void ca_merge(float &m, float &l, float2 other, float &f, float &g) {
@@ -586,6 +633,7 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
       mbar_init(smem_u32(&bk->job_empty[s]), CA_CONSUMERS);
     }
     bk->abort_flag = 0;
+    bk->verdict = 0u;
     fence_barrier_init();
   }
   if (threadIdx.x < 3) {
@@ -624,10 +672,13 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
         more = walk.next(a, off, segs, j);
       }
       if (!more) j.n = -1;
-      // The queue of items keeps working after an abort (its waits ignore the flag and are bounded on their own): all consumers must
-      // see the same sequence, ending with -1.
-      if (jc >= CA_JOBS) mbar_wait_drain(smem_u32(&bk->job_empty[slot]), ((jc / CA_JOBS) - 1) & 1, CA_WAIT_LIMIT);
-      __syncwarp();
+      // (the queue keeps working after an abort: all consumers see the same items, up to the one with -1)
+      if (jc >= CA_JOBS && !mbar_try_all(smem_u32(&bk->job_empty[slot]), ((jc / CA_JOBS) - 1) & 1) &&
+          !ca_wait_on(smem_u32(&bk->job_empty[slot]), ((jc / CA_JOBS) - 1) & 1, &bk->abort_flag, a.status, a.wait_limit)) {
+        // (its consumers may have left too: the query rows on their way land first)
+        for (int s = 0; s < CA_JOBS; ++s) mbar_settle(smem_u32(&bk->job_full[s]), ((jc - CA_JOBS + (s < slot ? CA_JOBS : 0)) / CA_JOBS) & 1, wc);
+        break;
+      }
       const bool going = more && !__shfl_sync(0xffffffffu, bk->abort_flag, 0);
       const uint32_t jbar = smem_u32(&bk->job_full[slot]);
       if (lane == 0) {
@@ -664,7 +715,7 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
     // every copy issued has landed before the block leaves (the consumers wait for the query rows whatever happens)
     for (int s = 0; s < CA_STAGES; ++s) {
       const int fills = issued > s ? (issued - s + CA_STAGES - 1) / CA_STAGES : 0;
-      if (fills > 0) mbar_wait_drain(smem_u32(&bk->full[s]), (fills - 1) & 1, CA_WAIT_LIMIT);
+      if (fills > 0) mbar_settle(smem_u32(&bk->full[s]), (fills - 1) & 1, wc);
     }
     // the block that leaves last puts the counters back to zero for the next launch (every block has drawn its last piece by then)
     if (pieces > (int)gridDim.x && lane == 0 && atomicAdd(a.work + 1, 1u) == gridDim.x - 1) {
@@ -684,10 +735,11 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
   bool handed = false;                           // (warps 2 and 3) the buffer holds something that may not have been read yet
   for (int jc = 0;; ++jc) {
     const int slot = jc % CA_JOBS;
-    const bool got = mbar_wait_drain(smem_u32(&bk->job_full[slot]), (jc / CA_JOBS) & 1, CA_WAIT_LIMIT);
-    __syncwarp();
+    if (!mbar_try_all(smem_u32(&bk->job_full[slot]), (jc / CA_JOBS) & 1) &&
+        !ca_wait_on_item(&bk->verdict, jc, smem_u32(&bk->job_full[slot]), (jc / CA_JOBS) & 1, &bk->abort_flag, a.status, a.wait_limit))
+      break;
     const CaJob j = bk->job[slot];
-    if (!got || j.n < 0) break;
+    if (j.n < 0) break;
     const bool two = j.R > 8;                    // rows 8 .. 15 are in use
     // Four heads together: a warp each.  Two: warps 0 and 2, 1 and 3 share one's keys.  One: all four do.
     const int hg = j.together, sub = warp & (hg - 1), slice = warp / hg, keys = StreamWork::KEYS / hg, head = j.head + sub;
@@ -1075,15 +1127,14 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
   WaitCtx wc{&bk->abort_flag, a.status, STATUS_CACHE_TIMEOUT, a.wait_limit};
   pdl_enter();
   const bool stop = ca_plan<TileWork, CT_THREADS>(a, off, segs, n_seg, bk->warp_part);
-  // the next item; false: there is none
+  // the next item; false: there is none, or the block gives up
   auto take = [&](int jc, CaJob &j) {
     const int slot = jc % CT_JOBS;
-    const bool got = mbar_wait_drain(smem_u32(&bk->job_full[slot]), (jc / CT_JOBS) & 1, CA_WAIT_LIMIT);
-    __syncwarp();
+    if (!mbar_wait_all(smem_u32(&bk->job_full[slot]), (jc / CT_JOBS) & 1, wc)) return false;
     j = bk->job[slot];
     __syncwarp();
     mbar_arrive_lane0(smem_u32(&bk->job_empty[slot]), lane);
-    return got && j.n >= 0;
+    return j.n >= 0;
   };
 
   // The launch gives every thread 168 registers; a softmax thread holds its row's 128 logits and needs more, the first
@@ -1111,9 +1162,9 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
         } else {
           j.n = -1;
         }
-        // (the queue of items keeps working after an abort: every consumer must see the same sequence, ending with -1)
-        if (jc >= CT_JOBS) mbar_wait_drain(smem_u32(&bk->job_empty[slot]), ((jc / CT_JOBS) - 1) & 1, CA_WAIT_LIMIT);
-        __syncwarp();
+        // (after an abort nothing more is announced: the flag ends every wait of the consumers)
+        if (jc >= CT_JOBS && !mbar_wait_all(smem_u32(&bk->job_empty[slot]), ((jc / CT_JOBS) - 1) & 1, wc)) break;
+        if (__shfl_sync(0xffffffffu, bk->abort_flag, 0)) break;
         if (lane == 0) bk->job[slot] = j;
         mbar_arrive_lane0(smem_u32(&bk->job_full[slot]), lane);
         if (!more) break;
@@ -1139,8 +1190,8 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       // every copy issued has landed before the block leaves
       for (int s = 0; s < CT_SLOTS; ++s) {
         const int fills = issued > s ? (issued - s + CT_SLOTS - 1) / CT_SLOTS : 0;
-        if ((raw_any >> s) & 1u) mbar_wait_drain(smem_u32(&bk->raw[s]), ((raw_odd >> s) & 1u) ^ 1u, CA_WAIT_LIMIT);
-        if (fills > 0 && !((raw_last >> s) & 1u)) mbar_wait_drain(smem_u32(&bk->full[s]), (fills - 1) & 1, CA_WAIT_LIMIT);
+        if ((raw_any >> s) & 1u) mbar_settle(smem_u32(&bk->raw[s]), ((raw_odd >> s) & 1u) ^ 1u, wc);
+        if (fills > 0 && !((raw_last >> s) & 1u)) mbar_settle(smem_u32(&bk->full[s]), (fills - 1) & 1, wc);
       }
       __syncwarp();
     } else if (warp == 1) {
@@ -1195,7 +1246,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       }
       // every MMA this warp issued has completed before tensor memory is given back
       tc_commit_w(smem_u32(&bk->mma_done), leader);
-      mbar_wait_drain(smem_u32(&bk->mma_done), 0, CA_WAIT_LIMIT);
+      mbar_settle(smem_u32(&bk->mma_done), 0, wc);
       __syncwarp();
     } else if (warp == 2) {
       // ---------------------------------------------------------------- value rows that must not reach every query row
@@ -1304,7 +1355,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       }
       // every copy issued has landed before the block leaves
       for (int g = 0; g < 2; ++g)
-        if ((g ? tiled[1] : tiled[0]) > 0) mbar_wait_drain(smem_u32(&bk->q_full[g]), ((g ? tiled[1] : tiled[0]) - 1) & 1, CA_WAIT_LIMIT);
+        if ((g ? tiled[1] : tiled[0]) > 0) mbar_settle(smem_u32(&bk->q_full[g]), ((g ? tiled[1] : tiled[0]) - 1) & 1, wc);
       __syncwarp();
     }
   } else {

@@ -804,3 +804,49 @@ def test_a_wait_that_runs_out_is_reported_and_the_context_recovers(ctx, nq):
     c.run(ctx)
     A.asap_check(ctx)
     assert torch.equal(c.out, good)
+
+
+GIVING_UP = {
+    "one_head": dict(lens=[30000, 9000], nq=[1, 1], H=14, kv=2),
+    "rows_eight_and_up": dict(lens=[20000, 3000], nq=[3, 2], H=40, kv=8),
+    "two_heads_together": dict(lens=[4000] * 40, nq=[2] * 40, H=16, kv=4),
+    "four_heads_together": dict(lens=[3000] * 60, nq=[1] * 60, H=32, kv=32),
+    "tiles_and_streams": dict(lens=[2000] * 12, nq=[1] * 6 + [40] * 6, H=32, kv=8, groups=[(0, 8, 3000), (8, 12, 500)]),
+    "short_items": dict(lens=[70] * 100, nq=[3] * 100, H=32, kv=8, groups=[(0, 60, 400), (60, 100, 130)]),
+}
+
+
+@pytest.mark.parametrize("weights", [False, True], ids=["", "weights"])
+@pytest.mark.parametrize("name", GIVING_UP)
+def test_a_wait_that_gives_up_is_never_silent(ctx, name, weights):
+    """Limits from a clock to more than any wait takes, so that waits of every kind run out, in some blocks and warps and not in others: the
+    call comes to an end and is reported, or its results are right to the last bit."""
+    c = Case(**GIVING_UP[name], dtype=torch.bfloat16, seed=50, weights=weights)
+    base = c.weights.clone() if weights else None
+    args = c.args()
+    scratch = torch.full((A.asap_cache_attention_scratch_bytes(ctx, args),), 0x7f, dtype=torch.uint8, device=DEV)
+
+    def go():
+        c.out.fill_(7)
+        c.lse.fill_(7)
+        if weights:
+            c.weights.copy_(base)
+        A.asap_cache_attention(ctx, args, scratch)
+        return [t.clone() for t in (c.out, c.lse, c.weights) if t is not None]
+
+    want = go()
+    A.asap_check(ctx)
+    reported = 0
+    for limit in [1, 10, 40, 100, 250, 500, 800, 1200, 2000, 4000, 8000, 16000, 50000, 200000, 10 ** 9]:
+        A.asap_debug_wait_limit(ctx, limit)
+        got = go()
+        try:
+            A.asap_check(ctx)
+        except A.AsapError as e:
+            assert e.status == -6 and "cache attention" in str(e) and limit < 10 ** 9
+            reported += 1
+            continue
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), limit
+    assert reported > 0
+    assert all(torch.equal(a, b) for a, b in zip(go(), want))
+    A.asap_check(ctx)
