@@ -1072,7 +1072,8 @@ struct CtBook {
   int warp_part[CT_THREADS / 32];
   uint32_t tmem_base;
   int abort_flag;
-  int bad[4];              // the item (modulo 4) has value rows with infinities or NaN that not all of its query rows admit
+  int bad[2 * CT_JOBS];    // the item (modulo their number) has value rows with infinities or NaN that not all of its query rows admit.  The softmax warps
+                           // read it at the item's end; warp 2 may then be CT_JOBS items further on, where the next one's announcement waits for them
 };
 
 // Key tile kt holds rows that not all query rows of the pair admit: its values pass through warp 2.
@@ -1111,7 +1112,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
     mbar_init(smem_u32(&bk->s_empty), 4);                 // the softmax warps that have taken an S into registers
     mbar_init(smem_u32(&bk->mma_done), 1);
     bk->abort_flag = 0;
-    for (int i = 0; i < 4; ++i) bk->bad[i] = 0;
+    for (int i = 0; i < 2 * CT_JOBS; ++i) bk->bad[i] = 0;
     fence_barrier_init();
     tma_prefetch_desc(&tmap_k);
     tma_prefetch_desc(&tmap_v);
@@ -1256,7 +1257,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       uint32_t raw_phase = 0u;                    // per ring slot
       CaJob j;
       for (int jc = 0; take(jc, j); ++jc) {
-        if (lane == 0) *reinterpret_cast<volatile int *>(&bk->bad[jc & 3]) = 0;
+        if (lane == 0) *reinterpret_cast<volatile int *>(&bk->bad[jc % (2 * CT_JOBS)]) = 0;
         __syncwarp();
         for (int k = 0; k < j.n; ++k) {
           const int kt = j.kt0 + k;
@@ -1293,7 +1294,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
               }
               *p = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            if (lane == 0) *reinterpret_cast<volatile int *>(&bk->bad[jc & 3]) = 1;
+            if (lane == 0) *reinterpret_cast<volatile int *>(&bk->bad[jc % (2 * CT_JOBS)]) = 1;
           }
           __threadfence_block();
           fence_proxy_async();
@@ -1497,7 +1498,7 @@ ca_tile_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       if (at >= 0 && write) (complete ? a.full_ml : a.rec_ml[1])[at] = none ? make_float2(-INFINITY, 0.f) : make_float2(-neg_ref, l_run);
       if (n_act == 0) continue;
       float *dst = complete ? a.full_o : a.rec_o[1];
-      const bool bad = *reinterpret_cast<volatile int *>(&bk->bad[jc & 3]) != 0;
+      const bool bad = *reinterpret_cast<volatile int *>(&bk->bad[jc % (2 * CT_JOBS)]) != 0;
       // (A thread stores its own row, 32 bytes at a time: whole sectors.)
 #pragma unroll 1
       for (int c0 = 0; c0 < 128; c0 += 32) {

@@ -320,6 +320,31 @@ def test_a_query_row_does_not_see_later_rows(ctx, value, which, name, H, kv, nq)
         assert torch.isnan(c.out[t:]).all()
 
 
+@pytest.mark.parametrize("value", [float("nan"), float("inf")], ids=["nan", "inf"])
+def test_values_of_late_rows_where_items_follow_each_other(ctx, value):
+    """Items of two row tiles between items of one, several to a block, most with an infinity or NaN in a value row that only their last query
+    rows admit: each item's mark reaches its own rows, and only those."""
+    nq = [[200, 30, 40, 60, 20, 35][i % 6] for i in range(280)]
+    c = Case(lens=[n + i % 5 for i, n in enumerate(nq)], nq=nq, H=4, kv=4, dtype=torch.bfloat16, seed=51, weights=False)
+    hit = [i for i in range(280) if i % 6 != 3]
+    row = torch.tensor([c.start[b] + c.len[b] - 3 for b in hit], device=DEV)
+    admits = torch.zeros(sum(nq), dtype=torch.bool, device=DEV)
+    for b in hit:
+        admits[c.q_cu[b + 1] - 3:c.q_cu[b + 1]] = True
+    c.v[row, :, 5] = 0.0
+    c.run(ctx)
+    good = c.out.clone()
+    assert torch.isfinite(good).all()
+    c.v[row, :, 5] = value
+    want = good.clone()
+    want[admits, :, 5] = value
+    for _ in range(5):
+        c.out.fill_(7)
+        c.run(ctx)
+        A.asap_check(ctx)
+        assert torch.equal(c.out.nan_to_num(123.0, 456.0), want.nan_to_num(123.0, 456.0))
+
+
 def test_nan_queries_stay_in_their_rows(ctx):
     c = Case(lens=[150, 80], nq=[3, 1], H=4, kv=2, dtype=torch.bfloat16, seed=9, weights=False, groups=[(0, 2, 90)])
     c.run(ctx)
