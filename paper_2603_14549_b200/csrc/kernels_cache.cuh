@@ -27,6 +27,12 @@ enum : uint32_t { STATUS_CACHE_TIMEOUT = 64u };   // a bounded wait ran out in a
 __device__ __forceinline__ void ld_prev8(const void *p, uint4 &v) {
   asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
 }
+// In place of pdl_enter in a kernel whose predecessor has waited for all that this one reads, before it let this one start.  That lies in L2 by now.
+// A processor's L1 may hold older copies, which the wait would have dropped: the fence does (what this thread loads from here on is no older).
+__device__ __forceinline__ void pdl_after() {
+  pdl_trigger();
+  __threadfence();
+}
 template <bool F16>
 __device__ __forceinline__ uint32_t pack2_t(float a, float b) {
   if constexpr (F16) {
@@ -645,7 +651,7 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
   // Behind the tile kernel of the same call: nothing but that kernel's plan is needed from it, and its blocks have all waited for what
   // precedes the call before this kernel can start.  So this one fills the processors that it leaves, and waits for its end at its own.
   const bool behind = a.pieces[1] != 0;
-  if (behind) pdl_trigger();
+  if (behind) pdl_after();
   else pdl_enter();
   const bool stop = ca_plan<StreamWork, CA_THREADS>(a, off, segs, n_seg, bk->warp_part);
 
@@ -1629,7 +1635,7 @@ ca_join_kernel(const __grid_constant__ CacheArgs a) {
   __shared__ float2 sh_ml[SPLIT ? CA_JOIN_WARPS : 1];
   // Behind the weights' kernel: its blocks have all waited for the partial results before this kernel can start, and nothing of its own is
   // needed.  The wait for its end comes last.
-  if (a.join_behind) pdl_trigger();
+  if (a.join_behind) pdl_after();
   else pdl_enter();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_seg = a.G + a.B, h0 = blockIdx.y * HEADS;
   // every query row of [q_cu[0], q_cu[B]) has an entry of this call unless the call is skipped

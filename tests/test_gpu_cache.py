@@ -814,6 +814,51 @@ def test_prune_then_decode_with_eviction(ctx):
     A.asap_check(ctx)
 
 
+def _decode(ctx, steps, wait, H, kv, seqs, groups, weights):
+    """Slot, rotation and attention `steps` times, every call's arrays written by the call before it; with `wait` the host waits for each call."""
+    cap, pre = 30, 200
+    rows, G = len(groups) * pre + seqs * cap, len(groups)
+    g = gen(77)
+    kc, vc = torch.randn(rows, kv, HEAD, device=DEV, generator=g).to(torch.bfloat16), torch.randn(rows, kv, HEAD, device=DEV, generator=g).to(torch.bfloat16)
+    start, length = i32([G * pre + b * cap for b in range(seqs)]), i32([b % cap for b in range(seqs)])
+    w, pos = torch.zeros(rows, device=DEV), torch.zeros(rows, dtype=torch.int32, device=DEV)
+    for b in range(seqs):
+        pos[G * pre + b * cap:G * pre + (b + 1) * cap] = torch.arange(cap, dtype=torch.int32, device=DEV)
+    new_pos, row = [i32([cap + s] * seqs) for s in range(steps)], i32([0] * seqs)
+    qkv = torch.randn(steps, seqs, H + 2 * kv, HEAD, device=DEV, generator=g).to(torch.bfloat16)
+    qr, out, lse = torch.empty(seqs, H, HEAD, dtype=torch.bfloat16, device=DEV), torch.empty(steps, seqs, H, HEAD, dtype=torch.bfloat16, device=DEV), torch.empty(seqs, H, device=DEV)
+    plan, calls, scratch = A.asap_rope_make(HEAD), [], None
+    kw = dict(group_cu=i32([0] + [b1 for _, b1 in groups]), prefix_start=i32([i * pre for i in range(G)]), prefix_len=i32([pre - i for i in range(G)]),
+              max_prefix=pre) if groups else {}
+    for s in range(steps):
+        q, k, v = qkv[s, :, :H], qkv[s, :, H:H + kv], qkv[s, :, H + kv:]
+        slot = A.CacheSlot(start, length, cap, w, pos, new_pos[s], row, sink=1, recent=3)
+        rope = A.RopeArgs(new_pos[s], [A.RopeTensor(q, qr), A.RopeTensor(k, kc, mapped=True), A.RopeTensor(v, vc, mapped=True, rotate=False)], dst_row=row)
+        att = A.CacheAttention(qr, kc, vc, out[s], start, length, max_len=cap, lse=lse, weights=w if weights else None, **kw)
+        if scratch is None:
+            scratch = torch.empty(A.asap_cache_attention_scratch_bytes(ctx, att), dtype=torch.uint8, device=DEV)
+        calls += [lambda x=slot: A.asap_cache_slot(ctx, x), lambda x=rope: A.asap_rope(ctx, plan, x), lambda x=att: A.asap_cache_attention(ctx, x, scratch)]
+    torch.cuda.synchronize()
+    for call in calls:
+        call()
+        if wait:
+            torch.cuda.synchronize()
+    A.asap_check(ctx)
+    return out, lse, w, pos, length, kc, vc
+
+
+@pytest.mark.parametrize("weights", [False, True], ids=["", "weights"])
+@pytest.mark.parametrize("H,kv,seqs,groups", [(8, 2, 12, [(0, 12)]), (16, 16, 40, [(0, 18), (18, 40)]), (8, 8, 1, []), (32, 8, 2, []), (4, 4, 30, [(0, 3), (3, 30)])],
+                         ids=["tiles", "more_tiles", "one_request", "two_requests", "both"])
+def test_steps_that_nobody_waits_between(ctx, H, kv, seqs, groups, weights):
+    """Lengths, rows, queries and keys that a call has just written are what the next one reads, through the same buffers step after step."""
+    steps = 40
+    want = _decode(ctx, steps, True, H, kv, seqs, groups, weights)
+    for _ in range(4):
+        got = _decode(ctx, steps, False, H, kv, seqs, groups, weights)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("nq", [[1, 1], [20, 40]], ids=["streamed", "tiles"])
 def test_a_wait_that_runs_out_is_reported_and_the_context_recovers(ctx, nq):
     # (long enough that every block has more tiles than its ring holds: some wait cannot be satisfied at once)
