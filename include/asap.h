@@ -321,7 +321,8 @@ typedef struct {
 } asap_cache_attention_args;
 
 /* `scratch`: caller-owned device memory of at least asap_cache_attention_scratch_bytes bytes (a function of the sizes and of whether
- * weights are given; 0 for arguments that the call refuses), 256-byte aligned; nothing is kept in it between calls.  Calls that may
+ * weights are given; 0 for sizes or an element type that the call refuses, with the reason in asap_last_error(NULL)), 256-byte aligned;
+ * nothing is kept in it between calls.  Calls that may
  * run at the same time need scratch of their own.  May be recorded by a stream capture; a replay uses the lengths that the arrays
  * hold then, within the bounds given. */
 size_t asap_cache_attention_scratch_bytes(const asap_ctx *ctx, const asap_cache_attention_args *args);
@@ -376,8 +377,8 @@ asap_status asap_cache_slot(asap_ctx *ctx, const asap_cache_slot_args *args, voi
 asap_status asap_check(asap_ctx *ctx, void *stream);
 
 /* Text of the last error recorded on this context (empty string if none).  Valid until the
- * next call on the context.  asap_last_error(NULL) describes a failed asap_init or
- * asap_select_static; that text lives in one buffer shared by all threads of the process. */
+ * next call on the context.  asap_last_error(NULL) describes a failed asap_init, asap_rope_make or
+ * asap_select_static, or sizes that asap_cache_attention_scratch_bytes refuses; that text lives in one buffer shared by all threads of the process. */
 const char *asap_last_error(const asap_ctx *ctx);
 
 /* Step 3 once more, for callers that cannot allocate device memory.  (The paper has no

@@ -39,7 +39,10 @@ bool strides_disjoint(long long rows, long long heads, long long dim, long long 
 constexpr int MAX_ROWS = 1 << 30;              // rows that 32-bit counters walk in strides
 constexpr long long MAX_STRIDE = 1LL << 39;    // elements of two bytes (a tensor map's strides are below 2^40 bytes)
 
-asap_status check_cache_attention(asap_ctx *ctx, const asap_cache_attention_args *p) {
+constexpr long long CA_MAX_NUMBERS = 1LL << 30;    // key tiles are numbered in 32 bits
+
+// The sizes and the type, which are all that the scratch depends on.  What passes keeps the layout's products within 64 bits.
+asap_status check_cache_sizes(asap_ctx *ctx, const asap_cache_attention_args *p) {
   const char *who = "asap_cache_attention";
   if (!p) return fail(ctx, ASAP_ERR_INVALID, "%s: null arguments", who);
   if (p->B <= 0 || p->H <= 0 || p->kv_heads <= 0 || p->n_q <= 0 || p->max_q <= 0 || p->cache_rows <= 0)
@@ -51,8 +54,14 @@ asap_status check_cache_attention(asap_ctx *ctx, const asap_cache_attention_args
   if (p->max_len < 0 || p->max_prefix < 0 || p->n_groups < 0 || p->max_len > p->cache_rows || p->max_prefix > p->cache_rows)
     return fail(ctx, ASAP_ERR_INVALID, "%s: need 0 <= max_len, max_prefix <= cache_rows and n_groups >= 0", who);
   if (p->max_q > p->n_q || p->n_groups > p->B) return fail(ctx, ASAP_ERR_INVALID, "%s: need max_q <= n_q and n_groups <= B", who);
-  if (p->B + p->n_groups > CA_MAX_SEGMENTS)
+  if ((long long)p->B + p->n_groups > CA_MAX_SEGMENTS)
     return fail(ctx, ASAP_ERR_UNSUPPORTED, "%s: at most %d sequences and groups in a call", who, CA_MAX_SEGMENTS);
+  if ((long long)p->n_q * p->H > CA_MAX_NUMBERS / 2) return fail(ctx, ASAP_ERR_UNSUPPORTED, "%s: n_q and H are too large together", who);
+  return ASAP_OK;
+}
+asap_status check_cache_attention(asap_ctx *ctx, const asap_cache_attention_args *p) {
+  const char *who = "asap_cache_attention";
+  ASAP_TRY(check_cache_sizes(ctx, p));
   if (!(p->scale >= 0.f) || p->scale > 1e30f) return fail(ctx, ASAP_ERR_INVALID, "%s: scale must be finite and not negative", who);
   if (!p->q || !p->k || !p->v || !p->out || !p->start || !p->len) return fail(ctx, ASAP_ERR_INVALID, "%s: null q / k / v / out / start / len", who);
   if (p->n_groups > 0 && (!p->group_cu || !p->prefix_start || !p->prefix_len))
@@ -74,6 +83,8 @@ asap_status check_cache_attention(asap_ctx *ctx, const asap_cache_attention_args
   return ASAP_OK;
 }
 
+constexpr const char *CA_TOO_LARGE = "asap_cache_attention: max_q, max_len, max_prefix and the batch are too large together";
+
 // Scratch of a call; `at` NULL: only its size.
 struct CaLayout {
   size_t bytes = 0;
@@ -85,7 +96,6 @@ struct CaLayout {
   int own_lanes = 0, pre_lanes = 0;          // threads side by side on the keys
   long long own_blocks = 0, pre_blocks = 0;  // blocks of a sequence and of a prefix
 };
-constexpr long long CA_MAX_NUMBERS = 1LL << 30;    // key tiles are numbered in 32 bits
 CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint8_t *at, CacheArgs *a) {
   CaLayout l;
   const size_t entries = (size_t)p->n_q * p->H, n_seg = (size_t)p->B + p->n_groups;
@@ -108,7 +118,7 @@ CaLayout ca_layout(const asap_ctx *ctx, const asap_cache_attention_args *p, uint
   const long long group_max = group_rows > 0 ? (group_rows < S ? group_rows : S) : 0, own_max = own_rows < S ? own_rows : S;
   const long long rows_max = group_max > own_max ? group_max : own_max;
   l.rec_rows = (int)(4 * rows_max < S ? 4 * rows_max : S);           // (as many heads together as make up to 16 rows)
-  l.too_large = streamed > CA_MAX_NUMBERS || tiled > CA_MAX_NUMBERS || (long long)entries > CA_MAX_NUMBERS / 2;
+  l.too_large = streamed > CA_MAX_NUMBERS || tiled > CA_MAX_NUMBERS;
   if (p->weights) {
     const auto lanes_of = [](long long pairs) { return pairs <= 64 ? 64 : pairs <= 512 ? 16 : 4; };
     l.few = p->n_groups == 0 && (long long)p->max_q * p->H <= CA_FEW_PAIRS && p->max_len > 0;
@@ -279,10 +289,11 @@ asap_status asap_rope(asap_ctx *ctx, const asap_rope_plan *plan, const asap_rope
 }
 
 size_t asap_cache_attention_scratch_bytes(const asap_ctx *ctx, const asap_cache_attention_args *p) {
-  if (!ctx || !p || p->B <= 0 || p->H <= 0 || p->kv_heads <= 0 || p->H % p->kv_heads != 0 || p->n_q <= 0 || p->max_len < 0 || p->max_prefix < 0 ||
-      p->n_groups < 0 || p->max_q <= 0)
-    return 0;
-  return ca_layout(ctx, p, nullptr, nullptr).bytes;
+  if (!ctx || check_cache_sizes(nullptr, p) != ASAP_OK) return 0;
+  const CaLayout layout = ca_layout(ctx, p, nullptr, nullptr);
+  if (!layout.too_large) return layout.bytes;
+  fail(nullptr, ASAP_ERR_UNSUPPORTED, CA_TOO_LARGE);
+  return 0;
 }
 
 asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args *p, void *scratch, size_t scratch_bytes, void *stream) {
@@ -291,7 +302,7 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
   ASAP_TRY(check_cache_attention(ctx, p));
   CacheArgs a;
   const CaLayout layout = ca_layout(ctx, p, static_cast<uint8_t *>(scratch), &a);
-  if (layout.too_large) return fail(ctx, ASAP_ERR_UNSUPPORTED, "asap_cache_attention: max_q, max_len, max_prefix and the batch are too large together");
+  if (layout.too_large) return fail(ctx, ASAP_ERR_UNSUPPORTED, CA_TOO_LARGE);
   if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255u) != 0 || scratch_bytes < layout.bytes)
     return fail(ctx, ASAP_ERR_WORKSPACE, "asap_cache_attention: scratch is null, not 256-byte aligned or smaller than asap_cache_attention_scratch_bytes");
   CaMaps maps;

@@ -145,6 +145,18 @@ def test_scratch_of_attention(lib, ctx):
     assert lib.asap_cache_attention(ctx, C.byref(_attend()), 4096 + 16, 1 << 40, None) == -3
 
 
+@pytest.mark.parametrize("kw", [dict(head_dim=64), dict(head_dim=256), dict(dtype=7), dict(B=1025, n_q=1025), dict(B=1000, n_q=1000, n_groups=30), dict(max_q=3),
+                                dict(max_q=0), dict(n_groups=3), dict(n_groups=-1), dict(max_len=1001), dict(max_prefix=1001), dict(cache_rows=0), dict(H=65537, kv_heads=1),
+                                dict(B=2 ** 31 - 1, n_q=2 ** 31 - 1, n_groups=1), dict(n_q=1 << 23, H=128, q_cu=4096), dict(n_q=2 ** 31 - 1, max_q=2 ** 31 - 1, H=65536),
+                                dict(B=1000, n_q=1000, H=1 << 16, kv_heads=1 << 16, max_len=2 ** 31 - 1, cache_rows=2 ** 31 - 1),
+                                dict(B=1023, H=513, kv_heads=1, n_q=1, max_len=38_600_000, cache_rows=38_600_000, weights=4096)])
+def test_scratch_of_sizes_that_attention_refuses(lib, ctx, kw):
+    assert lib.asap_cache_attention_scratch_bytes(ctx, C.byref(_attend(**kw))) == 0
+    assert b"asap_cache_attention" in lib.asap_last_error(None)
+    st = lib.asap_cache_attention(ctx, C.byref(_attend(**kw)), 4096, 1 << 40, None)
+    assert st in (-1, -5)
+
+
 def _evict(**kw):
     src, dst = (C.c_void_p * 2)(1 << 20, 1 << 22), (C.c_void_p * 2)(1 << 24, 1 << 26)
     for f in list(kw):
