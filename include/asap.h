@@ -323,7 +323,9 @@ typedef struct {
 /* `scratch`: caller-owned device memory of at least asap_cache_attention_scratch_bytes bytes (a function of the sizes and of whether
  * weights are given; 0 for sizes or an element type that the call refuses, with the reason in asap_last_error(NULL)), 256-byte aligned;
  * nothing is kept in it between calls.  Calls that may
- * run at the same time need scratch of their own.  May be recorded by a stream capture; a replay uses the lengths that the arrays
+ * run at the same time need a context AND scratch of their own: the calls of one context share the counters by which their blocks
+ * draw work, and two that overlap leave parts of it out.  Two captured graphs that may be replayed at the same time likewise.  May be
+ * recorded by a stream capture; a replay uses the lengths that the arrays
  * hold then, within the bounds given. */
 size_t asap_cache_attention_scratch_bytes(const asap_ctx *ctx, const asap_cache_attention_args *args);
 asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args *args, void *scratch, size_t scratch_bytes,
