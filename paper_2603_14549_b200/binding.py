@@ -497,7 +497,9 @@ def asap_cache_attention_scratch_bytes(ctx, args: CacheAttention) -> int:
 
 
 def asap_cache_attention(ctx, args: CacheAttention, scratch: torch.Tensor, stream=None) -> None:
-    """`scratch`: a contiguous device tensor of at least asap_cache_attention_scratch_bytes(ctx, args) bytes."""
+    """`scratch`: a contiguous tensor of at least asap_cache_attention_scratch_bytes(ctx, args) bytes on the device of the others."""
+    if scratch.device != args.device or not scratch.is_contiguous():
+        raise ValueError(f"scratch must be a contiguous tensor on {args.device}")
     status = (_lib or load_library()).asap_cache_attention(ctx, args.ref, scratch.data_ptr(), scratch.nbytes, _stream_of(args.device, stream))
     if status:
         _raise(ctx, status)

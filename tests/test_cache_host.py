@@ -1,8 +1,10 @@
 """What the calls around the key / value cache decide on the host, without a GPU: struct layouts, rotation plans, refusals."""
 import ctypes as C
 import math
+import types
 
 import pytest
+import torch
 
 from paper_2603_14549_b200 import binding as A
 from paper_2603_14549_b200 import build
@@ -155,6 +157,21 @@ def test_scratch_of_sizes_that_attention_refuses(lib, ctx, kw):
     assert b"asap_cache_attention" in lib.asap_last_error(None)
     st = lib.asap_cache_attention(ctx, C.byref(_attend(**kw)), 4096, 1 << 40, None)
     assert st in (-1, -5)
+
+
+@pytest.mark.parametrize("scratch", [torch.empty(1 << 16, dtype=torch.uint8), torch.empty(1 << 16, dtype=torch.uint8, device="meta"),
+                                     torch.empty(64, 64, dtype=torch.uint8, device="meta").t()], ids=["cpu", "meta", "strided"])
+def test_scratch_that_is_no_contiguous_tensor_of_the_device_is_refused(lib, ctx, monkeypatch, scratch):
+    """... before the library is called: on the GPU its address would be a bad one."""
+    class Never:
+        def __getattr__(self, name):
+            raise AssertionError("the library was called")
+
+    monkeypatch.setattr(A, "_lib", Never())
+    a = _attend()
+    device = torch.device("meta") if not scratch.is_contiguous() else torch.device("cuda", 0)
+    with pytest.raises(ValueError):
+        A.asap_cache_attention(ctx, types.SimpleNamespace(device=device, ref=C.addressof(a), c=a), scratch, stream=0)
 
 
 def _evict(**kw):
