@@ -52,6 +52,7 @@ struct asap_ctx {
   long long sim_pair_min_blocks = 0;        // blocks from which the similarity takes two row tiles per block (0: half the SM count)
   int sim_pair_stages = 0;                  // stages of that form (0: what fits 192 KB)
   int sim_cluster = 1;                      // 0: sliced similarity launches add their partials through global memory
+  int evict_cluster = 1;                    // 0: evictions of long sequences are ranked by one block each, like the others
   float *sim_part = nullptr;        // partial dot products / squared norms of a sliced similarity GEMM
   size_t sim_part_bytes = 0, cap_tiles = 0;
   int32_t *role = nullptr, *seg = nullptr, *members = nullptr;
@@ -207,6 +208,24 @@ void launch_pdl_cluster_z(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+// Whether the device can hold a cluster of `cluster_z` such blocks.
+template <typename... KArgs>
+bool cluster_fits(void (*kernel)(KArgs...), int cluster_z, int threads, size_t smem) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(1, 1, (unsigned)cluster_z);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = (unsigned)cluster_z;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int clusters = 0;
+  if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters >= 1) return true;
+  cudaGetLastError();
+  return false;
 }
 
 asap_status after_launch(asap_ctx *ctx, const char *what) {
@@ -824,6 +843,7 @@ asap_status asap_init(asap_ctx **ctx_out, int device, size_t max_total_tokens, i
   if (const char *env = getenv("ASAP_SIM_PAIR_MIN_BLOCKS")) ctx->sim_pair_min_blocks = atoll(env);
   if (const char *env = getenv("ASAP_SIM_PAIR_STAGES")) ctx->sim_pair_stages = atoi(env);
   if (const char *env = getenv("ASAP_SIM_CLUSTER")) ctx->sim_cluster = atoi(env);
+  if (const char *env = getenv("ASAP_EVICT_CLUSTER")) ctx->evict_cluster = atoi(env);
   ctx->head_norm = reinterpret_cast<float *>(ctx->arena + o_hnorm);
   ctx->kept_inv = reinterpret_cast<float *>(ctx->arena + o_kinv);
   ctx->counters_off = o_cnt; ctx->counters_bytes = n_cnt * sizeof(unsigned int);
@@ -858,24 +878,10 @@ asap_status asap_init(asap_ctx **ctx_out, int device, size_t max_total_tokens, i
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ca_smem_bytes(CA_MAX_SEGMENTS));
   for (auto kernel : {ca_tile_kernel<false, false>, ca_tile_kernel<false, true>, ca_tile_kernel<true, false>, ca_tile_kernel<true, true>})
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ct_smem_bytes(CA_MAX_SEGMENTS));
-  if (e == cudaSuccess && ctx->sim_cluster) {
-    // the cluster form of the sliced similarity launch needs eight co-resident blocks of up to 195 KB each in one
-    // cluster; where the device (or the partition of it this process sees) cannot place one, the form is not used
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(1, 1, 8);
-    cfg.blockDim = dim3(SIM_THREADS_TILED);
-    cfg.dynamicSmemBytes = 195 * 1024;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 8;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    int clusters = 0;
-    if (cudaOccupancyMaxActiveClusters(&clusters, sim_kernel<false>, &cfg) != cudaSuccess || clusters < 1) {
-      ctx->sim_cluster = 0;
-      cudaGetLastError();
-    }
-  }
+  // the cluster forms of the sliced similarity launch and of the eviction need eight co-resident blocks of up to 195 KB each in one
+  // cluster; where the device (or the partition of it this process sees) cannot place one, the form is not used
+  if (e == cudaSuccess && ctx->sim_cluster) ctx->sim_cluster = cluster_fits(sim_kernel<false>, 8, SIM_THREADS_TILED, 195 * 1024);
+  if (e == cudaSuccess && ctx->evict_cluster) ctx->evict_cluster = cluster_fits(evict_select_kernel<true>, EV_CLUSTER, EV_THREADS, EV_KEYS_BYTES);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
     cudaFree(ctx->arena);

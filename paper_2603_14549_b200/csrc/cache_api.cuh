@@ -418,12 +418,12 @@ asap_status asap_cache_evict(asap_ctx *ctx, const asap_cache_evict_args *p, void
   a.new_len = p->new_len; a.status = ctx->status;
   // (where max_len <= keep every sequence stays whole, and its rows are not ranked)
   const long long rounds = ((long long)p->B * EV_CLUSTER + ctx->num_sms - 1) / ctx->num_sms;
-  const bool cluster = p->max_len > p->keep && p->max_len >= (rounds == 1 ? EV_CLUSTER_MIN : rounds * EV_CLUSTER_MIN_ROUND);
+  const bool cluster = ctx->evict_cluster && p->max_len > p->keep && p->max_len >= (rounds == 1 ? EV_CLUSTER_MIN : rounds * EV_CLUSTER_MIN_ROUND);
   const long long share = p->max_len > p->keep ? (((long long)p->max_len + (cluster ? EV_CLUSTER : 1) - 1) / (cluster ? EV_CLUSTER : 1) + 31) / 32 * 32 : 0;
   a.cached = share * 4 <= EV_KEYS_BYTES ? (int)share : 0;
   DeviceGuard guard(ctx->device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  mark(ctx, "evict_select", st);
+  mark(ctx, cluster ? "evict_select_cluster" : "evict_select", st);
   if (cluster)
     launch_pdl_cluster_z(evict_select_kernel<true>, dim3(1, p->B, EV_CLUSTER), dim3(EV_THREADS), (size_t)a.cached * 4, st, EV_CLUSTER, a);
   else

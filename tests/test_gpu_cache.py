@@ -610,6 +610,32 @@ def test_eviction(ctx, lens, keep, sink, recent, row, special, in_place):
     assert torch.equal(_bits(ow), _bits(want_w)) and torch.equal(op, want_p)
 
 
+@pytest.mark.parametrize("special", [False, True], ids=["random", "special"])
+@pytest.mark.parametrize("lens,keep", [([20000, 31, 7000], 900), ([60000, 50001], 4096)])
+def test_long_evictions_without_clusters(ctx, monkeypatch, lens, keep, special):
+    """A device that cannot place a cluster of eight large blocks: one block ranks a long sequence, and gives what the cluster gives."""
+    monkeypatch.setenv("ASAP_EVICT_CLUSTER", "0")
+    single = A.asap_init(0, 64, 1, 1, HEAD)
+    start, rows, w, pos = _evict_case(len(lens) + keep, lens, special)
+    got, names = [], []
+    try:
+        for c in (ctx, single):
+            keep_idx, new_len = torch.full((len(lens), keep), 77, dtype=torch.int32, device=DEV), i32([0] * len(lens))
+            A.asap_profile(c, True)
+            A.asap_cache_evict(c, A.CacheEvict(i32(start), i32(lens), max(lens), keep, w.to(DEV), pos.to(DEV), keep_idx, new_len, sink=3, recent=40))
+            A.asap_check(c)
+            names.append(list(A.asap_profile_read(c)))
+            A.asap_profile(c, False)
+            got.append((keep_idx.tolist(), new_len.tolist()))
+    finally:
+        A.asap_free(single)
+    assert names == [["evict_select_cluster"], ["evict_select"]]
+    assert got[0] == got[1]
+    for b, (s, n) in enumerate(zip(start, lens)):
+        e = R.evict(w[s:s + n].tolist(), pos[s:s + n].tolist(), keep, 3, 40)
+        assert got[1][0][b] == e + [-1] * (keep - len(e)) and got[1][1][b] == len(e)
+
+
 def test_eviction_of_a_large_batch_with_one_long_sequence(ctx):
     """A block per sequence, and one whose keys do not fit its shared memory."""
     lens = [55000] + [60 + i for i in range(79)]
