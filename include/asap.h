@@ -299,7 +299,8 @@ asap_status asap_rope(asap_ctx *ctx, const asap_rope_plan *plan, const asap_rope
  * once for all of them.  For query head h, with key/value head h / (H / kv_heads),
  *     out[t, h, :] = sum_j p_j v_j,   p = Softmax_j(scale * q . k_j) over all admitted rows,   lse[t, h] = ln sum_j exp(scale * q . k_j)
  * and, if `weights` is given, weights[j] += (1 / H) sum over the query rows and heads of p_j, for every cache row j (in a fixed
- * order: a call gives the same bits every time).  A query row that admits nothing gets out = 0 and lse = -infinity.  Rows that
+ * order: a call gives the same bits every time).  A query row that admits nothing gets out = 0 and lse = -infinity.  Where one of its
+ * logits is NaN or +infinity, out, lse and what it adds to the weights are NaN; one of -infinity has no probability.  Rows that
  * no query row admits are not looked at, whatever they hold; a row that only later query rows admit does not touch earlier ones.
  * Offsets (q_cu, group_cu) that do not ascend within [0, n_q] and [0, B] skip the whole call.
  * Probabilities enter the second product rounded to the element type; logits, sums and outputs before the last rounding are fp32. */

@@ -345,6 +345,30 @@ def test_values_of_late_rows_where_items_follow_each_other(ctx, value):
         assert torch.equal(c.out.nan_to_num(123.0, 456.0), want.nan_to_num(123.0, 456.0))
 
 
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), float("nan")], ids=["inf", "-inf", "nan"])
+@pytest.mark.parametrize("H,kv,nq", [(2, 2, 5), (16, 2, 1), (4, 2, 70)], ids=["few", "one", "many"])
+def test_rows_that_admit_an_infinite_key(ctx, value, H, kv, nq):
+    """A key with an infinite element: rows whose logit is minus infinity give it no probability, and rows whose logit is plus infinity or NaN are NaN,
+    in the output and in lse.  The others keep every bit."""
+    c = Case(lens=[150, 90], nq=[nq, 2], H=H, kv=kv, dtype=torch.bfloat16, seed=52, weights=False)
+    c.run(ctx)
+    good, good_lse = c.out.clone(), c.lse.clone()
+    key = c.len[0] - nq                                          # the first row's own: all rows of the sequence admit it
+    c.k[c.start[0] + key, :, 5] = value
+    c.run(ctx)
+    A.asap_check(ctx)
+    with_it = (c.q[:nq, :, 5].double() * value) != -math.inf      # (NaN counts)
+    assert value != value or (0 < int(with_it.sum()) < with_it.numel())
+    assert torch.isnan(c.out[:nq][with_it]).all() and torch.isnan(c.lse[:nq][with_it]).all()
+    assert torch.equal(c.out[nq:], good[nq:]) and torch.equal(c.lse[nq:], good_lse[nq:])
+    # without it: the same as the formula over the other keys, a logit of minus infinity in its place
+    ref = c.ref()
+    fine = ~with_it
+    assert torch.isfinite(ref[0][:nq][fine]).all()
+    assert ((c.out[:nq].double() - ref[0][:nq]).abs() <= 2.0 ** -8 * ref[0][:nq].abs() + 2.0 ** -7 * ref[3][:nq])[fine].all()
+    assert ((c.lse[:nq].double() - ref[1][:nq]).abs()[fine] <= 2.0 ** -15 * (1 + ref[1][:nq].abs()[fine])).all()
+
+
 def test_nan_queries_stay_in_their_rows(ctx):
     c = Case(lens=[150, 80], nq=[3, 1], H=4, kv=2, dtype=torch.bfloat16, seed=9, weights=False, groups=[(0, 2, 90)])
     c.run(ctx)
@@ -437,6 +461,36 @@ def test_capture_replay_and_another_stream(ctx):
     A.asap_cache_attention(ctx, args, scratch, other)
     other.synchronize()
     assert torch.equal(first, c.out)
+
+
+@pytest.mark.parametrize("H,kv,groups", [(8, 2, [(0, 2, 400)]), (8, 8, None), (8, 2, None)], ids=["tiles", "streamed", "few"])
+def test_weights_of_a_replayed_call(ctx, H, kv, groups):
+    """The weights under the lengths that a replay finds, added to what the rows had."""
+    c = Case(lens=[300, 70, 33], nq=[1, 1, 1] if kv == 2 else [9, 2, 3], H=H, kv=kv, dtype=torch.bfloat16, seed=53, groups=groups, slack=200)
+    c.k.copy_(torch.nan_to_num(c.k)); c.v.copy_(torch.nan_to_num(c.v))
+    args = c.args(max_len=400)
+    scratch = torch.empty(A.asap_cache_attention_scratch_bytes(ctx, args), dtype=torch.uint8, device=DEV)
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        A.asap_cache_attention(ctx, args, scratch)
+        s.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            A.asap_cache_attention(ctx, args, scratch)
+    rows = c.k.shape[0]
+    own = sum(p for _, _, _, p in c.groups) + 10                  # (own rows behind the prefixes, apart from each other)
+    for lens in ([300, 70, 33], [1, 0, 200], [17, 333, 64], [0, 0, 0]):
+        c.len, c.start = lens, [own + sum(lens[:b]) for b in range(3)]
+        assert c.start[2] + lens[2] <= rows
+        c.dev["len"].copy_(i32(lens)); c.dev["start"].copy_(i32(c.start))
+        before = torch.rand(rows, device=DEV, generator=gen(sum(lens)))
+        c.weights.copy_(before)
+        graph.replay()
+        torch.cuda.synchronize()
+        A.asap_check(ctx)
+        ref = c.ref()
+        R.check_attention(c.out, c.lse, ref, torch.bfloat16, 800)
+        R.check_weights(c.weights, before, ref, sum(c.nq))
 
 
 def test_a_padded_batch(ctx):
