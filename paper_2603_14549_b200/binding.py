@@ -511,6 +511,7 @@ class CacheEvict:
 
     def __init__(self, start, len, max_len, keep, weights, pos, keep_idx, new_len, src=(), dst=(), dst_start=None, dst_weights=None,
                  dst_pos=None, sink=0, recent=0):
+        src, dst = list(src), list(dst)          # (iterables that can be walked once would look empty the second time)
         B, n, rows = start.numel(), 0, weights.numel()
         _tensors_ok(weights.device, start, len, weights, pos, keep_idx, new_len, dst_start, dst_weights, dst_pos, *src, *dst)
         _dense(torch.int32, start=start, len=len, pos=pos, keep_idx=keep_idx, new_len=new_len, dst_start=dst_start, dst_pos=dst_pos)
@@ -531,7 +532,7 @@ class CacheEvict:
         ps = (C.c_void_p * max(n, 1))(*[t.data_ptr() for t in src])
         pd = (C.c_void_p * max(n, 1))(*[t.data_ptr() for t in dst])
         self.device = weights.device
-        self.keep = (start, len, weights, pos, keep_idx, new_len, list(src), list(dst), dst_start, dst_weights, dst_pos, ps, pd)
+        self.keep = (start, len, weights, pos, keep_idx, new_len, src, dst, dst_start, dst_weights, dst_pos, ps, pd)
         self.c = CCacheEvictArgs(B, max_len, keep, sink, recent, rows, dst_rows[0], n, row_bytes, _ptr(start), _ptr(len), _ptr(dst_start),
                                  _ptr(weights), _ptr(pos), _ptr(keep_idx), _ptr(new_len), _ptr(dst_weights), _ptr(dst_pos), ps, pd)
         self.ref = C.addressof(self.c)

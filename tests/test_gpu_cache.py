@@ -716,6 +716,21 @@ def test_eviction_without_positions_or_tensors(ctx):
         assert op[start[b]:start[b] + len(e)].tolist() == e
 
 
+def test_eviction_of_tensors_given_as_iterators(ctx):
+    """Tensors that a generator hands out are moved like those of a list."""
+    lens = [100, 80]
+    start, rows, w, pos = _evict_case(11, lens)
+    src, dst = [torch.randn(rows, 8, device=DEV, generator=gen(i)) for i in range(2)], [torch.full((rows, 8), 9.0, device=DEV) for _ in range(2)]
+    keep_idx, new_len = torch.empty(2, 20, dtype=torch.int32, device=DEV), i32([0, 0])
+    args = A.CacheEvict(i32(start), i32(lens), 100, 20, w.to(DEV), pos.to(DEV), keep_idx, new_len, src=iter(src), dst=(t for t in dst))
+    assert args.c.n_tensors == 2
+    A.asap_cache_evict(ctx, args)
+    A.asap_check(ctx)
+    for b in range(2):
+        at = slice(start[b], start[b] + 20)
+        assert all(torch.equal(d[at], s[start[b] + keep_idx[b].long()]) for s, d in zip(src, dst))
+
+
 def test_eviction_of_weights_in_place_beside_tensors_apart(ctx):
     lens = [300, 7, 1200]
     start, rows, w, pos = _evict_case(9, lens)
