@@ -275,7 +275,7 @@ asap_status asap_rope(asap_ctx *ctx, const asap_rope_plan *plan, const asap_rope
     t.rows = 1;
     if (p->n_rows >= 16 * ctx->num_sms) t.rows = t.heads >= 128 ? 1 : t.heads > 128 / ROPE_MAX_ROWS ? 128 / t.heads : ROPE_MAX_ROWS;
     t.first_block = (int)blocks;
-    blocks += (p->n_rows + t.rows - 1) / t.rows;
+    blocks += ((long long)p->n_rows + t.rows - 1) / t.rows;
   }
   if (blocks > 0x7fffffffLL) return fail(ctx, ASAP_ERR_UNSUPPORTED, "%s: too many rows", who);
   const bool vec = plan->n_pairs % (plan->interleaved ? 4 : 8) == 0;

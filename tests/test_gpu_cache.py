@@ -115,6 +115,20 @@ def test_far_positions_keep_their_angles(ctx):
     _close_rotation(out, R.rotate(x, pos, HEAD, "half", _freq(plan)), x, x.dtype, 1.0)
 
 
+def test_the_largest_number_of_rows(ctx):
+    """2^31 - 1 rows of one source row, whose count cannot be rounded up to whole blocks in 32 bits."""
+    n, plan = 2 ** 31 - 1, A.asap_rope_make(8)
+    x = torch.randn(1, 1, 8, device=DEV, generator=gen(5)).to(torch.bfloat16).expand(n, 1, 8)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    out = torch.zeros(n, 1, 8, dtype=torch.bfloat16, device=DEV)
+    A.asap_rope(ctx, plan, A.RopeArgs(pos, [A.RopeTensor(x, out)]))
+    A.asap_check(ctx)
+    at = torch.cat([torch.arange(5000, device=DEV), torch.randint(0, n, (20000,), device=DEV, generator=gen(6)), torch.arange(n - 5000, n, device=DEV)])
+    _close_rotation(out[at], R.rotate(x[at], pos[at], 8, "half", _freq(plan)), x[at], torch.bfloat16, 1.0)
+    del pos, out
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------------------------------------------------ attention
 class Case:
     """Random sequences in a cache whose unused rows hold NaN."""
