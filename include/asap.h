@@ -303,7 +303,9 @@ asap_status asap_rope(asap_ctx *ctx, const asap_rope_plan *plan, const asap_rope
  * logits is NaN or +infinity, out, lse and what it adds to the weights are NaN; one of -infinity has no probability.  Rows that
  * no query row admits are not looked at, whatever they hold; a row that only later query rows admit does not touch earlier ones.
  * Offsets (q_cu, group_cu) that do not ascend within [0, n_q] and [0, B] skip the whole call.
- * Probabilities enter the second product rounded to the element type; logits, sums and outputs before the last rounding are fp32. */
+ * Logits, sums and outputs before the last rounding are fp32.  Probabilities enter the second product as two terms of the element type
+ * (twice its bits) in a segment of up to 16 rows, query rows x heads of a key / value head; in one of more they are rounded to the
+ * element type.  A segment is the own rows of a sequence, or a prefix with the query rows of all its sequences. */
 typedef struct {
   int32_t B, H, kv_heads, head_dim, dtype;  /* head_dim must be 128; kv_heads divides H */
   int32_t n_q;                              /* rows of q and out; q_cu[B] may be smaller, the rows behind it stay as they are */

@@ -42,6 +42,14 @@ __device__ __forceinline__ uint32_t pack2_t(float a, float b) {
     return pack2_rn(a, b);
   }
 }
+// ... rounded towards zero
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2_rz(float a, float b) {
+  uint32_t d;
+  if constexpr (F16) asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
+  else asm("cvt.rz.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
+  return d;
+}
 template <bool F16>
 __device__ __forceinline__ float2 unpack2_t(uint32_t w) {
   if constexpr (F16) return __half22float2(*reinterpret_cast<const __half2 *>(&w));
@@ -617,7 +625,8 @@ __device__ __forceinline__ void ca_merge(float &m, float &l, float2 other, float
 // m16n8k16 instruction and up to 8 query rows as its 8 columns: a tile of 64 keys takes half the instructions, and half the
 // accumulators, of the form with (mostly empty) 16 query rows.  Rows 8 .. 15, where there are any, are a second set of columns for the
 // same key and value fragments.  A warp's logits of 16 keys x 8 rows become the second product's operand by transposing two 8 x 8
-// matrices between the lanes.  Every warp keeps its own running maximum and sums; the four meet at an item's end.
+// matrices between the lanes, as two terms of the element type (one request 12.6 -> 12.9 us, the others within 0.7 %; error of bf16 outputs
+// against 64 bits 2.0e-3 -> 1.7e-3 of their size, which is their own rounding).  Every warp keeps its own running maximum and sums; the four meet at an item's end.
 template <bool F16>
 __global__ void __launch_bounds__(CA_THREADS, 2)
 ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ CacheArgs a) {
@@ -862,7 +871,11 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
           for (int n = 0; n < 8; ++n) { o[h][n][0] *= f[0]; o[h][n][1] *= f[1]; o[h][n][2] *= f[0]; o[h][n][3] *= f[1]; }
         }
       }
-      uint32_t p0[SETS], p1[SETS];               // probabilities of keys gq and gq + 8, rows 2 tq and 2 tq + 1
+      // Probabilities of keys gq and gq + 8, rows 2 tq and 2 tq + 1, as two terms of the element type: truncated, and what that leaves.  The
+      // instructions of the second one fit into the waits for memory, and the output is as exact as one of probabilities in 32 bits.  The
+      // remainder of a probability above zero stays above zero, so that an infinite value stays one (0 * inf is NaN).
+      constexpr float LEAST = F16 ? 0x1p-24f : 0x1p-126f;
+      uint32_t p0[SETS], p1[SETS], r0[SETS], r1[SETS];
 #pragma unroll
       for (int h = 0; h < SETS; ++h) {
         float p[4];
@@ -873,8 +886,11 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
           p[2 + e] = fast_exp2(x[h][2 + e] - ref);
           l[h][e] += p[e] + p[2 + e];
         }
-        p0[h] = pack2_t<F16>(p[0], p[1]);
-        p1[h] = pack2_t<F16>(p[2], p[3]);
+        p0[h] = pack2_rz<F16>(p[0], p[1]);
+        p1[h] = pack2_rz<F16>(p[2], p[3]);
+        const float2 a0 = unpack2_t<F16>(p0[h]), a1 = unpack2_t<F16>(p1[h]);
+        r0[h] = pack2_t<F16>(fmaxf(p[0] - a0.x, fminf(p[0], LEAST)), fmaxf(p[1] - a0.y, fminf(p[1], LEAST)));
+        r1[h] = pack2_t<F16>(fmaxf(p[2] - a1.x, fminf(p[2], LEAST)), fmaxf(p[3] - a1.y, fminf(p[3], LEAST)));
       }
       // ---- values.  Rows that no query row of the tile admits are cleared (0 * NaN is NaN).  A row that only some of them
       // admit may hold infinities or NaN too: then its part is added without the matrix instruction, to the rows that admit it.
@@ -900,7 +916,10 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
             const int k = __ffs(left) - 1;
 #pragma unroll
             for (int h = 0; h < SETS; ++h) {
-              const float2 pk = unpack2_t<F16>(__shfl_sync(0xffffffffu, (k & 8) ? p1[h] : p0[h], (k & 7) * 4 + tq));
+              float2 pk = unpack2_t<F16>(__shfl_sync(0xffffffffu, (k & 8) ? p1[h] : p0[h], (k & 7) * 4 + tq));
+              const float2 rk = unpack2_t<F16>(__shfl_sync(0xffffffffu, (k & 8) ? r1[h] : r0[h], (k & 7) * 4 + tq));
+              pk.x += rk.x;
+              pk.y += rk.y;
               const bool in0 = j0 + k < adm[h][0], in1 = j0 + k < adm[h][1];
 #pragma unroll
               for (int n = 0; n < 8; ++n)
@@ -923,7 +942,10 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
       }
       uint32_t b0[SETS], b1[SETS];
 #pragma unroll
-      for (int h = 0; h < SETS; ++h) { b0[h] = transpose8x8(p0[h]); b1[h] = transpose8x8(p1[h]); }
+      for (int h = 0; h < SETS; ++h) {
+        b0[h] = transpose8x8(p0[h]); b1[h] = transpose8x8(p1[h]);
+        r0[h] = transpose8x8(r0[h]); r1[h] = transpose8x8(r1[h]);
+      }
       {
         const int key = (mi >> 1) * 8 + mr;
         const uint32_t row = vs + key * 128;
@@ -934,6 +956,8 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
           ldsm4t(row + (n >> 2) * half_bytes + (((c & 7) ^ (key & 7)) << 4), v);
 #pragma unroll
           for (int h = 0; h < SETS; ++h) mma16816<F16>(o[h][n], v, b0[h], b1[h]);
+#pragma unroll
+          for (int h = 0; h < SETS; ++h) mma16816<F16>(o[h][n], v, r0[h], r1[h]);
         }
       }
     };
@@ -1054,7 +1078,9 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
 // ---------------------------------------------------------------------------------------
 // Segments of more than 16 stacked rows.  Persistent blocks; two row tiles of 128 rows share every key and value tile of 128 keys and take
 // turns on the tensor pipe: S = Q K^T into tensor memory, one thread per row turns it into probabilities relative to a reference
-// maximum, P goes back to tensor memory in the element type, O += P V accumulates there.
+// maximum, P goes back to tensor memory in the element type, O += P V accumulates there.  (P rounded to the element type: the second product
+// takes no other.  A second term would be half as many products again, and tensor memory is full.  Error of bf16 outputs against 64 bits 2.3e-3 of
+// their size, 1.7e-3 of which is their own rounding.)
 // What bounds it: a pair of key tiles takes 2300 to 2750 clocks, near the products' own rate, but an item's ends cost 8000 to 10000 more (the
 // first tile's maximum, 128 KB of results a block, nothing for the tensor pipe to do meanwhile) and a launch 11 us before its first
 // product: 13 sequences of 16 to 256 query rows over prefixes of 2915 rows, 32 heads: 146 us of the call's 193, where the

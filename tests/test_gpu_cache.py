@@ -359,6 +359,58 @@ def test_values_of_late_rows_where_items_follow_each_other(ctx, value):
         assert torch.equal(c.out.nan_to_num(123.0, 456.0), want.nan_to_num(123.0, 456.0))
 
 
+STREAMED = {
+    "few_keys": dict(lens=[2, 3, 5, 17, 33, 9], nq=[1] * 6, H=8, kv=8),
+    "one_head": dict(lens=[200, 7, 60], nq=[2, 1, 1], H=14, kv=2),
+    "two_sets_of_rows": dict(lens=[150, 31], nq=[3, 2], H=40, kv=8),
+    "two_heads_together": dict(lens=[120, 40], nq=[2, 2], H=16, kv=4),
+    "four_heads_together": dict(lens=[190, 20, 3], nq=[1] * 3, H=16, kv=16),
+    "prefix": dict(lens=[10, 20, 3, 40], nq=[1] * 4, H=8, kv=4, groups=[(0, 4, 100)]),
+}
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("name", STREAMED)
+def test_streamed_rows_lose_nothing_but_the_last_rounding(ctx, name, dtype):
+    """Up to 16 stacked rows: the output is off by its own rounding, as if the probabilities had 32 bits.  (Small logits: a probability's relative
+    error from its logit, 2^-15 of the logit's size as for the weights, is then far below a step of the element type.)  Rounded to the element
+    type the probabilities would be off by up to half a step each, 2^-8 or 2^-11 of theirs."""
+    c = Case(**STREAMED[name], dtype=dtype, seed=60, weights=False)
+    c.run(ctx, scale=0.005)
+    A.asap_check(ctx)
+    out, _, _, pv, size = c.ref(scale=0.005)
+    eps, sub = torch.finfo(dtype).eps, torch.finfo(dtype).tiny * torch.finfo(dtype).eps / 2
+    # the two terms (a step, and half a step of that), 32-bit sums, and the smallest numbers of the type as elsewhere
+    rel = eps * eps / 2 + 2.0 ** -15 * float(size.max()) + 2.0 ** -16 + 2.0 ** -15
+    assert rel < 2.0 ** -13
+    tol = eps / 2 * out.abs() * (1 + eps) + rel * pv + sub * (1 + 8.0 * 200)
+    bad = ~((c.out.double() - out).abs() <= tol)
+    assert not bad.any(), (int(bad.sum()), ((c.out.double() - out).abs() / tol).max().item())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf")], ids=["inf", "-inf"])
+@pytest.mark.parametrize("H,kv,nq,n", [(2, 2, 1, 1), (8, 8, 1, 300), (8, 2, 2, 150), (10, 1, 1, 70), (4, 2, 70, 200)],
+                         ids=["one_key", "four_heads", "two_heads", "one_head", "tiles"])
+def test_rows_that_admit_an_infinite_value(ctx, value, dtype, H, kv, nq, n):
+    """A value with an infinite element among the keys of every row, the one of the largest logit (a probability that the type holds exactly if it is
+    1) or another: that element of the output is infinite, the others keep every bit."""
+    for which in (0, n // 2):
+        c = Case(lens=[n, 40], nq=[nq, 1], H=H, kv=kv, dtype=dtype, seed=54, weights=False)
+        if which == 0:
+            c.k[c.start[0]] = c.q[0, ::H // kv] * 0.25
+        c.v[c.start[0] + which, :, 5] = 0.0
+        c.run(ctx, scale=0.02)
+        good = c.out.clone()
+        assert torch.isfinite(good).all()
+        c.v[c.start[0] + which, :, 5] = value
+        c.run(ctx, scale=0.02)
+        A.asap_check(ctx)
+        want = good.clone()
+        want[:nq, :, 5] = value
+        assert torch.equal(c.out, want)
+
+
 @pytest.mark.parametrize("value", [float("inf"), -float("inf"), float("nan")], ids=["inf", "-inf", "nan"])
 @pytest.mark.parametrize("H,kv,nq", [(2, 2, 5), (16, 2, 1), (4, 2, 70)], ids=["few", "one", "many"])
 def test_rows_that_admit_an_infinite_key(ctx, value, H, kv, nq):
