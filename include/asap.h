@@ -341,7 +341,7 @@ asap_status asap_cache_attention(asap_ctx *ctx, const asap_cache_attention_args 
  * position of the sequence), then by weight, largest first (-0 equals +0, NaN is below everything); lower row first among
  * equals.  For row i of the kept ones, each of the n_tensors (0 .. 64) tensors moves row start[b] + keep_idx[b][i] to row
  * dst_start[b] + i, and weights and pos likewise.  dst[t] == src[t] moves in place (dst_start NULL then; the sequences must not overlap);
- * partly overlapping tensors are refused.  keep and max_len are at most 2^30. */
+ * partly overlapping tensors are refused.  Rows to which one sequence's go must not belong to another's.  keep and max_len are at most 2^30. */
 typedef struct {
   int32_t B, max_len, keep, sink, recent;  /* 0 <= sink, 0 <= recent, sink + recent <= keep, 0 < keep */
   int32_t rows, dst_rows;                  /* rows of the sources / of the destinations */
@@ -351,7 +351,8 @@ typedef struct {
   const int32_t *dst_start;                /* [B]; NULL: start */
   const float *weights;                    /* [rows] */
   const int32_t *pos;                      /* [rows]; NULL: a row's number in its sequence */
-  int32_t *keep_idx;                       /* [B, keep] kept rows, sequence-relative, ascending; -1 behind the last */
+  int32_t *keep_idx;                       /* [B, keep] kept rows, sequence-relative, ascending; -1 behind the last, and
+                                              everywhere for a sequence that is skipped */
   int32_t *new_len;                        /* [B]; may be `len` */
   float *dst_weights;                      /* [dst_rows], may be NULL or `weights` */
   int32_t *dst_pos;                        /* [dst_rows], may be NULL or `pos` */

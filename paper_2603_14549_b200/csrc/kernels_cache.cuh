@@ -81,7 +81,7 @@ struct RopeArgs {
 // One element pair, or eight elements at a time (VEC) where the pairs allow it: half layout n_pairs % 8 == 0, interleaved
 // n_pairs % 4 == 0.  The angles of a row are taken once for all its heads: pos * turns modulo 2^64 is the fraction of a turn, whose
 // upper 32 bits, as a signed number, are the angle in [-1/2, 1/2) turns (2^-32 turns off at most); sincospi takes it in fp32.
-// What bounds it on prompts is the memory, kept busy by many warps with little in hand: 24531 rows of 32 + 2 x 32 heads 208 us, 89 % of a
+// What bounds it on prompts is the memory, kept busy by many warps with little in hand: 24531 rows of 32 + 2 x 32 heads 214 us, 87 % of a
 // copy's rate.  (Four rows of a piece under way together per thread, 74 registers, 237 us; warps with angles of their own, 94 registers, 315.)
 // A block takes about 128 heads of one tensor: four rows of 32 heads, sixteen of 8 or fewer.
 template <bool F16, bool VEC>
@@ -619,9 +619,10 @@ __device__ __forceinline__ void ca_merge(float &m, float &l, float2 other, float
   m = top;
 }
 
-// What bounds it is the memory where the cache is long: 64 sequences of 643 to 1100 rows of 32 heads, 0.89 GB, 152 us a call with its join and
-// weights (5.8 TB/s), 5 sequences of 2000 to 60000 rows of 8 heads, 0.63 GB, 106 us (5.9 TB/s).  A short call is the sum of its launches'
-// latencies: one token over 267 rows 12.5 us.  S^T = K Q^T and O^T = V^T P^T, with the keys and then the columns as the 16 rows of an
+// What bounds it is the memory where the cache is long: 64 sequences of 643 to 1100 rows of 32 heads, 0.89 GB, 155 us a call with its join and
+// weights (5.7 TB/s), 5 sequences of 2000 to 60000 rows of 8 heads, 0.63 GB, 108 us (5.8 TB/s).  A short call is the sum of its launches'
+// latencies: one token over 267 rows 12.8 us.  Two blocks fit on a processor up to 204 sequences and groups, whose list lies in shared memory too; above
+// that one does, and the rate falls (32 key / value heads, rows of 400 to 600: 204 sequences 6.38 TB/s, 205 5.95; 8 heads 5.30, 4.44).  S^T = K Q^T and O^T = V^T P^T, with the keys and then the columns as the 16 rows of an
 // m16n8k16 instruction and up to 8 query rows as its 8 columns: a tile of 64 keys takes half the instructions, and half the
 // accumulators, of the form with (mostly empty) 16 query rows.  Rows 8 .. 15, where there are any, are a second set of columns for the
 // same key and value fragments.  A warp's logits of 16 keys x 8 rows become the second product's operand by transposing two 8 x 8
@@ -1083,8 +1084,8 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
 // their size, 1.7e-3 of which is their own rounding.)
 // What bounds it: a pair of key tiles takes 2300 to 2750 clocks, near the products' own rate, but an item's ends cost 8000 to 10000 more (the
 // first tile's maximum, 128 KB of results a block, nothing for the tensor pipe to do meanwhile) and a launch 11 us before its first
-// product: 13 sequences of 16 to 256 query rows over prefixes of 2915 rows, 32 heads: 146 us of the call's 193, where the
-// products alone are 69 at the measured rate.  (Results through shared memory, queries gathered and items counted two tiles longer
+// product: 13 sequences of 16 to 256 query rows over prefixes of 2915 rows, 32 heads: 142 us of the call's 198, where the
+// products alone are 69 at the measured rate; the tensor pipe is active for 49 % of the cycles.  (Results through shared memory, queries gathered and items counted two tiles longer
 // than their keys, in place of four: 175.)
 // ---------------------------------------------------------------------------------------
 constexpr int CT_THREADS = 384;                 // warp 0: key / value copies, 1: MMA issue, 2: value rows to be cleared, 3: query rows, 4-11: softmax
