@@ -536,18 +536,18 @@ __device__ __forceinline__ int ca_wait_on(uint32_t bar, uint32_t parity, volatil
   for (int i = 0; !(ok = mbar_test_wait(bar, parity)) && i < CA_QUEUE_LOOKS; ++i) __nanosleep(1000);
   return __all_sync(0xffffffffu, ok) ? 2 : 0;
 }
-// A consumer warp: whether it takes item n.  The first late warp decides for all of them (`verdict`: 2 n + 2 none takes it, 2 n + 3 all do), and a
+// A consumer warp: whether it takes item n.  The first late warp decides for all of them (`decision`: 2 n + 2 none takes it, 2 n + 3 all do), and a
 // warp that is in time has seen an item that no other one has given up yet.
-__device__ __forceinline__ bool ca_wait_on_item(unsigned int *verdict, int n, uint32_t bar, uint32_t parity, volatile int *abort_flag, uint32_t *status,
+__device__ __forceinline__ bool ca_wait_on_item(unsigned int *decision, int n, uint32_t bar, uint32_t parity, volatile int *abort_flag, uint32_t *status,
                                              long long limit) {
   const int how = ca_wait_on(bar, parity, abort_flag, status, limit);
   if (how == 1) return true;
   const unsigned int mine = 2u * n + 2u + (how == 2 ? 1u : 0u);
   unsigned int said = 0u;
   if ((threadIdx.x & 31) == 0) {
-    said = *reinterpret_cast<volatile unsigned int *>(verdict);
+    said = *reinterpret_cast<volatile unsigned int *>(decision);
     while (said >> 1 != mine >> 1) {
-      const unsigned int before = atomicCAS(verdict, said, mine);
+      const unsigned int before = atomicCAS(decision, said, mine);
       said = before == said ? mine : before;
     }
   }
@@ -566,7 +566,7 @@ struct CaMaps {
 struct CaBook {
   uint64_t full[CA_STAGES], empty[CA_STAGES], job_full[CA_JOBS], job_empty[CA_JOBS];
   int warp_part[7];
-  unsigned int verdict;                    // see ca_wait_on_item
+  unsigned int decision;                    // see ca_wait_on_item
   int abort_flag;
   float2 ml[2][StreamWork::ROWS];
   CaJob job[CA_JOBS];
@@ -649,7 +649,7 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
       mbar_init(smem_u32(&bk->job_empty[s]), CA_CONSUMERS);
     }
     bk->abort_flag = 0;
-    bk->verdict = 0u;
+    bk->decision = 0u;
     fence_barrier_init();
   }
   if (threadIdx.x < 3) {
@@ -752,7 +752,7 @@ ca_stream_kernel(const __grid_constant__ CaMaps maps, const __grid_constant__ Ca
   for (int jc = 0;; ++jc) {
     const int slot = jc % CA_JOBS;
     if (!mbar_try_all(smem_u32(&bk->job_full[slot]), (jc / CA_JOBS) & 1) &&
-        !ca_wait_on_item(&bk->verdict, jc, smem_u32(&bk->job_full[slot]), (jc / CA_JOBS) & 1, &bk->abort_flag, a.status, a.wait_limit))
+        !ca_wait_on_item(&bk->decision, jc, smem_u32(&bk->job_full[slot]), (jc / CA_JOBS) & 1, &bk->abort_flag, a.status, a.wait_limit))
       break;
     const CaJob j = bk->job[slot];
     if (j.n < 0) break;
